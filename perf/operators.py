@@ -71,7 +71,8 @@ def _log_int(rng, lo, hi):
     return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
 
 
-MOST_SCORES = {"bf16": 16 * 16 * 512 * 512, "fp32": 1 << 22}
+MOST_SCORES = {"bf16": 16 * 16 * 512 * 384, "fp32": 1 << 22}  # of a drawn batch, and values of its widest tensor
+MOST_VALUES = {"bf16": 16 * 512 * 1024, "fp32": 16 * 512 * 256}
 
 
 def draw(rng):
@@ -100,7 +101,8 @@ def draw(rng):
     while most < 1:
         q_len, kv_len = max(5, q_len // 2), max(5, kv_len // 2)
         most = MOST_SCORES[dtype] // (q_len * kv_len * heads)
-    return dict(op=op, batch=_log_int(rng, 1, min(most, 32)), q_len=q_len, kv_len=kv_len, heads=heads,
+    most = min(most, MOST_VALUES[dtype] // (max(q_len * heads, kv_len * kv_heads) * dim), 32)
+    return dict(op=op, batch=_log_int(rng, 1, max(1, most)), q_len=q_len, kv_len=kv_len, heads=heads,
                 kv_heads=kv_heads, dim=dim, dtype=dtype, len_lo=rng.randint(kv_len // 4, kv_len))
 
 
