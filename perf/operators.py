@@ -91,7 +91,7 @@ def draw(rng):
     if op == "cross_token":
         q_len = rng.choice([1, 1, 1, 2, 4])
         kv_len = _log_int(rng, 1, 20000)
-        most = max(1, min(64, 4 * 4 * 20000 // (kv_len * kv_heads)))
+        most = max(1, min(64, 4 * 4 * 20000 * 128 // (kv_len * kv_heads * dim * DT[dtype].itemsize)))
         batch = _log_int(rng, 1, most)
         return dict(op="cross_fwd", batch=batch, q_len=q_len, kv_len=kv_len, heads=heads, kv_heads=kv_heads, dim=dim,
                     dtype=dtype, len_lo=rng.randint(0, kv_len))
