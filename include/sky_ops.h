@@ -98,6 +98,57 @@ sky_status sky_attention_bwd(const void* qkv, const void* ctx, const void* dctx,
                              void* workspace, size_t workspace_bytes, int32_t* d_status,
                              void* stream);
 
+/* ---- Heads before the attention ------------------------------------------
+ * How a head's values are paired for the rotation by position: value i with
+ * value i + D/2, or neighbours 2i and 2i + 1.  Pair i turns by the angle
+ * pos * theta^(-2i/D). */
+typedef enum { SKY_ROTATE_NONE = 0, SKY_ROTATE_HALVES = 1, SKY_ROTATE_PAIRS = 2 } sky_rotation;
+
+/* Rows of query and key heads: a row holds q_heads query heads, then k_heads
+ * key heads, of head_dim values each, and may be wider than they are (a packed
+ * QKV row with its V block, a K | V row): what lies behind them is neither read
+ * nor written.  Either number of heads may be 0. */
+typedef struct {
+  int32_t rows, q_heads, k_heads, head_dim;
+  sky_dtype dtype;       /* of heads and gains                            */
+  int64_t ldx, ldy;      /* values from one row to the next: of x and dx; of y and dy */
+  float eps;             /* added to the mean square, >= 0                */
+  sky_rotation rotation;
+  double theta;          /* > 0; ignored without a rotation               */
+} sky_qk_norm_shape;
+
+/* Norm of every head with the rotation in the same pass: a head x becomes
+ * y = R(pos) (g * x / sqrt(mean(x^2) + eps)), with the gain g = q_gain of the
+ * query heads and k_gain of the key heads (each [head_dim]; NULL: ones) and R
+ * the rotation by the row's position d_pos[row] (int32[rows], any value; may be
+ * NULL without a rotation).  Statistics, angles and products are fp32 or finer;
+ * angles keep their precision at every position.  y may be x where ldy == ldx,
+ * and must not overlap it otherwise.  Serves a batch of new tokens (a row each)
+ * as it does a training batch.
+ * Errors: INVALID_ARG (null, sizes, an unknown dtype or rotation, rows shorter
+ * than their heads), UNSUPPORTED (head_dim not a multiple of 16 or above 256,
+ * x or y not 16-byte aligned, ldx or ldy not a multiple of 16 bytes, rows of
+ * more than 2^24 values). */
+sky_status sky_qk_norm_fwd(const sky_qk_norm_shape* shape, const void* x, const void* q_gain,
+                           const void* k_gain, const int32_t* d_pos, void* y, void* stream);
+
+/* Scratch bytes of sky_qk_norm_bwd (partial gain gradients); 0 for a shape that
+ * it refuses. */
+size_t sky_qk_norm_bwd_workspace_bytes(const sky_qk_norm_shape* shape);
+
+/* Its backward, from the forward's input x (rows of ldx) and dy = dL/dy (rows
+ * of ldy): with dz = R(-pos) dy, xhat = x / sqrt(mean(x^2) + eps) and
+ * h = dz * g writes dx = (h - xhat mean(h xhat)) / sqrt(mean(x^2) + eps) (rows
+ * of ldx; may be dy where ldy == ldx, or x) and the fp32 gain gradients, the
+ * sums of dz * xhat over all rows and query (key) heads, to dq_gain and dk_gain
+ * ([head_dim]; either may be NULL), in a fixed order (deterministic).
+ * Errors as the forward's; INVALID_ARG for a workspace that is too small or not
+ * 4-byte aligned. */
+sky_status sky_qk_norm_bwd(const sky_qk_norm_shape* shape, const void* x, const void* dy,
+                           const void* q_gain, const void* k_gain, const int32_t* d_pos,
+                           void* dx, float* dq_gain, float* dk_gain, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 /* Residual + LayerNorm forward (post-LN placement): u = a + r with a the
  * linear layer's fp32 output and r the fp32 residual stream (r may be NULL);
  * y = gamma * (u - mean) * rstd + beta, rstd = 1/sqrt(var + eps), biased

@@ -18,6 +18,7 @@ SKY_OK, SKY_ERR_INVALID_ARG, SKY_ERR_OOM, SKY_ERR_CUDA, SKY_ERR_STATE, SKY_ERR_T
 SKY_DTYPE_BF16, SKY_DTYPE_FP32 = 0, 1
 SKY_GEMM_XWT, SKY_GEMM_XW, SKY_GEMM_XTW = 0, 1, 2
 SKY_EPI_STORE, SKY_EPI_BIAS_GELU, SKY_EPI_GELU_BWD = 0, 1, 2
+SKY_ROTATE_NONE, SKY_ROTATE_HALVES, SKY_ROTATE_PAIRS = 0, 1, 2
 SKY_NUM_PARAMS = 12
 
 
@@ -69,6 +70,14 @@ class SkyOptimizerConfig(C.Structure):
                 ("beta2", C.c_float), ("eps", C.c_float), ("weight_decay", C.c_float),
                 ("momentum", C.c_float)]
 
+
+class SkyQkNormShape(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int), ("ldx", C.c_int64),
+                ("ldy", C.c_int64), ("eps", C.c_float), ("rotation", C.c_int),
+                ("theta", C.c_double)]
+
+
 _VP, _I32, _SZ = C.c_void_p, C.c_int32, C.c_size_t
 _SIGNATURES = {
     "sky_slice_create": (C.c_int, [C.POINTER(SkySliceConfig), C.POINTER(_VP)]),
@@ -101,6 +110,10 @@ _SIGNATURES = {
     "sky_attention_bwd_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32]),
     "sky_attention_bwd": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _I32, _I32, _I32, _I32, C.c_int,
                                     _VP, _VP, _SZ, _VP, _VP]),
+    "sky_qk_norm_fwd": (C.c_int, [C.POINTER(SkyQkNormShape), _VP, _VP, _VP, _VP, _VP, _VP]),
+    "sky_qk_norm_bwd_workspace_bytes": (_SZ, [C.POINTER(SkyQkNormShape)]),
+    "sky_qk_norm_bwd": (C.c_int, [C.POINTER(SkyQkNormShape), _VP, _VP, _VP, _VP, _VP, _VP, _VP,
+                                  _VP, _VP, _SZ, _VP]),
     "sky_layernorm_fwd": (C.c_int, [_VP, _VP, _VP, _VP, _I32, _I32, C.c_float, C.c_int, _VP,
                                     _VP, _VP, _VP, _VP, _VP]),
     "sky_layernorm_bwd_workspace_bytes": (_SZ, [_I32, _I32]),

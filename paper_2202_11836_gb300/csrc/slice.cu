@@ -15,14 +15,13 @@
 #include <cstdarg>
 #include <cstdlib>
 #include <cstring>
-#include <exception>
-#include <new>
 #include <string>
 #include <vector>
 
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include "abi.h"
 #include "common.cuh"
 #include "gemm.h"
 #include "optimizer.h"
@@ -723,22 +722,6 @@ bool device_range(const void* p, size_t bytes, int device) {
 }  // namespace sky
 
 using namespace sky;
-
-#define ABI_GUARD_BEGIN try {
-#define ABI_GUARD_END                                              \
-  }                                                                \
-  catch (const std::bad_alloc&) {                                  \
-    set_error("host allocation failed");                           \
-    return SKY_ERR_OOM;                                            \
-  }                                                                \
-  catch (const std::exception& ex) {                               \
-    set_error("internal error: %s", ex.what());                    \
-    return SKY_ERR_CUDA;                                           \
-  }                                                                \
-  catch (...) {                                                    \
-    set_error("internal error");                                   \
-    return SKY_ERR_CUDA;                                           \
-  }
 
 extern "C" {
 

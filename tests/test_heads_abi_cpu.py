@@ -1,0 +1,69 @@
+"""What the head norms refuse, before any device is touched."""
+import ctypes as C
+import os
+
+import pytest
+
+from paper_2202_11836_gb300 import _lib as L
+
+INVALID, UNSUPPORTED = L.SKY_ERR_INVALID_ARG, L.SKY_ERR_UNSUPPORTED
+AT = C.c_void_p(1 << 20)  # an address that no refused call reads
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(L.LIB_PATH):
+        from paper_2202_11836_gb300 import build
+        build.build()
+    return L.lib()
+
+
+def norm_shape(**kw):
+    base = dict(rows=4, q_heads=2, k_heads=2, head_dim=64, dtype=L.SKY_DTYPE_BF16, ldx=256, ldy=256, eps=1e-6,
+                rotation=L.SKY_ROTATE_HALVES, theta=10000.0)
+    base.update(kw)
+    return L.SkyQkNormShape(**base)
+
+
+NORM_REFUSED = [
+    (dict(rows=0), INVALID), (dict(rows=-1), INVALID), (dict(q_heads=-1), INVALID),
+    (dict(q_heads=0, k_heads=0), INVALID), (dict(head_dim=0), INVALID), (dict(dtype=2), INVALID),
+    (dict(rotation=3), INVALID), (dict(rotation=-1), INVALID), (dict(eps=-1.0), INVALID),
+    (dict(eps=float("nan")), INVALID), (dict(theta=0.0), INVALID), (dict(theta=float("inf")), INVALID),
+    (dict(theta=float("nan")), INVALID), (dict(ldx=255), INVALID), (dict(ldy=248), INVALID), (dict(ldx=-256), INVALID),
+    (dict(head_dim=8), UNSUPPORTED), (dict(head_dim=72, ldx=512, ldy=512), UNSUPPORTED),
+    (dict(head_dim=272, ldx=2048, ldy=2048), UNSUPPORTED), (dict(ldx=260), UNSUPPORTED),
+    (dict(ldx=258, dtype=L.SKY_DTYPE_FP32), UNSUPPORTED), (dict(ldy=257), UNSUPPORTED),
+    (dict(q_heads=1 << 30, k_heads=1 << 30, ldx=1 << 60, ldy=1 << 60), UNSUPPORTED),
+]
+
+
+@pytest.mark.parametrize("bad,status", NORM_REFUSED, ids=lambda v: str(v))
+def test_norm_refuses_shapes(lib, bad, status):
+    s = norm_shape(**bad)
+    assert lib.sky_qk_norm_fwd(s, AT, AT, AT, AT, AT, None) == status
+    assert L.last_error()
+    assert lib.sky_qk_norm_bwd_workspace_bytes(s) == 0
+    assert lib.sky_qk_norm_bwd(s, AT, AT, AT, AT, AT, AT, AT, AT, AT, 1 << 40, None) == status
+
+
+def test_norm_refuses_arguments(lib):
+    s, odd = norm_shape(), C.c_void_p((1 << 20) + 8)
+    need = lib.sky_qk_norm_bwd_workspace_bytes(s)
+    assert need > 0 and lib.sky_qk_norm_bwd_workspace_bytes(None) == 0
+    fwd, bwd = lib.sky_qk_norm_fwd, lib.sky_qk_norm_bwd
+    assert fwd(None, AT, AT, AT, AT, AT, None) == INVALID
+    assert fwd(s, None, AT, AT, AT, AT, None) == INVALID
+    assert fwd(s, AT, AT, AT, AT, None, None) == INVALID
+    assert fwd(s, AT, AT, AT, None, AT, None) == INVALID  # a rotation without positions
+    assert fwd(s, odd, AT, AT, AT, AT, None) == UNSUPPORTED
+    assert fwd(s, AT, AT, AT, AT, odd, None) == UNSUPPORTED
+    assert fwd(norm_shape(ldy=264), AT, AT, AT, AT, AT, None) == INVALID  # in place, rows not where they were
+    ok = [AT, C.c_void_p(2 << 20), AT, AT, AT, C.c_void_p(3 << 20), AT, AT, AT]
+    for i in (0, 1, 5, 8):
+        assert bwd(s, *[None if j == i else a for j, a in enumerate(ok)], need, None) == INVALID
+    assert bwd(s, *[None if j == 4 else a for j, a in enumerate(ok)], need, None) == INVALID
+    for i in (0, 1, 5):
+        assert bwd(s, *[odd if j == i else a for j, a in enumerate(ok)], need, None) == UNSUPPORTED
+    assert bwd(s, *ok[:8], C.c_void_p((1 << 20) + 2), need, None) == INVALID
+    assert bwd(s, *ok, need - 1, None) == INVALID
