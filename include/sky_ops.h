@@ -98,6 +98,58 @@ sky_status sky_attention_bwd(const void* qkv, const void* ctx, const void* dctx,
                              void* workspace, size_t workspace_bytes, int32_t* d_status,
                              void* stream);
 
+/* ---- Attention over keys of another length ----------------------------------
+ * Queries [batch, q_len] (a decoder's) over keys and values [batch, kv_len] (an
+ * encoder's states, projected): rows ldq, ldk, ldv, ldo values apart, sequence
+ * after sequence, with the heads of a row side by side (head a at columns
+ * a*D..a*D+D-1), so a row may be part of a wider one (the K and V blocks of a
+ * K | V row, the blocks of a QKV row): what lies beside the heads is neither
+ * read nor written.  heads may be a multiple of kv_heads: query head a then
+ * reads key head a / (heads / kv_heads). */
+typedef struct {
+  int32_t batch, q_len, kv_len, heads, kv_heads, head_dim;
+  sky_dtype dtype;
+  int64_t ldq;           /* of q and dq      */
+  int64_t ldk, ldv;      /* of k, dk; v, dv  */
+  int64_t ldo;           /* of ctx and dctx  */
+} sky_cross_shape;
+
+/* ctx = softmax(q k^T / sqrt(D)) v over the valid keys j < d_len[b]
+ * (int32[batch], each in [0, kv_len]; a sequence without keys gets ctx = 0), and
+ * lse: fp32 [batch, heads, q_len], the normaliser of each row in the base-2
+ * units of sky_attention_fwd, -inf without keys (NULL if not wanted; the
+ * backward needs it).  Keys past the valid length may hold anything, infinities
+ * and NaN included.  All q_len rows are computed.  One query row a sequence is
+ * the step of a decoder that writes token by token: its rows of k and v are
+ * computed once and kept, kv_len being the room that they have.
+ * bf16 with head_dim 64 and every tensor and row distance on the 16-byte grid
+ * runs on the tensor cores; other head dims, up to 128, and other alignments run
+ * slower kernels of the same result.
+ * Errors: INVALID_ARG (null, sizes, heads no multiple of kv_heads, rows shorter
+ * than their heads, a tensor off its type's grid), UNSUPPORTED (head_dim above
+ * 128, batch above 65535, lengths above 2^24, heads above 1024, rows of more
+ * than 2^30 values, batch * q_len * heads of 2^33 or more); a length outside [0, kv_len] is clamped and sets bit 0 of
+ * *d_status. */
+sky_status sky_cross_attention_fwd(const sky_cross_shape* shape, const void* q, const void* k,
+                                   const void* v, const int32_t* d_len, void* ctx, float* lse,
+                                   int32_t* d_status, void* stream);
+
+/* Scratch bytes of sky_cross_attention_bwd; 0 for a shape that it refuses.  The
+ * workspace must be 16-byte aligned. */
+size_t sky_cross_attention_bwd_workspace_bytes(const sky_cross_shape* shape);
+
+/* Its backward, from dctx, the forward's inputs and its ctx and lse: dq (rows
+ * of ldq), and dk, dv (rows of ldk, ldv), summed over the query heads of each
+ * key head; keys past the valid length, and queries without keys, get zeros.
+ * Deterministic.  The gradients may not overlap the inputs or each other.
+ * Errors as the forward's; INVALID_ARG for a workspace that is too small or not
+ * 16-byte aligned. */
+sky_status sky_cross_attention_bwd(const sky_cross_shape* shape, const void* q, const void* k,
+                                   const void* v, const void* ctx, const void* dctx,
+                                   const float* lse, const int32_t* d_len, void* dq, void* dk,
+                                   void* dv, void* workspace, size_t workspace_bytes,
+                                   int32_t* d_status, void* stream);
+
 /* ---- Heads before the attention ------------------------------------------
  * How a head's values are paired for the rotation by position: value i with
  * value i + D/2, or neighbours 2i and 2i + 1.  Pair i turns by the angle

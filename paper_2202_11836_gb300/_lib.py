@@ -71,6 +71,13 @@ class SkyOptimizerConfig(C.Structure):
                 ("momentum", C.c_float)]
 
 
+class SkyCrossShape(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("q_len", C.c_int32), ("kv_len", C.c_int32),
+                ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int), ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldv", C.c_int64),
+                ("ldo", C.c_int64)]
+
+
 class SkyQkNormShape(C.Structure):
     _fields_ = [("rows", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int), ("ldx", C.c_int64),
@@ -110,6 +117,9 @@ _SIGNATURES = {
     "sky_attention_bwd_workspace_bytes": (_SZ, [_I32, _I32, _I32, _I32]),
     "sky_attention_bwd": (C.c_int, [_VP, _VP, _VP, _VP, _VP, _I32, _I32, _I32, _I32, C.c_int,
                                     _VP, _VP, _SZ, _VP, _VP]),
+    "sky_cross_attention_fwd": (C.c_int, [C.POINTER(SkyCrossShape)] + [_VP] * 8),
+    "sky_cross_attention_bwd_workspace_bytes": (_SZ, [C.POINTER(SkyCrossShape)]),
+    "sky_cross_attention_bwd": (C.c_int, [C.POINTER(SkyCrossShape)] + [_VP] * 11 + [_SZ, _VP, _VP]),
     "sky_qk_norm_fwd": (C.c_int, [C.POINTER(SkyQkNormShape), _VP, _VP, _VP, _VP, _VP, _VP]),
     "sky_qk_norm_bwd_workspace_bytes": (_SZ, [C.POINTER(SkyQkNormShape)]),
     "sky_qk_norm_bwd": (C.c_int, [C.POINTER(SkyQkNormShape), _VP, _VP, _VP, _VP, _VP, _VP, _VP,

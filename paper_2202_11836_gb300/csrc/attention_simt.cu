@@ -1,0 +1,455 @@
+// Masked scaled dot-product attention on the CUDA cores, for every head dim up to 128
+// and any strides: fp32 arithmetic on fp32 or bf16 storage, queries of one length over
+// keys of another.  The fp32 path of self attention, and cross attention wherever the
+// tensor-core kernels do not apply.
+#include <algorithm>
+#include <cfloat>
+#include <type_traits>
+
+#include "attention_simt.h"
+#include "common.cuh"
+
+namespace sky {
+namespace attn {
+
+// The valid keys of sequence b; a bad length is clamped and reported.
+__device__ __forceinline__ int valid_keys(const Geometry& g, int b) {
+  int len = g.lens[b];
+  if (len < g.least || len > g.Skv) {
+    if (g.status && threadIdx.x == 0) atomicOr(g.status, kStatusBadLength);
+    len = len < g.least ? g.least : g.Skv;
+  }
+  return len;
+}
+
+// delta[b, a, s] = sum_d dctx * ctx: one warp per (row, head), rows of ldo.
+template <typename T>
+__global__ void attn_delta(const T* __restrict__ ctx, const T* __restrict__ dctx, int S, int64_t ldo,
+                           int A, int D, int64_t rows, float* __restrict__ delta) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t w = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
+  const int l = threadIdx.x & 31;
+  if (w >= rows * A) return;
+  const int64_t row = w / A;
+  const int a = (int)(w % A);
+  const T* c = ctx + row * ldo + a * D;
+  const T* dc = dctx + row * ldo + a * D;
+  float acc = 0.f;
+  for (int d = l; d < D; d += 32) acc += to_f32(c[d]) * to_f32(dc[d]);
+  acc = warp_sum(acc);
+  if (l == 0) {
+    const int64_t b = row / S, s = row % S;
+    delta[(b * A + a) * S + s] = acc;
+  }
+}
+
+// A CTA of four warps owns 16 rows
+// of one (sequence, head) and walks the other side in tiles of 64 rows staged in
+// shared memory.  Half a warp owns two rows, so row maxima and sums are
+// shuffles among 16 lanes and a row's probabilities go to shared memory and
+// back within the half warp.  Score products: 2 rows x 4 columns a thread (six
+// 16-byte shared loads for 32 FMAs); accumulating products: 2 rows x 4 dims.
+// Short sequences and few heads make these latency-bound; a warp per row with
+// scalar loads took 116 us forward and 182 us backward at 4 x 101 tokens, 12
+// heads of 64.
+constexpr int FR = 16, FC = 64, F_THR = 128;  // rows of a CTA, columns of a tile
+constexpr int FP_LD = FC + 4;                 // row stride of the probability tiles
+// (the backward of sequences up to 16 tokens: tiles of 16 columns, NC = 1 of 4)
+
+// Rows are staged F_THR / G a pass, G threads a row (D <= 4 G), through registers, so
+// that a tile's loads are all in flight before the first is stored.  Loading and
+// storing in turn waited for each: 4 x 32 tokens, 2 heads of 64, forward 6.4 us,
+// now 3.8, backward 10.7 and 7.3; 4 x 101, 12 heads 17.0 and 12.2, 39.9 and 29.4; 4 x
+// 256, 24 heads of 32 52.6 and 48.7 (58.1 with 16 threads a row).
+template <int G, int NC = FC / 16>
+struct Stage {  // a tile's 16 NC rows: BATCHES of PASSES passes, R rows each
+  static constexpr int ROWS = 16 * NC;
+  static constexpr int PASSES = ROWS * G / F_THR < 8 ? ROWS * G / F_THR : 8;
+  static constexpr int R = PASSES * F_THR / G, BATCHES = ROWS / R;
+  static constexpr int OWN = FR * G / F_THR;  // passes of the CTA's FR rows
+  static constexpr int CC = G > 16 ? G / 16 : 1;  // 64-value column groups of an output row
+};
+// Four values of a row
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
+                     __uint_as_float(w.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store4(float* p, const float4& v) { *reinterpret_cast<float4*>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float4& v) {
+  __nv_bfloat162 w[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
+  *reinterpret_cast<uint2*>(p) = *reinterpret_cast<uint2*>(w);
+}
+// Rows from `rows` on are zeros.  vec: D, ld and X allow load4.
+template <int G, typename T, int N>
+__device__ __forceinline__ void load_rows(const T* __restrict__ X, int64_t ld, int r0, int rows, int D, bool vec,
+                                          float4 (&v)[N]) {
+  const int c = (threadIdx.x % G) * 4;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int r = r0 + F_THR / G * i + threadIdx.x / G;
+    v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (r < rows && c < D) {
+      const T* p = X + static_cast<int64_t>(r) * ld + c;
+      if (vec) {
+        v[i] = load4(p);
+      } else {
+        v[i].x = to_f32(p[0]);
+        if (c + 1 < D) v[i].y = to_f32(p[1]);
+        if (c + 2 < D) v[i].z = to_f32(p[2]);
+        if (c + 3 < D) v[i].w = to_f32(p[3]);
+      }
+    }
+  }
+}
+template <int G, int N>
+__device__ __forceinline__ void put_rows(float* s, int LD, int D, const float4 (&v)[N]) {
+  const int c = (threadIdx.x % G) * 4;
+  if (c >= D) return;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    *reinterpret_cast<float4*>(s + (F_THR / G * i + threadIdx.x / G) * LD + c) = v[i];
+}
+// acc[i][c] = row (2 ty + i) . column row (tx + 16 c), over D (a multiple of 4 in shared memory)
+template <int NC>
+__device__ __forceinline__ void scores(const float* rows, const float* cols, int LD, int D, float (&acc)[2][NC]) {
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int c = 0; c < NC; ++c) acc[i][c] = 0.f;
+  for (int d = 0; d < D; d += 4) {
+    float4 r[2], k[NC];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r[i] = *reinterpret_cast<const float4*>(rows + (2 * ty + i) * LD + d);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) k[c] = *reinterpret_cast<const float4*>(cols + (tx + 16 * c) * LD + d);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        acc[i][c] = fmaf(r[i].w, k[c].w, fmaf(r[i].z, k[c].z, fmaf(r[i].y, k[c].y, fmaf(r[i].x, k[c].x, acc[i][c]))));
+  }
+}
+// o[i][cc] += sum_j w[2 ty + i][j] cols[j][4 tx + 64 cc ..] over the tile's first n columns (n <= 64)
+template <int CC, int W_LD = FP_LD>
+__device__ __forceinline__ void accumulate(const float* w, const float* cols, int LD, int D, int n, float4 (&o)[2][CC]) {
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  for (int j = 0; j < n; j += 4) {
+    float4 p[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p[i] = *reinterpret_cast<const float4*>(w + (2 * ty + i) * W_LD + j);
+#pragma unroll
+    for (int cc = 0; cc < CC; ++cc) {
+      const int d = 4 * tx + 64 * cc;
+      if (d >= D) continue;
+      float4 v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float4*>(cols + (j + e) * LD + d);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float pe[4] = {p[i].x, p[i].y, p[i].z, p[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          o[i][cc].x = fmaf(pe[e], v[e].x, o[i][cc].x);
+          o[i][cc].y = fmaf(pe[e], v[e].y, o[i][cc].y);
+          o[i][cc].z = fmaf(pe[e], v[e].z, o[i][cc].z);
+          o[i][cc].w = fmaf(pe[e], v[e].w, o[i][cc].w);
+        }
+      }
+    }
+  }
+}
+template <int CC, typename T>
+__device__ __forceinline__ void store_rows(T* X, int64_t ld, int r0, int rows, int D, bool vec, float scale0,
+                                           float scale1, const float4 (&o)[2][CC]) {
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = r0 + 2 * ty + i;
+    if (r >= rows) continue;
+    const float sc = i ? scale1 : scale0;
+#pragma unroll
+    for (int cc = 0; cc < CC; ++cc) {
+      const int d = 4 * tx + 64 * cc;
+      if (d >= D) continue;
+      const float4 v = make_float4(o[i][cc].x * sc, o[i][cc].y * sc, o[i][cc].z * sc, o[i][cc].w * sc);
+      T* p = X + static_cast<int64_t>(r) * ld + d;
+      if (vec) {
+        store4(p, v);
+      } else {
+        p[0] = from_f32<T>(v.x);
+        if (d + 1 < D) p[1] = from_f32<T>(v.y);
+        if (d + 2 < D) p[2] = from_f32<T>(v.z);
+        if (d + 3 < D) p[3] = from_f32<T>(v.w);
+      }
+    }
+  }
+}
+__device__ __forceinline__ float half_warp_max(float v) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float half_warp_sum(float v) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+template <typename T, int G>
+__global__ void __launch_bounds__(F_THR) attn_fwd_simt(const Geometry g, T* __restrict__ ctx, float* __restrict__ lse) {
+  using ST = Stage<G>;
+  constexpr int CC = ST::CC;
+  pdl_wait();
+  extern __shared__ __align__(16) float sm[];
+  const int LD = g.LD, D = g.D, Sq = g.Sq;
+  const bool vec = g.vec;
+  float *sq = sm, *sk = sq + FR * LD, *sv = sk + FC * LD, *sp = sv + FC * LD;
+  const int tiles = (Sq + FR - 1) / FR;
+  const int a = static_cast<int>(blockIdx.x) / tiles, q0 = (static_cast<int>(blockIdx.x) % tiles) * FR, b = blockIdx.y;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int len = valid_keys(g, b), kv = a / g.group;
+  const T* q = static_cast<const T*>(g.q) + static_cast<int64_t>(b) * Sq * g.ldq + a * D;
+  const T* k = static_cast<const T*>(g.k) + static_cast<int64_t>(b) * g.Skv * g.ldk + kv * D;
+  const T* v = static_cast<const T*>(g.v) + static_cast<int64_t>(b) * g.Skv * g.ldv + kv * D;
+  const float sc = 1.f / sqrtf((float)D);
+  float4 own[ST::OWN];
+  load_rows<G>(q, g.ldq, q0, Sq, D, vec, own);
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float4 o[2][CC] = {};
+  for (int k0 = 0; k0 < len; k0 += FC) {
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < ST::BATCHES; ++h) {
+      constexpr int R = ST::R;
+      float4 kx[ST::PASSES], vx[ST::PASSES];
+      load_rows<G>(k, g.ldk, k0 + R * h, len, D, vec, kx);
+      load_rows<G>(v, g.ldv, k0 + R * h, len, D, vec, vx);
+      if (h == 0 && k0 == 0) put_rows<G>(sq, LD, D, own);
+      put_rows<G>(sk + R * h * LD, LD, D, kx);
+      put_rows<G>(sv + R * h * LD, LD, D, vx);
+    }
+    __syncthreads();
+    float s[2][4];
+    scores(sq, sk, LD, D, s);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[i][c] = k0 + tx + 16 * c < len ? s[i][c] * sc : -INFINITY;
+        mx = fmaxf(mx, s[i][c]);
+      }
+      // (finite also while every score so far is -inf: those keys then add nothing)
+      const float mn = fmaxf(fmaxf(m[i], half_warp_max(mx)), -FLT_MAX);
+      const float al = expf(m[i] - mn);  // 0 in the first tile
+      m[i] = mn;
+      float sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const float e = expf(s[i][c] - mn);  // masked: 0
+        sp[(2 * ty + i) * FP_LD + tx + 16 * c] = e;
+        sum += e;
+      }
+      l[i] = l[i] * al + half_warp_sum(sum);
+#pragma unroll
+      for (int cc = 0; cc < CC; ++cc) {
+        o[i][cc].x *= al; o[i][cc].y *= al; o[i][cc].z *= al; o[i][cc].w *= al;
+      }
+    }
+    __syncwarp();
+    accumulate<CC>(sp, sv, LD, D, min(FC, len - k0), o);
+    __syncwarp();
+  }
+  pdl_trigger();
+  store_rows<CC>(ctx + static_cast<int64_t>(b) * Sq * g.ldo + a * D, g.ldo, q0, Sq, D, vec, len > 0 ? 1.f / l[0] : 0.f,
+                 len > 0 ? 1.f / l[1] : 0.f, o);
+  if (tx == 0 && lse)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (q0 + 2 * ty + i < Sq)  // (without a key: -inf)
+        lse[(static_cast<int64_t>(b) * g.A + a) * Sq + q0 + 2 * ty + i] = (m[i] + logf(l[i])) * 1.4426950408889634f;  // base 2
+}
+
+// dQ: own rows are queries (Q, dO), columns keys (K, V).  dK, dV: own rows are keys (K,
+// V), columns the queries (Q, dO) of every head of the group, head after head.  Blocks of
+// the two kinds alternate, then come what is left of the more numerous.  Either way
+//   P = exp2(s log2(e)/sqrt(D) - lse_q),  dS = P (dp - delta_q),
+// s and dp the products of the first and second operands; dQ or dK = dS . first
+// operand of the columns / sqrt(D), dV = P . dO.  Four CTAs an SM (128 registers) are
+// faster up to a head dim of 64 (29.8 us against 34.7 at 4 x 101, 12 heads), above it
+// the registers are (50.6 against 57.0 at 2 x 200, 6 heads of 128).
+template <typename T, int G, int NC>
+__global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geometry g, const T* __restrict__ dctx,
+                                                      const float* __restrict__ lse, const float* __restrict__ delta,
+                                                      T* __restrict__ dq, T* __restrict__ dk, T* __restrict__ dv) {
+  using ST = Stage<G, NC>;
+  constexpr int CC = ST::CC, TC = ST::ROWS, P_LD = TC + 4;
+  pdl_wait();
+  extern __shared__ __align__(16) float sm[];
+  const int LD = g.LD, D = g.D, Sq = g.Sq, Skv = g.Skv;
+  const bool vec = g.vec;
+  float *r0s = sm, *r1s = r0s + FR * LD, *c0s = r1s + FR * LD, *c1s = c0s + TC * LD;
+  float *sds = c1s + TC * LD, *sp = sds + FR * P_LD, *sl = sp + FR * P_LD, *sd = sl + TC;
+  const int qtiles = (Sq + FR - 1) / FR, ktiles = (Skv + FR - 1) / FR;
+  const int both = min(qtiles * g.A, ktiles * (g.A / g.group)), x = blockIdx.x;
+  const bool keys = x < 2 * both ? x & 1 : qtiles * g.A < ktiles * (g.A / g.group);  // own rows are keys
+  const int u = x < 2 * both ? x >> 1 : x - both, tiles = keys ? ktiles : qtiles;
+  const int head = u / tiles, r0 = (u % tiles) * FR, b = blockIdx.y;  // of its kind
+  const int kv = keys ? head : head / g.group, heads = keys ? g.group : 1;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int len = valid_keys(g, b);
+  const T* k = static_cast<const T*>(g.k) + static_cast<int64_t>(b) * Skv * g.ldk + kv * D;
+  const T* v = static_cast<const T*>(g.v) + static_cast<int64_t>(b) * Skv * g.ldv + kv * D;
+  const float sc = 1.f / sqrtf((float)D), sl2 = sc * 1.4426950408889634f;
+  float4 o0[2][CC] = {}, o1[2][CC] = {};
+  const int rows = keys ? Skv : Sq, cols = keys ? Sq : len;
+  float4 own0[ST::OWN], own1[ST::OWN];
+  for (int h = 0; h < heads && (!keys || r0 < len); ++h) {
+    const int a = keys ? kv * g.group + h : head;
+    const T* q = static_cast<const T*>(g.q) + static_cast<int64_t>(b) * Sq * g.ldq + a * D;
+    const T* dO = dctx + static_cast<int64_t>(b) * Sq * g.ldo + a * D;
+    const float *lse_b = lse + (static_cast<int64_t>(b) * g.A + a) * Sq, *del_b = delta + (static_cast<int64_t>(b) * g.A + a) * Sq;
+    if (h == 0) {
+      load_rows<G>(keys ? k : q, keys ? g.ldk : g.ldq, r0, rows, D, vec, own0);
+      load_rows<G>(keys ? v : dO, keys ? g.ldv : g.ldo, r0, rows, D, vec, own1);
+    }
+    float lr[2] = {}, dr[2] = {};
+    if (!keys)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = min(r0 + 2 * ty + i, Sq - 1);
+        lr[i] = lse_b[r];
+        dr[i] = del_b[r];
+      }
+    for (int c0 = 0; c0 < cols; c0 += TC) {
+      __syncthreads();
+      // columns: queries (Q, dO; all S) or keys (K, V; the valid ones)
+      const T *x0 = keys ? q : k, *x1 = keys ? dO : v;
+      float lc = 0.f, dc = 0.f;
+      if (keys && threadIdx.x < TC) {
+        const int c = min(c0 + static_cast<int>(threadIdx.x), Sq - 1);
+        lc = lse_b[c];
+        dc = del_b[c];
+      }
+#pragma unroll
+      for (int t = 0; t < ST::BATCHES; ++t) {
+        constexpr int R = ST::R;
+        float4 v0[ST::PASSES], v1[ST::PASSES];
+        load_rows<G>(x0, keys ? g.ldq : g.ldk, c0 + R * t, cols, D, vec, v0);
+        load_rows<G>(x1, keys ? g.ldo : g.ldv, c0 + R * t, cols, D, vec, v1);
+        if (t == 0 && c0 == 0 && h == 0) {
+          put_rows<G>(r0s, LD, D, own0);
+          put_rows<G>(r1s, LD, D, own1);
+        }
+        put_rows<G>(c0s + R * t * LD, LD, D, v0);
+        put_rows<G>(c1s + R * t * LD, LD, D, v1);
+      }
+      if (keys && threadIdx.x < TC) {
+        sl[threadIdx.x] = lc;
+        sd[threadIdx.x] = dc;
+      }
+      __syncthreads();
+      float s[2][NC], dp[2][NC];
+      scores(r0s, c0s, LD, D, s);
+      scores(r1s, c1s, LD, D, dp);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int cl = tx + 16 * c;
+          const bool live = c0 + cl < cols && (!keys || r0 + 2 * ty + i < len);
+          const float p = live ? exp2f(fmaf(s[i][c], sl2, -(keys ? sl[cl] : lr[i]))) : 0.f;
+          sds[(2 * ty + i) * P_LD + cl] = live ? p * (dp[i][c] - (keys ? sd[cl] : dr[i])) : 0.f;
+          if (keys) sp[(2 * ty + i) * P_LD + cl] = p;
+        }
+      __syncwarp();
+      const int n = min(TC, cols - c0);
+      accumulate<CC, P_LD>(sds, c0s, LD, D, n, o0);
+      if (keys) accumulate<CC, P_LD>(sp, c1s, LD, D, n, o1);
+      __syncwarp();
+    }
+  }
+  pdl_trigger();
+  T* out = keys ? dk + static_cast<int64_t>(b) * Skv * g.ldk + kv * D : dq + static_cast<int64_t>(b) * Sq * g.ldq + head * D;
+  store_rows<CC>(out, keys ? g.ldk : g.ldq, r0, rows, D, vec, sc, sc, o0);
+  if (keys) store_rows<CC>(dv + static_cast<int64_t>(b) * Skv * g.ldv + kv * D, g.ldv, r0, rows, D, vec, 1.f, 1.f, o1);
+}
+
+// Launch shape: the shared row stride (four floats past the head dim, so the 16 lanes of
+// a score product read different banks) and the bytes it makes.
+constexpr int row_stride(int D) { return (D + 3) / 4 * 4 + 4; }
+constexpr int fwd_smem(int D) { return ((FR + 2 * FC) * row_stride(D) + FR * FP_LD) * 4; }
+constexpr int bwd_smem(int D, int NC) {
+  return ((2 * FR + 32 * NC) * row_stride(D) + 2 * FR * (16 * NC + 4) + 32 * NC) * 4;
+}
+template <int G>
+using Group = std::integral_constant<int, G>;
+// Whether every head row allows 4-value accesses.
+template <typename T>
+bool rows_of_4(const Geometry& g, const void* ctx, const void* x = nullptr, const void* y = nullptr,
+               const void* z = nullptr) {
+  const auto on = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0; };
+  return g.D % 4 == 0 && (g.ldq | g.ldk | g.ldv | g.ldo) % 4 == 0 && on(g.q) && on(g.k) && on(g.v) && on(ctx) && on(x) &&
+         on(y) && on(z);
+}
+
+template <typename T>
+cudaError_t launch_fwd_simt(Geometry g, int B, T* ctx, float* lse, cudaStream_t stream) {
+  g.LD = row_stride(g.D);
+  g.vec = rows_of_4<T>(g, ctx);
+  const auto go = [&](auto group, auto kern) {  // `group` threads a row: head dims up to four times that
+    static OncePerDevice once;
+    const cudaError_t e = allow_smem(once, kern, fwd_smem(4 * decltype(group)::value));
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kern, dim3((unsigned)ceil_div(g.Sq, FR) * g.A, B), dim3(F_THR), fwd_smem(g.D), stream, 1, g, ctx,
+                      lse);
+  };
+  count_launches(1);
+  return g.D <= 32   ? go(Group<8>{}, attn_fwd_simt<T, 8>)
+         : g.D <= 64 ? go(Group<16>{}, attn_fwd_simt<T, 16>)
+                     : go(Group<32>{}, attn_fwd_simt<T, 32>);
+}
+
+template <typename T>
+cudaError_t launch_bwd_simt(Geometry g, int B, const T* ctx, const T* dctx, const float* lse, float* delta, T* dq, T* dk,
+                            T* dv, cudaStream_t stream) {
+  const int64_t rows = static_cast<int64_t>(B) * g.Sq;
+  const cudaError_t le = launch_pdl(attn_delta<T>, dim3(ceil_div(rows * g.A * 32, 256)), dim3(256), 0, stream, 1, ctx,
+                                    dctx, g.Sq, g.ldo, g.A, g.D, rows, delta);
+  count_launches(2);
+  if (le != cudaSuccess) return le;
+  g.LD = row_stride(g.D);
+  g.vec = rows_of_4<T>(g, dctx, dq, dk, dv);
+  const unsigned blocks = (unsigned)ceil_div(g.Sq, FR) * g.A + (unsigned)ceil_div(g.Skv, FR) * (g.A / g.group);
+  const auto go = [&](auto group, auto nc, auto kern) {
+    constexpr int G = decltype(group)::value, NC = decltype(nc)::value;
+    static OncePerDevice once;
+    const cudaError_t e = allow_smem(once, kern, bwd_smem(4 * G, NC));
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kern, dim3(blocks, B), dim3(F_THR), bwd_smem(g.D, NC), stream, 1, g, dctx, lse,
+                      static_cast<const float*>(delta), dq, dk, dv);
+  };
+  // Up to 16 tokens a 64-column tile is mostly empty: 128 x 8 tokens, 6 heads of 128
+  // 52.4 us with it, 27.8 with 16 columns (a warp a row 28.8); 12 of 64 45.2 and 25.5
+  // (41.1); 64 x 16, 12 of 64 29.8 and 18.3 (70.4).
+  const auto width = [&](auto group) {
+    constexpr int G = decltype(group)::value;
+    return std::max(g.Sq, g.Skv) <= 16 ? go(group, std::integral_constant<int, 1>{}, attn_bwd_simt<T, G, 1>)
+                                       : go(group, std::integral_constant<int, 4>{}, attn_bwd_simt<T, G, 4>);
+  };
+  return g.D <= 32 ? width(Group<8>{}) : g.D <= 64 ? width(Group<16>{}) : width(Group<32>{});
+}
+
+template cudaError_t launch_fwd_simt(Geometry, int, float*, float*, cudaStream_t);
+template cudaError_t launch_fwd_simt(Geometry, int, __nv_bfloat16*, float*, cudaStream_t);
+template cudaError_t launch_bwd_simt(Geometry, int, const float*, const float*, const float*, float*, float*, float*,
+                                     float*, cudaStream_t);
+template cudaError_t launch_bwd_simt(Geometry, int, const __nv_bfloat16*, const __nv_bfloat16*, const float*, float*,
+                                     __nv_bfloat16*, __nv_bfloat16*, __nv_bfloat16*, cudaStream_t);
+
+}  // namespace attn
+}  // namespace sky

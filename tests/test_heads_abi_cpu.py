@@ -1,4 +1,4 @@
-"""What the head norms refuse, before any device is touched."""
+"""What the head norms and cross attention refuse, before any device is touched."""
 import ctypes as C
 import os
 
@@ -67,3 +67,49 @@ def test_norm_refuses_arguments(lib):
         assert bwd(s, *[odd if j == i else a for j, a in enumerate(ok)], need, None) == UNSUPPORTED
     assert bwd(s, *ok[:8], C.c_void_p((1 << 20) + 2), need, None) == INVALID
     assert bwd(s, *ok, need - 1, None) == INVALID
+
+
+def cross_shape(**kw):
+    base = dict(batch=2, q_len=3, kv_len=5, heads=4, kv_heads=2, head_dim=64, dtype=L.SKY_DTYPE_BF16, ldq=256, ldk=256,
+                ldv=256, ldo=256)
+    base.update(kw)
+    return L.SkyCrossShape(**base)
+
+
+CROSS_REFUSED = [(dict([(n, v)]), INVALID) for n in ("batch", "q_len", "kv_len", "heads", "kv_heads", "head_dim")
+                 for v in (0, -1)] + [
+    (dict(kv_heads=3), INVALID), (dict(kv_heads=8), INVALID), (dict(dtype=2), INVALID), (dict(dtype=-1), INVALID),
+    (dict(ldq=255), INVALID), (dict(ldo=0), INVALID), (dict(ldk=127), INVALID), (dict(ldv=-256), INVALID),
+    (dict(head_dim=129, ldq=1024, ldk=1024, ldv=1024, ldo=1024), UNSUPPORTED), (dict(batch=65536), UNSUPPORTED),
+    (dict(q_len=(1 << 24) + 1), UNSUPPORTED), (dict(kv_len=(1 << 24) + 1), UNSUPPORTED),
+    (dict(heads=1026, ldq=1 << 20, ldo=1 << 20), UNSUPPORTED), (dict(ldk=(1 << 30) + 1), UNSUPPORTED),
+    (dict(batch=60000, q_len=1 << 20), UNSUPPORTED),
+]
+
+
+@pytest.mark.parametrize("bad,status", CROSS_REFUSED, ids=lambda v: str(v))
+def test_cross_refuses_shapes(lib, bad, status):
+    s = cross_shape(**bad)
+    assert lib.sky_cross_attention_fwd(s, *[AT] * 7, None) == status
+    assert L.last_error()
+    assert lib.sky_cross_attention_bwd_workspace_bytes(s) == 0
+    assert lib.sky_cross_attention_bwd(s, *[AT] * 11, 1 << 40, AT, None) == status
+
+
+def test_cross_refuses_arguments(lib):
+    s, odd = cross_shape(), C.c_void_p((1 << 20) + 1)
+    need = lib.sky_cross_attention_bwd_workspace_bytes(s)
+    assert need > 0 and lib.sky_cross_attention_bwd_workspace_bytes(None) == 0
+    fwd, bwd = lib.sky_cross_attention_fwd, lib.sky_cross_attention_bwd
+    assert fwd(None, *[AT] * 7, None) == INVALID
+    for i in range(5):  # q, k, v, lengths, ctx
+        assert fwd(s, *[None if j == i else AT for j in range(7)], None) == INVALID
+    for i in (0, 1, 2, 4):
+        assert fwd(s, *[odd if j == i else AT for j in range(7)], None) == INVALID
+    assert bwd(None, *[AT] * 11, need, None, None) == INVALID
+    for i in range(11):
+        assert bwd(s, *[None if j == i else AT for j in range(11)], need, None, None) == INVALID
+    for i in (0, 1, 2, 3, 4, 7, 8, 9):
+        assert bwd(s, *[odd if j == i else AT for j in range(11)], need, None, None) == INVALID
+    assert bwd(s, *[C.c_void_p((1 << 20) + 8) if j == 10 else AT for j in range(11)], need, None, None) == INVALID
+    assert bwd(s, *[AT] * 11, need - 1, None, None) == INVALID
