@@ -39,10 +39,12 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <mutex>
 #include <type_traits>
 
+#include "attention_tc.h"
 #include "common.cuh"
 #include "ptx.cuh"
 #include "residency.h"
@@ -67,6 +69,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 // until the phase completes instead of spinning on issue slots that the
 // softmax warps (the critical path) share with the producer and MMA threads.
 constexpr uint32_t kWaitHint = 10000;
+constexpr uint64_t kTimeoutNs = 2000000000;  // of a wait, as in self attention
 
 // Forward kernel with NS score buffers: four CTAs an SM with one, two with two.
 // Shared-memory layout (offsets from a 1024-byte aligned base).  TMEM: S_0, then
@@ -87,18 +90,49 @@ static_assert(FwdShape<1>::CTAS * (FwdShape<1>::SMEM + 1024) <= 233472, "four fo
 static_assert(FwdShape<1>::STAGES * 2 * KV_BYTES >= BQ * HD * 4, "a partial O goes over the K/V stages");
 constexpr float kRescaleLog2 = 8.f;
 
+// Cross attention (X kernels): queries [B][S] over keys [B][Skv] in tensors of their own,
+// whose 4-D maps [B][rows][heads][64] fill what lies past a sequence's last row with zeros
+// and drop it from stores.  Row r of a 128- or 64-row query tile is head r % 2^pack of
+// query r >> pack: 2^pack heads that share keys share a tile, so short targets fill it.
+// A sequence may have no valid key, and what lies in its rows behind them, infinities and
+// NaN included, reaches nothing: scores there are replaced by -inf, and the rows of the
+// last tile that a product would multiply with a zero probability are cleared in shared
+// memory first.
+struct CrossGeometry {
+  int Skv;    // rows of keys
+  int group;  // query heads of a key head
+  int pack;   // log2 of the heads in a query tile
+};
+
 struct FwdParams {
   int S, H, A;
   const int32_t* lens;
-  __nv_bfloat16* ctx;
-  float* lse;
+  float* lse;  // X: or null
   int32_t* status;
   uint64_t timeout_ns;
+  CrossGeometry x;
 };
 
-template <int KS, int NS>
+// The valid keys of sequence b, in [least, S]; a bad length is clamped and reported.
+__device__ __forceinline__ int valid_keys(const int32_t* lens, int b, int least, int S, int32_t* status) {
+  int len = lens[b];
+  if (len < least || len > S) {
+    if (status && threadIdx.x == 0) atomicOr(status, kStatusBadLength);
+    len = len < least ? least : S;
+  }
+  return len;
+}
+
+// Clears rows [from, 64) of a 64-row tile of 128-byte rows (any swizzle: it stays within
+// a row); thread t of n.  The caller fences before the next product reads the tile.
+__device__ __forceinline__ void clear_rows(uint8_t* tile, int from, int t, int n) {
+  for (int i = from * 8 + t; i < 64 * 8; i += n) ptx::st_shared_v4(ptx::smem_u32(tile) + i * 16, 0, 0, 0, 0);
+}
+
+template <int KS, int NS, bool X>
 __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __grid_constant__ CUtensorMap tmQ,
                                                     const __grid_constant__ CUtensorMap tmKV,
+                                                    const __grid_constant__ CUtensorMap tmV,  // X
                                                     const __grid_constant__ CUtensorMap tmOut,
                                                     const FwdParams p) {
   using SH = FwdShape<NS>;
@@ -113,11 +147,13 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
   uint64_t* pv_done = p_full + NS;           // [NS] O += P_j V_j complete
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pv_done + NS);
 
-  const int qt = blockIdx.x / KS, split = blockIdx.x % KS, a = blockIdx.y, b = blockIdx.z;
+  const int pack = X ? p.x.pack : 0;
+  const int qt = blockIdx.x / KS, split = blockIdx.x % KS, a = blockIdx.y << pack, b = blockIdx.z;  // (first) head
   const int S = p.S, H = p.H;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row0 = b * S;  // first token row of this sequence
-  const int q0 = qt * BQ;
+  const int q0 = qt * (BQ >> pack);
+  const int kvh = X ? a / p.x.group : 0;
   const uint64_t lim = p.timeout_ns;
 
   if (threadIdx.x == 0) {
@@ -135,6 +171,7 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
     ptx::fence_proxy_async_smem();
     ptx::prefetch_tensormap(&tmQ);
     ptx::prefetch_tensormap(&tmKV);
+    if (X) ptx::prefetch_tensormap(&tmV);
   }
   if (warp == 1) {
     ptx::tmem_alloc(tmem_slot, SH::TMEM_COLS);
@@ -146,11 +183,7 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
   const uint32_t tmem = *tmem_slot;
   const uint32_t tS0 = tmem, tO = tmem + 64 * NS;
   pdl_wait();
-  int len = p.lens[b];
-  if (len < 1 || len > S) {
-    if (p.status && threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
-    len = len < 1 ? 1 : S;
-  }
+  const int len = valid_keys(p.lens, b, X ? 0 : 1, X ? p.x.Skv : S, p.status);
   const int n_all = (len + BKV - 1) / BKV;
   const int j0 = split * n_all / KS, n_kt = (split + 1) * n_all / KS - j0;  // this CTA's key tiles
   const int last = n_kt > 0 ? n_kt - 1 : 0;
@@ -160,7 +193,8 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
     const bool issuer = ptx::elect_one();
     if (issuer) {
       ptx::mbar_arrive_expect_tx(q_full, Q_BYTES);
-      ptx::tma_load_2d(smem + SH::Q_OFF, &tmQ, q_full, a * HD, row0 + q0);
+      if constexpr (X) ptx::tma_load_4d(smem + SH::Q_OFF, &tmQ, q_full, 0, a, q0, b);
+      else ptx::tma_load_2d(smem + SH::Q_OFF, &tmQ, q_full, a * HD, row0 + q0);
     }
     __syncwarp();
     int issued = 0;
@@ -172,8 +206,13 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
       if (issuer) {
         uint8_t* kv = smem + SH::KV_OFF + st * 2 * KV_BYTES;
         ptx::mbar_arrive_expect_tx(&kv_full[st], 2 * KV_BYTES);
-        ptx::tma_load_2d(kv, &tmKV, &kv_full[st], H + a * HD, row0 + (j0 + j) * BKV);
-        ptx::tma_load_2d(kv + KV_BYTES, &tmKV, &kv_full[st], 2 * H + a * HD, row0 + (j0 + j) * BKV);
+        if constexpr (X) {
+          ptx::tma_load_4d(kv, &tmKV, &kv_full[st], 0, kvh, (j0 + j) * BKV, b);
+          ptx::tma_load_4d(kv + KV_BYTES, &tmV, &kv_full[st], 0, kvh, (j0 + j) * BKV, b);
+        } else {
+          ptx::tma_load_2d(kv, &tmKV, &kv_full[st], H + a * HD, row0 + (j0 + j) * BKV);
+          ptx::tma_load_2d(kv + KV_BYTES, &tmKV, &kv_full[st], 2 * H + a * HD, row0 + (j0 + j) * BKV);
+        }
       }
       __syncwarp();
       ++issued;
@@ -272,6 +311,11 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
       };
       if (!wait_all(&s_full[j % NS], (j / NS) & 1)) { ok = false; break; }
       ptx::tc_fence_after();
+      if (X && left < BKV) {  // P is 0 there, and V anything
+        if (!wait_all(&kv_full[j % SH::STAGES], (j / SH::STAGES) & 1)) { ok = false; break; }
+        clear_rows(smem + SH::KV_OFF + (j % SH::STAGES) * 2 * KV_BYTES + KV_BYTES, left, r, 128);
+        ptx::fence_proxy_async_smem();
+      }
       // row max of the raw scores (scaling by log2(e)/sqrt(D) > 0 commutes with
       // max): the high half, then the low half, which stays in registers
       load_half(1);
@@ -360,10 +404,11 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
       // epilogue: O / l -> ctx (bf16) as 128-byte-swizzled rows over the Q
       // tile (the last S product has read it), stored by one TMA that drops the
       // rows past S; the log-sum-exp directly
-      if (ok && wait_all(&pv_done[last % NS], (last / NS) & 1)) {
+      const bool any = !X || n_kt > 0;  // (without a key O was never written, and Q may still be on its way)
+      if (ok && (any ? wait_all(&pv_done[last % NS], (last / NS) & 1) : wait_all(q_full, 0))) {
         ptx::tc_fence_after();
         const float inv = 1.f / l;
-        const int q = q0 + r;
+        const int q = q0 + (r >> pack);
         const uint32_t orow = ptx::smem_u32(smem + SH::Q_OFF) + r * 128;
 #pragma unroll
         for (int c = 0; c < HD / 32; ++c) {
@@ -375,17 +420,20 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
             uint32_t w[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-              w[t] = ptx::pack_bf16(__uint_as_float(v[8 * u + 2 * t]) * inv,
-                                    __uint_as_float(v[8 * u + 2 * t + 1]) * inv);
+              w[t] = any ? ptx::pack_bf16(__uint_as_float(v[8 * u + 2 * t]) * inv,
+                                          __uint_as_float(v[8 * u + 2 * t + 1]) * inv)
+                         : 0u;
             ptx::st_shared_v4(orow + (((c * 4 + u) ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
           }
         }
-        if (q < S) p.lse[(static_cast<int64_t>(b) * p.A + a) * S + q] = m + log2f(l);
+        if (q < S && (!X || p.lse))  // (without a key: -inf + -inf)
+          p.lse[(static_cast<int64_t>(b) * p.A + a + (r & ((1 << pack) - 1))) * S + q] = m + log2f(l);
       }
       ptx::fence_proxy_async_smem();  // the staged rows -> the TMA store
       asm volatile("bar.sync 1, 128;" ::: "memory");  // the four softmax warps
       if (warp == 2 && lane == 0) {
-        ptx::tma_store_3d(&tmOut, smem + SH::Q_OFF, a * HD, q0, b);
+        if constexpr (X) ptx::tma_store_4d(&tmOut, smem + SH::Q_OFF, 0, a, q0, b);
+        else ptx::tma_store_3d(&tmOut, smem + SH::Q_OFF, a * HD, q0, b);
         ptx::bulk_commit_group();
         ptx::bulk_wait_group_read0();  // before the CTA's memory goes
       }
@@ -414,7 +462,7 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
         w[s] = exp2f(w[s] - mx);
         l += w[s] * ptx::ld_cluster_f2(ptx::mapa_shared(ml, s)).y;
       }
-      const float inv = 1.f / l;
+      const float inv = !X || n_all > 0 ? 1.f / l : 0.f;
       const uint32_t orow = ptx::smem_u32(smem + SH::Q_OFF) + lr * 128;
 #pragma unroll
       for (int i = 0; i < G; ++i) {
@@ -430,12 +478,14 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
         ptx::st_shared_v2(orow + (((g >> 1) ^ (lr & 7)) << 4) + (g & 1) * 8, ptx::pack_bf16(o.x * inv, o.y * inv),
                           ptx::pack_bf16(o.z * inv, o.w * inv));
       }
-      const int q = q0 + row;
-      if (sub == 0 && q < S) p.lse[(static_cast<int64_t>(b) * p.A + a) * S + q] = mx + log2f(l);
+      const int q = q0 + (row >> pack), first = q0 + ((split * ROWS) >> pack);
+      if (sub == 0 && q < S && (!X || p.lse))
+        p.lse[(static_cast<int64_t>(b) * p.A + a + (row & ((1 << pack) - 1))) * S + q] = mx + log2f(l);
       ptx::fence_proxy_async_smem();
       asm volatile("bar.sync 1, 128;" ::: "memory");
-      if (warp == 2 && lane == 0 && q0 + split * ROWS < S) {
-        ptx::tma_store_3d(&tmOut, smem + SH::Q_OFF, a * HD, q0 + split * ROWS, b);
+      if (warp == 2 && lane == 0 && first < S) {
+        if constexpr (X) ptx::tma_store_4d(&tmOut, smem + SH::Q_OFF, 0, a, first, b);
+        else ptx::tma_store_3d(&tmOut, smem + SH::Q_OFF, a * HD, first, b);
         ptx::bulk_commit_group();
         ptx::bulk_wait_group_read0();
       }
@@ -671,6 +721,10 @@ struct BwdParams {
   float* colpart;
   int32_t* status;
   uint64_t timeout_ns;
+  CrossGeometry x;
+  // X: dk, dv and their row distances; xtab [B][A >> pack][2][S << pack]
+  __nv_bfloat16 *dk, *dv;
+  int64_t ldk, ldv;
 };
 
 // v[j] of lane l -> after the call, v[0] of lane l holds the sum over the
@@ -697,8 +751,10 @@ __device__ __forceinline__ void softmax_warps_sync() {
   asm volatile("bar.sync 1, 256;" ::: "memory");
 }
 
+template <bool X>
 __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorMap tmQ,
                                                           const __grid_constant__ CUtensorMap tmKV,
+                                                          const __grid_constant__ CUtensorMap tmV,  // X
                                                           const __grid_constant__ CUtensorMap tmO,
                                                           const __grid_constant__ CUtensorMap tmOut,
                                                           const BwdParams p) {
@@ -720,16 +776,14 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
   uint64_t* done = dq_done + 1;  // [2], one per issuing warp
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
 
-  const int qt = blockIdx.x, a = blockIdx.y, b = blockIdx.z;
+  const int pack = X ? p.x.pack : 0;
+  const int qt = blockIdx.x, a = blockIdx.y << pack, b = blockIdx.z;  // (first) head
   const int S = p.S, H = p.H;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int len = p.lens[b];
-  if (len < 1 || len > S) {
-    if (p.status && threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
-    len = len < 1 ? 1 : S;
-  }
+  const int len = valid_keys(p.lens, b, X ? 0 : 1, X ? p.x.Skv : S, p.status);
   const int n_kt = (len + BKV - 1) / BKV;
-  const int row0 = b * S, q0 = qt * BQ;
+  const int row0 = b * S, q0 = qt * (BQ >> pack);
+  const int kvh = X ? a / p.x.group : 0;
   const uint64_t lim = p.timeout_ns;
 
   if (threadIdx.x == 0) {
@@ -765,8 +819,13 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
       ptx::prefetch_tensormap(&tmO);
       ptx::prefetch_tensormap(&tmKV);
       ptx::mbar_arrive_expect_tx(qd_full, DQ_QD_BYTES);
-      ptx::tma_load_2d(smem + DQ_Q_OFF, &tmQ, qd_full, a * HD, row0 + q0);
-      ptx::tma_load_2d(smem + DQ_DO_OFF, &tmO, qd_full, a * HD, row0 + q0);
+      if constexpr (X) {
+        ptx::tma_load_4d(smem + DQ_Q_OFF, &tmQ, qd_full, 0, a, q0, b);
+        ptx::tma_load_4d(smem + DQ_DO_OFF, &tmO, qd_full, 0, a, q0, b);
+      } else {
+        ptx::tma_load_2d(smem + DQ_Q_OFF, &tmQ, qd_full, a * HD, row0 + q0);
+        ptx::tma_load_2d(smem + DQ_DO_OFF, &tmO, qd_full, a * HD, row0 + q0);
+      }
       int issued = 0;
       for (int j = 0; j < n_kt; ++j) {
         const int st = j % DQ_STAGES;
@@ -774,8 +833,13 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
           break;
         uint8_t* kv = smem + DQ_KV_OFF + st * 2 * KV_BYTES;
         ptx::mbar_arrive_expect_tx(&kv_full[st], 2 * KV_BYTES);
-        ptx::tma_load_2d(kv, &tmKV, &kv_full[st], H + a * HD, row0 + j * BKV);
-        ptx::tma_load_2d(kv + KV_BYTES, &tmKV, &kv_full[st], 2 * H + a * HD, row0 + j * BKV);
+        if constexpr (X) {
+          ptx::tma_load_4d(kv, &tmKV, &kv_full[st], 0, kvh, j * BKV, b);
+          ptx::tma_load_4d(kv + KV_BYTES, &tmV, &kv_full[st], 0, kvh, j * BKV, b);
+        } else {
+          ptx::tma_load_2d(kv, &tmKV, &kv_full[st], H + a * HD, row0 + j * BKV);
+          ptx::tma_load_2d(kv + KV_BYTES, &tmKV, &kv_full[st], 2 * H + a * HD, row0 + j * BKV);
+        }
         ++issued;
       }
       ptx::mbar_wait(qd_full, 0, lim, p.status, kWaitHint);
@@ -844,10 +908,10 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
     const int q4 = warp & 3;
     const int hf = (warp - 2) >> 2;  // column half: keys [32 hf, 32 hf + 32) of a tile
     const int r = q4 * 32 + lane;
-    const int q = q0 + r;
+    const int q = q0 + (r >> pack);
     const uint32_t lane_base = static_cast<uint32_t>(q4 * 32) << 16;
     const float sl2 = LOG2E * 0.125f;
-    const int64_t sidx = (static_cast<int64_t>(b) * p.A + a) * S + (q < S ? q : 0);
+    const int64_t sidx = (static_cast<int64_t>(b) * p.A + a + (r & ((1 << pack) - 1))) * S + (q < S ? q : 0);
     const float nlse2 = q < S ? -p.lse[sidx] : -INFINITY;  // P = 0 on rows past S
     const float dl = q < S ? p.delta[sidx] : 0.f;
     const uint64_t sc2 = pack2(sl2, sl2), nlse = pack2(nlse2, nlse2), ndl = pack2(-dl, -dl);
@@ -866,6 +930,11 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
       ptx::tc_fence_before();
       ptx::mbar_arrive(s_free);
       const int kbase = j * BKV + hf * 32;
+      if (X && j * BKV + BKV > len) {  // dS is 0 there, and K anything; S_j and dP_j have read it
+        if (!wait_all(&kv_full[j % DQ_STAGES], (j / DQ_STAGES) & 1)) { ok = false; break; }
+        clear_rows(smem + DQ_KV_OFF + (j % DQ_STAGES) * 2 * KV_BYTES, len - j * BKV, r + hf * 128, NSM_B);
+        ptx::fence_proxy_async_smem();
+      }
       uint32_t pk[16];
 #pragma unroll
       for (int i = 0; i < 32; i += 2) {
@@ -897,7 +966,8 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
     // bf16 rows over the Q tile (the last S product has read it); one thread
     // then stores the tile by TMA, which drops the rows past S
     float* red = reinterpret_cast<float*>(smem + DQ_KV_OFF);  // [4 row quarters][64]: ring is idle
-    if (ok && wait_all(dq_done, (n_kt - 1) & 1)) {
+    const bool any = !X || n_kt > 0;  // (without a key dQ was never written, and Q may still be on its way)
+    if (ok && (any ? wait_all(dq_done, (n_kt - 1) & 1) : wait_all(qd_full, 0))) {
       ptx::tc_fence_after();
       const uint32_t orow = ptx::smem_u32(smem + DQ_Q_OFF) + r * 128;
       uint32_t o[32];
@@ -908,27 +978,29 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
         uint32_t w[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-          w[t] = ptx::pack_bf16(__uint_as_float(o[8 * u + 2 * t]) * 0.125f,
-                                __uint_as_float(o[8 * u + 2 * t + 1]) * 0.125f);
+          w[t] = any ? ptx::pack_bf16(__uint_as_float(o[8 * u + 2 * t]) * 0.125f,
+                                      __uint_as_float(o[8 * u + 2 * t + 1]) * 0.125f)
+                     : 0u;
         ptx::st_shared_v4(orow + (((hf * 4 + u) ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
       }
-      if (p.colpart) {  // column sums of the stored values over this warp's 32 rows
+      if (!X && p.colpart) {  // column sums of the stored values over this warp's 32 rows
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = q < S ? bf16_round(__uint_as_float(o[j]) * 0.125f) : 0.f;
         lanes_column_sum(v, lane);
         red[q4 * 64 + hf * 32 + lane] = v[0];
       }
-    } else if (p.colpart) {
+    } else if (!X && p.colpart) {
       red[q4 * 64 + hf * 32 + lane] = 0.f;
     }
     ptx::fence_proxy_async_smem();  // the staged rows -> the TMA store
     softmax_warps_sync();
     if (warp == 2 && lane == 0) {
-      ptx::tma_store_3d(&tmOut, smem + DQ_Q_OFF, a * HD, q0, b);
+      if constexpr (X) ptx::tma_store_4d(&tmOut, smem + DQ_Q_OFF, 0, a, q0, b);
+      else ptx::tma_store_3d(&tmOut, smem + DQ_Q_OFF, a * HD, q0, b);
       ptx::bulk_commit_group();
     }
-    if (p.colpart && q4 == 0) {  // the four row quarters, added in order, by the quarter-0 warps
+    if (!X && p.colpart && q4 == 0) {  // the four row quarters, added in order, by the quarter-0 warps
       const int c = hf * 32 + lane;
       const float sum = ((red[c] + red[64 + c]) + red[128 + c]) + red[192 + c];
       p.colpart[(static_cast<int64_t>(b) * gridDim.x + qt) * (3 * H) + a * HD + c] = sum;
@@ -991,26 +1063,36 @@ constexpr int KV_SMEM = KV_BAR_OFF + 128 + 1024;
 static_assert(3 * (KV_SMEM + 1024) > 233472 && 2 * (KV_SMEM + 1024) <= 233472,
               "exactly two dK/dV CTAs per SM");
 
+template <bool X>
 __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtensorMap tmK,
+                                                            const __grid_constant__ CUtensorMap tmV,  // X
                                                             const __grid_constant__ CUtensorMap tmQ,
                                                             const __grid_constant__ CUtensorMap tmO,
                                                             const __grid_constant__ CUtensorMap tmOut,
+                                                            const __grid_constant__ CUtensorMap tmOutV,  // X
                                                             const BwdParams p) {
   // wait first, then let the dQ kernel start: once every CTA here has passed
   // the wait, the delta pre-pass (and everything before it) is complete
   pdl_wait();
   pdl_trigger();
   extern __shared__ uint8_t smem_raw[];
-  const int kt = blockIdx.x, a = blockIdx.y, b = blockIdx.z;
+  const int kt = blockIdx.x, a = blockIdx.y, b = blockIdx.z;  // X: a is the key head
   const int S = p.S, H = p.H;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int len = p.lens[b];
-  if (len < 1 || len > S) {
-    if (p.status && threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
-    len = len < 1 ? 1 : S;
-  }
+  const int len = valid_keys(p.lens, b, X ? 0 : 1, X ? p.x.Skv : S, p.status);
   const int row0 = b * S, k0 = kt * BK2;
   const int64_t rs = 3 * static_cast<int64_t>(H);
+  if (X && k0 >= len) {  // as below
+    for (int i = threadIdx.x; i < BK2 * 8; i += NTHR_B) {
+      const int rr = i >> 3, c = i & 7;
+      if (k0 + rr < p.x.Skv) {
+        const int64_t row = static_cast<int64_t>(b) * p.x.Skv + k0 + rr;
+        *reinterpret_cast<uint4*>(p.dk + row * p.ldk + a * HD + c * 8) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(p.dv + row * p.ldv + a * HD + c * 8) = make_uint4(0, 0, 0, 0);
+      }
+    }
+    return;
+  }
   if (k0 >= len) {  // keys of this tile are all padding: zero gradients
     for (int i = threadIdx.x; i < BK2 * 8; i += NTHR_B) {
       const int rr = i >> 3, c = i & 7;
@@ -1038,7 +1120,9 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
   uint64_t* dk_done = dv_done + 1;          // dK += dS^T_i Q_i complete: dP^T columns free
   uint64_t* done = dk_done + 1;             // [2], one per issuing warp
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
-  const int n_qt = (S + BQ2 - 1) / BQ2;
+  const int pack = X ? p.x.pack : 0, qrows = S << pack;    // rows of queries of a block of 2^pack heads
+  const int n_q = (qrows + BQ2 - 1) / BQ2;                  // their tiles
+  const int n_qt = X ? n_q * (p.x.group >> pack) : n_q;     // of every block that reads these keys, in turn
   const uint64_t lim = p.timeout_ns;
 
   if (threadIdx.x == 0) {
@@ -1083,23 +1167,42 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
       ptx::prefetch_tensormap(&tmQ);
       ptx::prefetch_tensormap(&tmO);
       ptx::mbar_arrive_expect_tx(kv_full, 2 * KV2_BYTES);
-      ptx::tma_load_2d(smem + KV_K_OFF, &tmK, kv_full, H + a * HD, row0 + k0);
-      ptx::tma_load_2d(smem + KV_V_OFF, &tmK, kv_full, 2 * H + a * HD, row0 + k0);
+      if constexpr (X) {
+        ptx::prefetch_tensormap(&tmV);
+        ptx::tma_load_4d(smem + KV_K_OFF, &tmK, kv_full, 0, a, k0, b);
+        ptx::tma_load_4d(smem + KV_V_OFF, &tmV, kv_full, 0, a, k0, b);
+      } else {
+        ptx::tma_load_2d(smem + KV_K_OFF, &tmK, kv_full, H + a * HD, row0 + k0);
+        ptx::tma_load_2d(smem + KV_V_OFF, &tmK, kv_full, 2 * H + a * HD, row0 + k0);
+      }
     }
     // this (sequence, head)'s X_lse rows, followed by its X_delta rows
-    const uint4* xs_b = p.xtab + (static_cast<int64_t>(b) * p.A + a) * 2 * S;
-    int issued = 0;
+    int block = X ? a * (p.x.group >> pack) : a;  // of heads
+    const uint4* xs_b = p.xtab + (static_cast<int64_t>(b) * (p.A >> pack) + block) * 2 * qrows;
+    int issued = 0, t = 0;  // t: the tile within the block
     for (int i = 0; i < n_qt && lane == 0; ++i) {
       const int st = i % KV_STAGES;
       if (!ptx::mbar_wait(&q_empty[st], ((i / KV_STAGES) & 1) ^ 1u, lim, p.status, kWaitHint)) break;
-      const uint32_t xbytes = static_cast<uint32_t>(min(BQ2, S - i * BQ2)) * XROW_BYTES;
+      const uint32_t xbytes = static_cast<uint32_t>(min(BQ2, qrows - t * BQ2)) * XROW_BYTES;
       ptx::mbar_arrive_expect_tx(&q_full[st], 2 * QO2_BYTES + 2 * xbytes);
-      ptx::tma_load_2d(smem + KV_Q_OFF + st * QO2_BYTES, &tmQ, &q_full[st], a * HD, row0 + i * BQ2);
-      ptx::tma_load_2d(smem + KV_O_OFF + st * QO2_BYTES, &tmO, &q_full[st], a * HD, row0 + i * BQ2);
+      if constexpr (X) {
+        const int h = block << pack, q0 = (t * BQ2) >> pack;
+        ptx::tma_load_4d(smem + KV_Q_OFF + st * QO2_BYTES, &tmQ, &q_full[st], 0, h, q0, b);
+        ptx::tma_load_4d(smem + KV_O_OFF + st * QO2_BYTES, &tmO, &q_full[st], 0, h, q0, b);
+      } else {
+        ptx::tma_load_2d(smem + KV_Q_OFF + st * QO2_BYTES, &tmQ, &q_full[st], a * HD, row0 + i * BQ2);
+        ptx::tma_load_2d(smem + KV_O_OFF + st * QO2_BYTES, &tmO, &q_full[st], a * HD, row0 + i * BQ2);
+      }
       uint8_t* x = smem + KV_X_OFF + st * 2 * X_BYTES;
-      ptx::bulk_load(x, xs_b + i * BQ2, xbytes, &q_full[st]);
-      ptx::bulk_load(x + X_BYTES, xs_b + S + i * BQ2, xbytes, &q_full[st]);
+      ptx::bulk_load(x, xs_b + t * BQ2, xbytes, &q_full[st]);
+      ptx::bulk_load(x + X_BYTES, xs_b + qrows + t * BQ2, xbytes, &q_full[st]);
       ++issued;
+      ++t;
+      if (X && t == n_q) {  // the next block of heads
+        t = 0;
+        ++block;
+        xs_b += 2 * static_cast<int64_t>(qrows);
+      }
     }
     if (lane == 0) {
       ptx::mbar_wait(kv_full, 0, lim, p.status, kWaitHint);
@@ -1178,7 +1281,7 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
       const bool mine = ptx::mbar_wait(bar, parity, lim, p.status, kWaitHint);
       return __all_sync(0xffffffffu, mine);
     };
-    for (int i = 0; i < n_qt; ++i) {
+    for (int i = 0, t0 = 0; i < n_qt; ++i, t0 = X && t0 + 1 == n_q ? 0 : t0 + 1) {
       if (!wait_all(st_full, i & 1) || !wait_all(dpt_full, i & 1)) { ok = false; break; }
       ptx::tc_fence_after();
       uint32_t sv[32], dv[32];
@@ -1196,7 +1299,7 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
         pp[t >> 1] = ptx::pack_bf16(pt.x, pt.y);
         dd[t >> 1] = ptx::pack_bf16(ds.x, ds.y);
       }
-      const int nq = S - i * BQ2 - hf * 32;  // queries of this half inside the sequence
+      const int nq = qrows - t0 * BQ2 - hf * 32;  // queries of this half inside the sequence
       if (nq < 32) {  // warp-uniform: queries past S
 #pragma unroll
         for (int t = 0; t < 32; t += 2) {
@@ -1243,7 +1346,7 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
                                   __uint_as_float(o[c][8 * u + 2 * t + 1]) * sc);
           ptx::st_shared_v4(orow + (((c * 4 + u) ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
         }
-      if (p.colpart) {  // column sums of the stored values over this warp's 32 rows
+      if (!X && p.colpart) {  // column sums of the stored values over this warp's 32 rows
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           float v[32];
@@ -1253,18 +1356,23 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
           red[(hf * 4 + q4) * 64 + c * 32 + lane] = v[0];
         }
       }
-    } else if (p.colpart) {
+    } else if (!X && p.colpart) {
       red[(hf * 4 + q4) * 64 + lane] = 0.f;
       red[(hf * 4 + q4) * 64 + 32 + lane] = 0.f;
     }
     ptx::fence_proxy_async_smem();  // the staged rows -> the TMA store
     softmax_warps_sync();
     if (warp == 2 && lane == 0) {
-      ptx::tma_store_3d(&tmOut, smem + KV_K_OFF, H + a * HD, k0, b);
-      ptx::tma_store_3d(&tmOut, smem + KV_V_OFF, 2 * H + a * HD, k0, b);
+      if constexpr (X) {
+        ptx::tma_store_4d(&tmOut, smem + KV_K_OFF, 0, a, k0, b);
+        ptx::tma_store_4d(&tmOutV, smem + KV_V_OFF, 0, a, k0, b);
+      } else {
+        ptx::tma_store_3d(&tmOut, smem + KV_K_OFF, H + a * HD, k0, b);
+        ptx::tma_store_3d(&tmOut, smem + KV_V_OFF, 2 * H + a * HD, k0, b);
+      }
       ptx::bulk_commit_group();
     }
-    if (p.colpart && q4 == 0) {  // the four row quarters, added in order, by the quarter-0 warps
+    if (!X && p.colpart && q4 == 0) {  // the four row quarters, added in order, by the quarter-0 warps
       const float* rh = red + hf * 4 * 64;
       float* dst = p.colpart + (static_cast<int64_t>(b) * gridDim.x + kt) * rs + (1 + hf) * H + a * HD;
 #pragma unroll
@@ -1594,6 +1702,66 @@ bool seq_map(CUtensorMap* map, void* base, int B, int S, int W, int rows) {
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// Heads of 64 of [B][rows] rows `ld` values apart: box {64 values, `heads` heads, `take`
+// rows of one sequence}, 128B swizzle; what lies outside is read as zeros and not written.
+bool cross_map(CUtensorMap* map, const void* base, int heads, int rows, int B, int64_t ld, int take_heads, int take) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(HD), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows),
+                        static_cast<cuuint64_t>(B)};
+  cuuint64_t strides[3] = {HD * 2, static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * 2 * rows};
+  cuuint32_t box[4] = {static_cast<cuuint32_t>(HD), static_cast<cuuint32_t>(take_heads), static_cast<cuuint32_t>(take), 1u};
+  cuuint32_t estr[4] = {1u, 1u, 1u, 1u};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// log2 of the heads that share a query tile of `rows` rows: the fewest tiles, then the
+// fewest heads.
+int best_pack(const attn::Geometry& g, int rows) {
+  int best = 0;
+  int64_t least = 0;
+  for (int p = 0; p <= 5 && g.group % (1 << p) == 0; ++p) {
+    const int64_t tiles = ((static_cast<int64_t>(g.Sq) << p) + rows - 1) / rows * (g.A >> p);
+    if (p == 0 || tiles < least) {
+      best = p;
+      least = tiles;
+    }
+  }
+  return best;
+}
+
+// Which form of the forward kernel: see attention_fwd_tc.
+struct FwdForm {
+  bool two;
+  int ks;
+};
+FwdForm fwd_form(int64_t ctas, int tiles) {
+  const int sms = sm_count() > 0 ? sm_count() : 148;
+  return {5 * ctas <= 13 * sms || (tiles >= 24 && ctas <= 6 * sms),
+          tiles >= 12 && 2 * ctas <= sms ? 4 : tiles >= 24 && ctas <= sms ? 2 : 1};
+}
+
+// Calls go<KS, NS> as the form says.
+template <typename F>
+cudaError_t with_form(const FwdForm& f, F&& go) {
+  const std::integral_constant<int, 1> c1{};
+  const std::integral_constant<int, 2> c2{};
+  const std::integral_constant<int, 4> c4{};
+  return !f.two ? go(c1, c1) : f.ks == 1 ? go(c1, c2) : f.ks == 2 ? go(c2, c2) : go(c4, c2);
+}
+template <bool X, int KS, int NS, typename... Args>
+cudaError_t launch_fwd(dim3 grid, cudaStream_t stream, const Args&... args) {
+  auto kern = attn_fwd_tc<KS, NS, X>;
+  constexpr int SMEM = KS > 1 ? kSplitAttentionSmem : FwdShape<NS>::SMEM;
+  static_assert(SMEM >= FwdShape<NS>::SMEM && (KS == 1 || FwdShape<NS>::TMEM_COLS <= 256), "see residency.h");
+  static OncePerDevice once;
+  const cudaError_t attr = allow_smem(once, kern, SMEM);
+  if (attr != cudaSuccess) return attr;
+  return launch_pdl(kern, grid, dim3(NTHR), SMEM, stream, KS, args...);
+}
 }  // namespace
 
 }  // namespace attn_tc
@@ -1614,7 +1782,7 @@ sky_status attention_fwd_tc(const void* qkv, const int32_t* lens, int B, int S, 
     static OncePerDevice once;
     const cudaError_t at = allow_smem(once, attn_fwd_short_tc, FS_SMEM);
     if (at != cudaSuccess) return cuda_fail(at, "attention smem attribute");
-    FwdParams p{S, H, A, lens, static_cast<__nv_bfloat16*>(ctx), lse, status, timeout_ns};
+    FwdParams p{S, H, A, lens, lse, status, timeout_ns, {}};
     const cudaError_t e = launch_pdl(attn_fwd_short_tc, dim3(A, B), dim3(NTHR), FS_SMEM, stream, 1, tq, tout, p);
     count_launches(1);
     return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core attention forward launch");
@@ -1629,29 +1797,17 @@ sky_status attention_fwd_tc(const void* qkv, const int32_t* lens, int B, int S, 
   //  keys in four while that leaves two CTAs an SM and each three tiles: 1024 x 9 heads
   //    (72) 8.3, unsplit 10.0; in two up to one CTA an SM and from 24 tiles on: 2048 x
   //    8 (128) 14.3 and 17.4; 800 x 12 (84, 13 tiles) 8.2 and 7.4.
-  const int sms = sm_count() > 0 ? sm_count() : 148, tiles = ceil_div(S, BKV);
-  const int64_t ctas = static_cast<int64_t>(ceil_div(S, BQ)) * A * B;
-  const bool two = 5 * ctas <= 13 * sms || (tiles >= 24 && ctas <= 6 * sms);
-  const int ks = tiles >= 12 && 2 * ctas <= sms ? 4 : tiles >= 24 && ctas <= sms ? 2 : 1;
+  const int tiles = ceil_div(S, BKV);
+  const FwdForm form = fwd_form(static_cast<int64_t>(ceil_div(S, BQ)) * A * B, tiles);
   SKY_CHECK(head_map(&tq, qkv, T, 3 * H, BQ) && head_map(&tkv, qkv, T, 3 * H, BKV) &&
-                seq_map(&tout, ctx, B, S, H, BQ / ks),
+                seq_map(&tout, ctx, B, S, H, BQ / form.ks),
             SKY_ERR_CUDA,
             "cuTensorMapEncodeTiled failed for the attention operands");
-  FwdParams p{S, H, A, lens, static_cast<__nv_bfloat16*>(ctx), lse, status, timeout_ns};
-  auto go = [&](auto splits, auto bufs) {
+  FwdParams p{S, H, A, lens, lse, status, timeout_ns, {}};
+  const cudaError_t e = with_form(form, [&](auto splits, auto bufs) {
     constexpr int KS = decltype(splits)::value, NS = decltype(bufs)::value;
-    auto kern = attn_fwd_tc<KS, NS>;
-    constexpr int SMEM = KS > 1 ? kSplitAttentionSmem : FwdShape<NS>::SMEM;
-    static_assert(SMEM >= FwdShape<NS>::SMEM && (KS == 1 || FwdShape<NS>::TMEM_COLS <= 256), "see residency.h");
-    static OncePerDevice once;
-    const cudaError_t attr = allow_smem(once, kern, SMEM);
-    if (attr != cudaSuccess) return attr;
-    return launch_pdl(kern, dim3(ceil_div(S, BQ) * KS, A, B), dim3(NTHR), SMEM, stream, KS, tq, tkv, tout, p);
-  };
-  const std::integral_constant<int, 1> c1{};
-  const std::integral_constant<int, 2> c2{};
-  const std::integral_constant<int, 4> c4{};
-  const cudaError_t e = !two ? go(c1, c1) : ks == 1 ? go(c1, c2) : ks == 2 ? go(c2, c2) : go(c4, c2);
+    return launch_fwd<false, KS, NS>(dim3(ceil_div(S, BQ) * KS, A, B), stream, tq, tkv, tkv, tout, p);
+  });
   count_launches(1);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core attention forward launch");
 }
@@ -1670,7 +1826,8 @@ sky_status attention_bwd_short_tc(const void* qkv, const void* ctx, const void* 
   static OncePerDevice once;
   const cudaError_t attr = allow_smem(once, attn_bwd_short_tc, SH_SMEM);
   if (attr != cudaSuccess) return cuda_fail(attr, "attention backward smem attribute");
-  BwdParams p{S, H, A, lens, lse, nullptr, nullptr, static_cast<__nv_bfloat16*>(dqkv), colpart, status, timeout_ns};
+  BwdParams p{S, H, A, lens, lse, nullptr, nullptr, static_cast<__nv_bfloat16*>(dqkv), colpart, status, timeout_ns,
+              {}, nullptr, nullptr, 0, 0};
   const cudaError_t e = launch_pdl(attn_bwd_short_tc, dim3(A, B), dim3(SH_THR), SH_SMEM, stream, 1, tq, to, tc,
                                    tout, p);
   count_launches(1);
@@ -1692,20 +1849,142 @@ sky_status attention_bwd_tc(const void* qkv, const void* dctx, const float* lse,
                 seq_map(&tout, dqkv, B, S, 3 * H, BK2),
             SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the attention backward operands");
   static OncePerDevice once1, once2;
-  const cudaError_t a1 = allow_smem(once1, attn_bwd_dq_tc, DQ_SMEM), a2 = allow_smem(once2, attn_bwd_dkdv_tc, KV_SMEM);
+  const cudaError_t a1 = allow_smem(once1, attn_bwd_dq_tc<false>, DQ_SMEM),
+                    a2 = allow_smem(once2, attn_bwd_dkdv_tc<false>, KV_SMEM);
   if (a1 != cudaSuccess) return cuda_fail(a1, "attention dQ smem attribute");
   if (a2 != cudaSuccess) return cuda_fail(a2, "attention dK/dV smem attribute");
   SKY_CHECK((reinterpret_cast<uintptr_t>(xtab) & 15) == 0, SKY_ERR_INVALID_ARG,
             "attention backward workspace must be 16-byte aligned");
   BwdParams p{S, H, A, lens, lse, delta, xtab, static_cast<__nv_bfloat16*>(dqkv), colpart, status,
-              timeout_ns};
-  cudaError_t e = launch_pdl(attn_bwd_dkdv_tc, dim3(ceil_div(S, BK2), A, B), dim3(NTHR_B), KV_SMEM,
-                             stream, 1, tk128, tq64, to64, tout, p);
+              timeout_ns, {}, nullptr, nullptr, 0, 0};
+  cudaError_t e = launch_pdl(attn_bwd_dkdv_tc<false>, dim3(ceil_div(S, BK2), A, B), dim3(NTHR_B), KV_SMEM,
+                             stream, 1, tk128, tk128, tq64, to64, tout, tout, p);
   if (e == cudaSuccess)
-    e = launch_pdl(attn_bwd_dq_tc, dim3(ceil_div(S, BQ), A, B), dim3(NTHR_B), DQ_SMEM, stream, 1,
-                   tq128, tkv64, to128, tout, p);
+    e = launch_pdl(attn_bwd_dq_tc<false>, dim3(ceil_div(S, BQ), A, B), dim3(NTHR_B), DQ_SMEM, stream, 1,
+                   tq128, tkv64, tkv64, to128, tout, p);
   count_launches(2);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core attention backward launch");
+}
+
+// ------------------------------------------------------- cross attention
+namespace attn_tc {
+// delta[b, a, s] = sum over a head of dctx * ctx, for the dQ kernel, and the dK/dV
+// kernel's per-query rows [B][A >> pack][2][Sq << pack]: the log-sum-exp over c =
+// log2(e)/sqrt(D), then delta, negated and split as its comment says.  Eight lanes of 16
+// bytes a head.
+__global__ void __launch_bounds__(256) attn_delta_cross(const __nv_bfloat16* __restrict__ ctx,
+                                                        const __nv_bfloat16* __restrict__ dctx, int64_t ldo, int S,
+                                                        int A, int pack, int64_t heads, const float* __restrict__ lse,
+                                                        float* __restrict__ delta, uint4* __restrict__ xtab) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t i = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 3;
+  if (i >= heads) return;  // (whole groups of eight lanes)
+  const int l = threadIdx.x & 7;
+  const int64_t row = i / A, b = row / S;
+  const int a = static_cast<int>(i - row * A), s = static_cast<int>(row - b * S);
+  const int64_t at = row * ldo + a * HD + l * 8;
+  const uint4 x = *reinterpret_cast<const uint4*>(ctx + at), y = *reinterpret_cast<const uint4*>(dctx + at);
+  const int64_t sidx = (b * A + a) * S + s;
+  const float lz = l == 0 ? lse[sidx] : 0.f;
+  const __nv_bfloat162* xs = reinterpret_cast<const __nv_bfloat162*>(&x);
+  const __nv_bfloat162* ys = reinterpret_cast<const __nv_bfloat162*>(&y);
+  float acc = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 u = __bfloat1622float2(xs[e]), w = __bfloat1622float2(ys[e]);
+    acc += u.x * w.x + u.y * w.y;
+  }
+  const uint32_t mask = 0xffu << (threadIdx.x & 24);
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) acc += __shfl_xor_sync(mask, acc, o);
+  if (l != 0) return;
+  delta[sidx] = acc;
+  auto row16 = [](float v) {  // -v as [hi, lo, 0, ...] in bf16
+    const __nv_bfloat16 hi = __float2bfloat16_rn(-v);
+    const __nv_bfloat16 lo = __float2bfloat16_rn(-v - __bfloat162float(hi));
+    return make_uint4(static_cast<uint32_t>(__bfloat16_as_ushort(hi)) |
+                          (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16),
+                      0u, 0u, 0u);
+  };
+  uint4* t = xtab + (b * (A >> pack) + (a >> pack)) * 2 * (static_cast<int64_t>(S) << pack) +
+             (static_cast<int64_t>(s) << pack) + (a & ((1 << pack) - 1));
+  t[0] = row16(__fdiv_rn(lz, LOG2E * 0.125f));
+  t[static_cast<int64_t>(S) << pack] = row16(acc);
+}
+}  // namespace attn_tc
+
+bool cross_attention_tc_fits(const attn::Geometry& g, std::initializer_list<const void*> tensors) {
+  bool ok = g.D == attn_tc::HD && (g.ldq | g.ldk | g.ldv | g.ldo) % 8 == 0;
+  for (const void* p : tensors) ok = ok && (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+  // a tensor map's strides stay below 2^40 bytes
+  const int64_t most = std::max(std::max(g.ldq, g.ldo) * g.Sq, std::max(g.ldk, g.ldv) * g.Skv);
+  return ok && most < (int64_t{1} << 38);
+}
+
+sky_status cross_attention_fwd_tc(const attn::Geometry& g, int B, void* ctx, float* lse, cudaStream_t stream) {
+  using namespace attn_tc;
+  const int pack = best_pack(g, BQ), hp = 1 << pack, tiles = ceil_div(static_cast<int64_t>(g.Sq) << pack, BQ);
+  const FwdForm form = fwd_form(static_cast<int64_t>(tiles) * (g.A >> pack) * B, ceil_div(g.Skv, BKV));
+  const int Akv = g.A / g.group;
+  CUtensorMap tq, tk, tv, tout;
+  SKY_CHECK(cross_map(&tq, g.q, g.A, g.Sq, B, g.ldq, hp, BQ >> pack) &&
+                cross_map(&tk, g.k, Akv, g.Skv, B, g.ldk, 1, BKV) && cross_map(&tv, g.v, Akv, g.Skv, B, g.ldv, 1, BKV) &&
+                cross_map(&tout, ctx, g.A, g.Sq, B, g.ldo, hp, BQ / form.ks >> pack),
+            SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the cross attention operands");
+  FwdParams p{g.Sq, 0, g.A, g.lens, lse, g.status, kTimeoutNs, {g.Skv, g.group, pack}};
+  const cudaError_t e = with_form(form, [&](auto splits, auto bufs) {
+    constexpr int KS = decltype(splits)::value, NS = decltype(bufs)::value;
+    return launch_fwd<true, KS, NS>(dim3(tiles * KS, g.A >> pack, B), stream, tq, tk, tv, tout, p);
+  });
+  count_launches(1);
+  return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core cross attention forward launch");
+}
+
+static size_t cross_delta_bytes(const attn::Geometry& g, int B) {
+  return (static_cast<size_t>(B) * g.A * g.Sq * sizeof(float) + 15) & ~size_t{15};
+}
+size_t cross_attention_bwd_tc_ws(const attn::Geometry& g, int B) {
+  return cross_delta_bytes(g, B) + static_cast<size_t>(B) * g.A * g.Sq * 2 * attn_tc::XROW_BYTES;
+}
+
+sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ctx, const void* dctx, const float* lse,
+                                  void* dq, void* dk, void* dv, void* ws, cudaStream_t stream) {
+  using namespace attn_tc;
+  const int packQ = best_pack(g, BQ), packK = best_pack(g, BQ2), hq = 1 << packQ, hk = 1 << packK;
+  const int Akv = g.A / g.group;
+  CUtensorMap tq128, to128, tk64, tv64, tdq, tk128, tv128, tq64, to64, tdk, tdv;
+  SKY_CHECK(cross_map(&tq128, g.q, g.A, g.Sq, B, g.ldq, hq, BQ >> packQ) &&
+                cross_map(&to128, dctx, g.A, g.Sq, B, g.ldo, hq, BQ >> packQ) &&
+                cross_map(&tdq, dq, g.A, g.Sq, B, g.ldq, hq, BQ >> packQ) &&
+                cross_map(&tk64, g.k, Akv, g.Skv, B, g.ldk, 1, BKV) && cross_map(&tv64, g.v, Akv, g.Skv, B, g.ldv, 1, BKV) &&
+                cross_map(&tk128, g.k, Akv, g.Skv, B, g.ldk, 1, BK2) && cross_map(&tv128, g.v, Akv, g.Skv, B, g.ldv, 1, BK2) &&
+                cross_map(&tq64, g.q, g.A, g.Sq, B, g.ldq, hk, BQ2 >> packK) &&
+                cross_map(&to64, dctx, g.A, g.Sq, B, g.ldo, hk, BQ2 >> packK) &&
+                cross_map(&tdk, dk, Akv, g.Skv, B, g.ldk, 1, BK2) && cross_map(&tdv, dv, Akv, g.Skv, B, g.ldv, 1, BK2),
+            SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the cross attention backward operands");
+  static OncePerDevice once1, once2;
+  const cudaError_t a1 = allow_smem(once1, attn_bwd_dq_tc<true>, DQ_SMEM),
+                    a2 = allow_smem(once2, attn_bwd_dkdv_tc<true>, KV_SMEM);
+  if (a1 != cudaSuccess) return cuda_fail(a1, "cross attention dQ smem attribute");
+  if (a2 != cudaSuccess) return cuda_fail(a2, "cross attention dK/dV smem attribute");
+  float* delta = static_cast<float*>(ws);
+  uint4* xtab = reinterpret_cast<uint4*>(static_cast<char*>(ws) + cross_delta_bytes(g, B));
+  const int64_t heads = static_cast<int64_t>(B) * g.Sq * g.A;
+  cudaError_t e = launch_pdl(attn_delta_cross, dim3(ceil_div(heads, 32)), dim3(256), 0, stream, 1,
+                             static_cast<const __nv_bfloat16*>(ctx), static_cast<const __nv_bfloat16*>(dctx), g.ldo,
+                             g.Sq, g.A, packK, heads, lse, delta, xtab);
+  BwdParams p{g.Sq, 0, g.A, g.lens, lse, delta, xtab, nullptr, nullptr, g.status, kTimeoutNs, {g.Skv, g.group, packK},
+              static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv), g.ldk, g.ldv};
+  if (e == cudaSuccess)
+    e = launch_pdl(attn_bwd_dkdv_tc<true>, dim3(ceil_div(g.Skv, BK2), Akv, B), dim3(NTHR_B), KV_SMEM, stream, 1, tk128,
+                   tv128, tq64, to64, tdk, tdv, p);
+  p.x.pack = packQ;
+  if (e == cudaSuccess)
+    e = launch_pdl(attn_bwd_dq_tc<true>, dim3(ceil_div(static_cast<int64_t>(g.Sq) << packQ, BQ), g.A >> packQ, B),
+                   dim3(NTHR_B), DQ_SMEM, stream, 1, tq128, tk64, tv64, to128, tdq, p);
+  count_launches(3);
+  return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core cross attention backward launch");
 }
 
 }  // namespace sky

@@ -6,9 +6,11 @@
 //   dQ = dS K / sqrt(D),  dK = sum of dS^T Q / sqrt(D),  dV = sum of P^T dctx
 // over the query heads of a key head.
 #include <algorithm>
+#include <type_traits>
 
 #include "abi.h"
 #include "attention_simt.h"
+#include "attention_tc.h"
 #include "common.cuh"
 
 namespace sky {
@@ -45,12 +47,15 @@ attn::Geometry geometry(const sky_cross_shape& s, const void* q, const void* k, 
           s.head_dim, 0, false, len, 0, status};
 }
 
-size_t workspace(const sky_cross_shape& s) {  // delta
-  return static_cast<size_t>(s.batch) * s.heads * s.q_len * sizeof(float);
+// The most that any choice of kernels takes: pointers, which it depends on, are not known.
+size_t workspace(const sky_cross_shape& s) {
+  return cross_attention_bwd_tc_ws(geometry(s, nullptr, nullptr, nullptr, nullptr, nullptr), s.batch);
 }
 
 template <typename T>
 sky_status forward(const sky_cross_shape& s, const attn::Geometry& g, void* ctx, float* lse, cudaStream_t st) {
+  if (std::is_same<T, __nv_bfloat16>::value && cross_attention_tc_fits(g, {g.q, g.k, g.v, ctx}))
+    return cross_attention_fwd_tc(g, s.batch, ctx, lse, st);
   const cudaError_t e = attn::launch_fwd_simt(g, s.batch, static_cast<T*>(ctx), lse, st);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "cross attention forward launch");
 }
@@ -58,6 +63,8 @@ sky_status forward(const sky_cross_shape& s, const attn::Geometry& g, void* ctx,
 template <typename T>
 sky_status backward(const sky_cross_shape& s, const attn::Geometry& g, const void* ctx, const void* dctx,
                     const float* lse, void* dq, void* dk, void* dv, void* ws, cudaStream_t st) {
+  if (std::is_same<T, __nv_bfloat16>::value && cross_attention_tc_fits(g, {g.q, g.k, g.v, ctx, dctx, dq, dk, dv}))
+    return cross_attention_bwd_tc(g, s.batch, ctx, dctx, lse, dq, dk, dv, ws, st);
   const cudaError_t e =
       attn::launch_bwd_simt(g, s.batch, static_cast<const T*>(ctx), static_cast<const T*>(dctx), lse,
                             static_cast<float*>(ws), static_cast<T*>(dq), static_cast<T*>(dk), static_cast<T*>(dv), st);
