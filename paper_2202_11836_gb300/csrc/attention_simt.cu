@@ -8,19 +8,10 @@
 
 #include "attention_simt.h"
 #include "common.cuh"
+#include "row4.cuh"
 
 namespace sky {
 namespace attn {
-
-// The valid keys of sequence b; a bad length is clamped and reported.
-__device__ __forceinline__ int valid_keys(const Geometry& g, int b) {
-  int len = g.lens[b];
-  if (len < g.least || len > g.Skv) {
-    if (g.status && threadIdx.x == 0) atomicOr(g.status, kStatusBadLength);
-    len = len < g.least ? g.least : g.Skv;
-  }
-  return len;
-}
 
 // delta[b, a, s] = sum_d dctx * ctx: one warp per (row, head), rows of ldo.
 template <typename T>
@@ -70,18 +61,6 @@ struct Stage {  // a tile's 16 NC rows: BATCHES of PASSES passes, R rows each
   static constexpr int OWN = FR * G / F_THR;  // passes of the CTA's FR rows
   static constexpr int CC = G > 16 ? G / 16 : 1;  // 64-value column groups of an output row
 };
-// Four values of a row
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16),
-                     __uint_as_float(w.y & 0xffff0000u));
-}
-__device__ __forceinline__ void store4(float* p, const float4& v) { *reinterpret_cast<float4*>(p) = v; }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float4& v) {
-  __nv_bfloat162 w[2] = {__floats2bfloat162_rn(v.x, v.y), __floats2bfloat162_rn(v.z, v.w)};
-  *reinterpret_cast<uint2*>(p) = *reinterpret_cast<uint2*>(w);
-}
 // Rows from `rows` on are zeros.  vec: D, ld and X allow load4.
 template <int G, typename T, int N>
 __device__ __forceinline__ void load_rows(const T* __restrict__ X, int64_t ld, int r0, int rows, int D, bool vec,

@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "common.cuh"
+
 namespace sky {
 namespace attn {
 
@@ -21,6 +23,16 @@ struct Geometry {
   int least;              // of a length: 1, or 0 where a sequence may have no keys
   int32_t* status;
 };
+
+// The valid keys of sequence b; a bad length is clamped and reported.
+__device__ __forceinline__ int valid_keys(const Geometry& g, int b) {
+  int len = g.lens[b];
+  if (len < g.least || len > g.Skv) {
+    if (g.status && threadIdx.x == 0) atomicOr(g.status, kStatusBadLength);
+    len = len < g.least ? g.least : g.Skv;
+  }
+  return len;
+}
 
 // T: float or __nv_bfloat16.  lse may be null.
 template <typename T>

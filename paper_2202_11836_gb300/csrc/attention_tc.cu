@@ -1703,8 +1703,8 @@ bool seq_map(CUtensorMap* map, void* base, int B, int S, int W, int rows) {
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Heads of 64 of [B][rows] rows `ld` values apart: box {64 values, `heads` heads, `take`
-// rows of one sequence}, 128B swizzle; what lies outside is read as zeros and not written.
+}  // namespace
+
 bool cross_map(CUtensorMap* map, const void* base, int heads, int rows, int B, int64_t ld, int take_heads, int take) {
   auto fn = encode_fn();
   if (!fn) return false;
@@ -1718,6 +1718,7 @@ bool cross_map(CUtensorMap* map, const void* base, int heads, int rows, int B, i
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+namespace {
 // log2 of the heads that share a query tile of `rows` rows: the fewest tiles, then the
 // fewest heads.
 int best_pack(const attn::Geometry& g, int rows) {

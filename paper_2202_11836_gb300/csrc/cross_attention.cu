@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "abi.h"
+#include "attention_few.h"
 #include "attention_simt.h"
 #include "attention_tc.h"
 #include "common.cuh"
@@ -55,7 +56,9 @@ size_t workspace(const sky_cross_shape& s) {
 template <typename T>
 sky_status forward(const sky_cross_shape& s, const attn::Geometry& g, void* ctx, float* lse, cudaStream_t st) {
   if (std::is_same<T, __nv_bfloat16>::value && cross_attention_tc_fits(g, {g.q, g.k, g.v, ctx}))
-    return cross_attention_fwd_tc(g, s.batch, ctx, lse, st);
+    return cross_attention_few_fits(g) ? cross_attention_few(g, s.batch, ctx, lse, st)
+                                       : cross_attention_fwd_tc(g, s.batch, ctx, lse, st);
+  if (cross_attention_few_simt_pays(g, s.batch)) return cross_attention_few_simt(g, s.batch, static_cast<T*>(ctx), lse, st);
   const cudaError_t e = attn::launch_fwd_simt(g, s.batch, static_cast<T*>(ctx), lse, st);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "cross attention forward launch");
 }

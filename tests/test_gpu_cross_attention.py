@@ -284,6 +284,16 @@ def test_few_query_rows(sq, heads, kv_heads, skv, lens, dtype):
     c.check_backward(c.backward(*c.given()))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("sq,heads,kv_heads,dim,shift", [(1, 3, 3, 20, 0), (1, 4, 1, 33, 1), (2, 6, 2, 128, 0),
+                                                         (4, 8, 2, 80, 4), (3, 14, 1, 64, 1), (1, 2, 2, 3, 0),
+                                                         (1, 1, 1, 32, 0), (4, 1, 1, 100, 0)])
+def test_few_query_rows_of_other_heads(sq, heads, kv_heads, dim, shift, dtype):
+    c = Case(sq, 650, heads, kv_heads, [650, 0, 1, 31, 32, 33, 300], dtype=dtype, dim=dim, beside=shift,
+             shift=shift).poison()
+    c.check_forward(*c.forward())
+
+
 def test_captured_and_replayed():
     c = Case(33, 150, 4, 2, [150, 80])
     ctx, (dq, dk, dv) = c.new["ctx"](), [c.new[n]() for n in ("dq", "dk", "dv")]
