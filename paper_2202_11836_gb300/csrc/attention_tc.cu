@@ -1409,10 +1409,18 @@ constexpr int SH_SMEM = SH_BAR + 128;
 constexpr int SH_THR = 320;  // warp 0 TMA, warp 1 MMA issue, warps 2..9 softmax
 static_assert(2 * (SH_SMEM + 1024) <= 233472, "two CTAs per SM");
 
+// X: a key head's queries, S of each of the 2^pack heads that share it, are the tile's
+// rows; maps of Q, K, V and of dQ, dK, dV.
+struct ShortMaps {
+  CUtensorMap k, v, dk, dv;
+};
+
+template <bool X>
 __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_constant__ CUtensorMap tmQKV,
                                                                const __grid_constant__ CUtensorMap tmO,
                                                                const __grid_constant__ CUtensorMap tmC,
                                                                const __grid_constant__ CUtensorMap tmOut,
+                                                               const __grid_constant__ ShortMaps tmX,
                                                                const BwdParams p) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* qk_full = reinterpret_cast<uint64_t*>(smem + SH_BAR);
@@ -1423,7 +1431,8 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(g_full + 1);
 
   const int a = blockIdx.x, b = blockIdx.y;
-  const int S = p.S, H = p.H;
+  const int pack = X ? p.x.pack : 0, head0 = a << pack;
+  const int S = p.S << pack, H = p.H;  // rows of the tile that hold a query
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row0 = b * S;
   const uint64_t lim = p.timeout_ns;
@@ -1450,21 +1459,28 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
   const uint32_t tS = tmem, tdP = tmem + 128;                      // 128 columns each
   const uint32_t tdV = tmem, tdK = tmem + 64, tdQ = tmem + 128;    // over them, 64 each
   pdl_wait();
-  int len = p.lens[b];
-  if (len < 1 || len > S) {
-    if (p.status && threadIdx.x == 0) atomicOr(p.status, kStatusBadLength);
-    len = len < 1 ? 1 : S;
-  }
+  const int len = valid_keys(p.lens, b, X ? 0 : 1, X ? p.x.Skv : S, p.status);
 
   if (warp == 0) {
     if (lane == 0) {
       ptx::mbar_arrive_expect_tx(qk_full, 2 * Q_BYTES);
-      ptx::tma_load_2d(smem + SH_Q, &tmQKV, qk_full, a * HD, row0);
-      ptx::tma_load_2d(smem + SH_K, &tmQKV, qk_full, H + a * HD, row0);
+      if constexpr (X) {
+        ptx::tma_load_4d(smem + SH_Q, &tmQKV, qk_full, 0, head0, 0, b);
+        ptx::tma_load_4d(smem + SH_K, &tmX.k, qk_full, 0, a, 0, b);
+      } else {
+        ptx::tma_load_2d(smem + SH_Q, &tmQKV, qk_full, a * HD, row0);
+        ptx::tma_load_2d(smem + SH_K, &tmQKV, qk_full, H + a * HD, row0);
+      }
       ptx::mbar_arrive_expect_tx(ov_full, 3 * Q_BYTES);
-      ptx::tma_load_2d(smem + SH_O, &tmO, ov_full, a * HD, row0);
-      ptx::tma_load_2d(smem + SH_DS, &tmC, ov_full, a * HD, row0);  // ctx, until dS is formed
-      ptx::tma_load_2d(smem + SH_V, &tmQKV, ov_full, 2 * H + a * HD, row0);
+      if constexpr (X) {
+        ptx::tma_load_4d(smem + SH_O, &tmO, ov_full, 0, head0, 0, b);
+        ptx::tma_load_4d(smem + SH_DS, &tmC, ov_full, 0, head0, 0, b);
+        ptx::tma_load_4d(smem + SH_V, &tmX.v, ov_full, 0, a, 0, b);
+      } else {
+        ptx::tma_load_2d(smem + SH_O, &tmO, ov_full, a * HD, row0);
+        ptx::tma_load_2d(smem + SH_DS, &tmC, ov_full, a * HD, row0);  // ctx, until dS is formed
+        ptx::tma_load_2d(smem + SH_V, &tmQKV, ov_full, 2 * H + a * HD, row0);
+      }
       // bounded waits for the copies before the CTA may exit
       ptx::mbar_wait(qk_full, 0, lim, p.status, kWaitHint);
       ptx::mbar_wait(ov_full, 0, lim, p.status, kWaitHint);
@@ -1534,7 +1550,10 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
     const uint32_t lane_base = static_cast<uint32_t>(q4 * 32) << 16;
     const float sl2 = LOG2E * 0.125f;
     const bool live = r < S;
-    const float nlse2 = live ? -p.lse[(static_cast<int64_t>(b) * p.A + a) * S + r] : 0.f;
+    const float nlse2 =
+        !live ? 0.f
+        : X   ? -p.lse[(static_cast<int64_t>(b) * p.A + head0 + (r & ((1 << pack) - 1))) * p.S + (r >> pack)]
+              : -p.lse[(static_cast<int64_t>(b) * p.A + a) * S + r];
     auto wait_all = [&](uint64_t* bar) {
       return __all_sync(0xffffffffu, ptx::mbar_wait(bar, 0, lim, p.status, kWaitHint));
     };
@@ -1592,6 +1611,11 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
           ptx::st_shared_v4(sd + at, dd[0], dd[1], dd[2], dd[3]);
         }
       }
+      if (X && (len & 15)) {  // the products' last 16-row block of keys: dS is 0 behind, and K anything
+        const uint32_t k0 = ptx::smem_u32(smem + SH_K) + len * 128;
+        const int i = hf * 128 + r;  // the rows' 16-byte pieces
+        if (i < (16 - (len & 15)) * 8) ptx::st_shared_v4(k0 + i * 16, 0, 0, 0, 0);
+      }
       ptx::fence_proxy_async_smem();  // P, dS -> the MMAs
       ptx::tc_fence_before();
       ptx::mbar_arrive(pds_full);
@@ -1614,6 +1638,10 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
         uint32_t o[32];
         ptx::tmem_ld_32x32b_x32((is_q ? tdQ : (hf == 0 ? tdK : tdV)) + lane_base + col, o);
         ptx::tmem_ld_wait();
+        if (X && (is_q ? len == 0 : r >= len)) {  // queries without keys; keys past the valid length
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0u;
+        }
         const float m = is_q ? 0.125f : sc;
         const uint32_t orow = ptx::smem_u32(smem + (is_q ? SH_Q : (hf == 0 ? SH_K : SH_V))) + r * 128;
 #pragma unroll
@@ -1624,7 +1652,7 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
             w[t] = ptx::pack_bf16(__uint_as_float(o[8 * u + 2 * t]) * m, __uint_as_float(o[8 * u + 2 * t + 1]) * m);
           ptx::st_shared_v4(orow + (((col / 8 + u) ^ (r & 7)) << 4), w[0], w[1], w[2], w[3]);
         }
-        if (p.colpart) {  // column sums of the stored values over this warp's 32 rows
+        if (!X && p.colpart) {  // column sums of the stored values over this warp's 32 rows
           float v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = live ? bf16_round(__uint_as_float(o[j]) * m) : 0.f;
@@ -1632,20 +1660,26 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
           red[((is_q ? 0 : sel) * 4 + q4) * 64 + col + lane] = v[0];
         }
       }
-    } else if (p.colpart) {
+    } else if (!X && p.colpart) {
       red[(hf == 0 ? 1 : 2) * 256 + q4 * 64 + lane] = red[(hf == 0 ? 1 : 2) * 256 + q4 * 64 + 32 + lane] = 0.f;
       red[q4 * 64 + hf * 32 + lane] = 0.f;
     }
     ptx::fence_proxy_async_smem();  // the staged rows -> the TMA stores
     softmax_warps_sync();
     if (warp == 2 && lane == 0) {
-      ptx::tma_store_3d(&tmOut, smem + SH_Q, a * HD, 0, b);
-      ptx::tma_store_3d(&tmOut, smem + SH_K, H + a * HD, 0, b);
-      ptx::tma_store_3d(&tmOut, smem + SH_V, 2 * H + a * HD, 0, b);
+      if constexpr (X) {
+        ptx::tma_store_4d(&tmOut, smem + SH_Q, 0, head0, 0, b);
+        ptx::tma_store_4d(&tmX.dk, smem + SH_K, 0, a, 0, b);
+        ptx::tma_store_4d(&tmX.dv, smem + SH_V, 0, a, 0, b);
+      } else {
+        ptx::tma_store_3d(&tmOut, smem + SH_Q, a * HD, 0, b);
+        ptx::tma_store_3d(&tmOut, smem + SH_K, H + a * HD, 0, b);
+        ptx::tma_store_3d(&tmOut, smem + SH_V, 2 * H + a * HD, 0, b);
+      }
       ptx::bulk_commit_group();
     }
     const int t = static_cast<int>(threadIdx.x) - 64;
-    if (p.colpart && t < 3 * HD) {  // the four row quarters, added in order
+    if (!X && p.colpart && t < 3 * HD) {  // the four row quarters, added in order
       const int g = t / HD, c = t % HD;
       const float* x = red + g * 256 + c;
       p.colpart[static_cast<int64_t>(b) * 3 * H + g * H + a * HD + c] = ((x[0] + x[64]) + x[128]) + x[192];
@@ -1825,12 +1859,12 @@ sky_status attention_bwd_short_tc(const void* qkv, const void* ctx, const void* 
                 seq_map(&tout, dqkv, B, S, 3 * H, BQ),
             SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the attention backward operands");
   static OncePerDevice once;
-  const cudaError_t attr = allow_smem(once, attn_bwd_short_tc, SH_SMEM);
+  const cudaError_t attr = allow_smem(once, attn_bwd_short_tc<false>, SH_SMEM);
   if (attr != cudaSuccess) return cuda_fail(attr, "attention backward smem attribute");
   BwdParams p{S, H, A, lens, lse, nullptr, nullptr, static_cast<__nv_bfloat16*>(dqkv), colpart, status, timeout_ns,
               {}, nullptr, nullptr, 0, 0};
-  const cudaError_t e = launch_pdl(attn_bwd_short_tc, dim3(A, B), dim3(SH_THR), SH_SMEM, stream, 1, tq, to, tc,
-                                   tout, p);
+  const cudaError_t e = launch_pdl(attn_bwd_short_tc<false>, dim3(A, B), dim3(SH_THR), SH_SMEM, stream, 1, tq, to, tc,
+                                   tout, ShortMaps{}, p);
   count_launches(1);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core attention backward launch");
 }
@@ -1872,46 +1906,57 @@ namespace attn_tc {
 // delta[b, a, s] = sum over a head of dctx * ctx, for the dQ kernel, and the dK/dV
 // kernel's per-query rows [B][A >> pack][2][Sq << pack]: the log-sum-exp over c =
 // log2(e)/sqrt(D), then delta, negated and split as its comment says.  Eight lanes of 16
-// bytes a head.
+// bytes a head, DELTA_HEADS heads in flight.
+constexpr int DELTA_HEADS = 4;
 __global__ void __launch_bounds__(256) attn_delta_cross(const __nv_bfloat16* __restrict__ ctx,
                                                         const __nv_bfloat16* __restrict__ dctx, int64_t ldo, int S,
                                                         int A, int pack, int64_t heads, const float* __restrict__ lse,
                                                         float* __restrict__ delta, uint4* __restrict__ xtab) {
   pdl_wait();
   pdl_trigger();
-  const int64_t i = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 3;
-  if (i >= heads) return;  // (whole groups of eight lanes)
   const int l = threadIdx.x & 7;
-  const int64_t row = i / A, b = row / S;
-  const int a = static_cast<int>(i - row * A), s = static_cast<int>(row - b * S);
-  const int64_t at = row * ldo + a * HD + l * 8;
-  const uint4 x = *reinterpret_cast<const uint4*>(ctx + at), y = *reinterpret_cast<const uint4*>(dctx + at);
-  const int64_t sidx = (b * A + a) * S + s;
-  const float lz = l == 0 ? lse[sidx] : 0.f;
-  const __nv_bfloat162* xs = reinterpret_cast<const __nv_bfloat162*>(&x);
-  const __nv_bfloat162* ys = reinterpret_cast<const __nv_bfloat162*>(&y);
-  float acc = 0.f;
+  const int64_t i0 = static_cast<int64_t>(blockIdx.x) * (32 * DELTA_HEADS) + (threadIdx.x >> 3);  // head: i0 + 32 n
+  uint4 x[DELTA_HEADS], y[DELTA_HEADS];
+  float lz[DELTA_HEADS];
+  int64_t b[DELTA_HEADS];
+  int a[DELTA_HEADS], s[DELTA_HEADS];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 u = __bfloat1622float2(xs[e]), w = __bfloat1622float2(ys[e]);
-    acc += u.x * w.x + u.y * w.y;
+  for (int n = 0; n < DELTA_HEADS; ++n) {
+    const int64_t i = i0 + 32 * n < heads ? i0 + 32 * n : 0, row = i / A;
+    b[n] = row / S;
+    a[n] = static_cast<int>(i - row * A);
+    s[n] = static_cast<int>(row - b[n] * S);
+    const int64_t at = row * ldo + a[n] * HD + l * 8;
+    x[n] = *reinterpret_cast<const uint4*>(ctx + at);
+    y[n] = *reinterpret_cast<const uint4*>(dctx + at);
+    lz[n] = l == 0 ? lse[(b[n] * A + a[n]) * S + s[n]] : 0.f;
   }
-  const uint32_t mask = 0xffu << (threadIdx.x & 24);
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) acc += __shfl_xor_sync(mask, acc, o);
-  if (l != 0) return;
-  delta[sidx] = acc;
-  auto row16 = [](float v) {  // -v as [hi, lo, 0, ...] in bf16
-    const __nv_bfloat16 hi = __float2bfloat16_rn(-v);
-    const __nv_bfloat16 lo = __float2bfloat16_rn(-v - __bfloat162float(hi));
-    return make_uint4(static_cast<uint32_t>(__bfloat16_as_ushort(hi)) |
-                          (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16),
-                      0u, 0u, 0u);
-  };
-  uint4* t = xtab + (b * (A >> pack) + (a >> pack)) * 2 * (static_cast<int64_t>(S) << pack) +
-             (static_cast<int64_t>(s) << pack) + (a & ((1 << pack) - 1));
-  t[0] = row16(__fdiv_rn(lz, LOG2E * 0.125f));
-  t[static_cast<int64_t>(S) << pack] = row16(acc);
+  for (int n = 0; n < DELTA_HEADS; ++n) {
+    const __nv_bfloat162* xs = reinterpret_cast<const __nv_bfloat162*>(&x[n]);
+    const __nv_bfloat162* ys = reinterpret_cast<const __nv_bfloat162*>(&y[n]);
+    float acc = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 u = __bfloat1622float2(xs[e]), w = __bfloat1622float2(ys[e]);
+      acc += u.x * w.x + u.y * w.y;
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+    if (l != 0 || i0 + 32 * n >= heads) continue;
+    delta[(b[n] * A + a[n]) * S + s[n]] = acc;
+    auto row16 = [](float v) {  // -v as [hi, lo, 0, ...] in bf16
+      const __nv_bfloat16 hi = __float2bfloat16_rn(-v);
+      const __nv_bfloat16 lo = __float2bfloat16_rn(-v - __bfloat162float(hi));
+      return make_uint4(static_cast<uint32_t>(__bfloat16_as_ushort(hi)) |
+                            (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16),
+                        0u, 0u, 0u);
+    };
+    uint4* t = xtab + (b[n] * (A >> pack) + (a[n] >> pack)) * 2 * (static_cast<int64_t>(S) << pack) +
+               (static_cast<int64_t>(s[n]) << pack) + (a[n] & ((1 << pack) - 1));
+    t[0] = row16(__fdiv_rn(lz[n], LOG2E * 0.125f));
+    t[static_cast<int64_t>(S) << pack] = row16(acc);
+  }
 }
 }  // namespace attn_tc
 
@@ -1949,9 +1994,37 @@ size_t cross_attention_bwd_tc_ws(const attn::Geometry& g, int B) {
   return cross_delta_bytes(g, B) + static_cast<size_t>(B) * g.A * g.Sq * 2 * attn_tc::XROW_BYTES;
 }
 
+// One tile of queries, of all heads that share a key head, and one of keys: everything in
+// one launch.
+static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, int pack, const void* ctx,
+                                               const void* dctx, const float* lse, void* dq, void* dk, void* dv,
+                                               cudaStream_t stream) {
+  using namespace attn_tc;
+  const int hp = 1 << pack, take = BQ >> pack, Akv = g.A / g.group;
+  CUtensorMap tq, to, tc, tdq;
+  ShortMaps x;
+  SKY_CHECK(cross_map(&tq, g.q, g.A, g.Sq, B, g.ldq, hp, take) && cross_map(&to, dctx, g.A, g.Sq, B, g.ldo, hp, take) &&
+                cross_map(&tc, ctx, g.A, g.Sq, B, g.ldo, hp, take) && cross_map(&tdq, dq, g.A, g.Sq, B, g.ldq, hp, take) &&
+                cross_map(&x.k, g.k, Akv, g.Skv, B, g.ldk, 1, BQ) && cross_map(&x.v, g.v, Akv, g.Skv, B, g.ldv, 1, BQ) &&
+                cross_map(&x.dk, dk, Akv, g.Skv, B, g.ldk, 1, BQ) && cross_map(&x.dv, dv, Akv, g.Skv, B, g.ldv, 1, BQ),
+            SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the cross attention backward operands");
+  static OncePerDevice once;
+  const cudaError_t attr = allow_smem(once, attn_bwd_short_tc<true>, SH_SMEM);
+  if (attr != cudaSuccess) return cuda_fail(attr, "cross attention backward smem attribute");
+  const BwdParams p{g.Sq, 0, g.A, g.lens, lse, nullptr, nullptr, nullptr, nullptr, g.status, kTimeoutNs,
+                    {g.Skv, g.group, pack}, nullptr, nullptr, 0, 0};
+  const cudaError_t e = launch_pdl(attn_bwd_short_tc<true>, dim3(Akv, B), dim3(SH_THR), SH_SMEM, stream, 1, tq, to, tc,
+                                   tdq, x, p);
+  count_launches(1);
+  return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core cross attention backward launch");
+}
+
 sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ctx, const void* dctx, const float* lse,
                                   void* dq, void* dk, void* dv, void* ws, cudaStream_t stream) {
   using namespace attn_tc;
+  for (int pack = 0; pack <= 7; ++pack)
+    if (g.group == 1 << pack && static_cast<int64_t>(g.Sq) << pack <= BQ && g.Skv <= BQ)
+      return cross_attention_bwd_short_tc(g, B, pack, ctx, dctx, lse, dq, dk, dv, stream);
   const int packQ = best_pack(g, BQ), packK = best_pack(g, BQ2), hq = 1 << packQ, hk = 1 << packK;
   const int Akv = g.A / g.group;
   CUtensorMap tq128, to128, tk64, tv64, tdq, tk128, tv128, tq64, to64, tdk, tdv;
@@ -1972,7 +2045,7 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ct
   float* delta = static_cast<float*>(ws);
   uint4* xtab = reinterpret_cast<uint4*>(static_cast<char*>(ws) + cross_delta_bytes(g, B));
   const int64_t heads = static_cast<int64_t>(B) * g.Sq * g.A;
-  cudaError_t e = launch_pdl(attn_delta_cross, dim3(ceil_div(heads, 32)), dim3(256), 0, stream, 1,
+  cudaError_t e = launch_pdl(attn_delta_cross, dim3(ceil_div(heads, 32 * DELTA_HEADS)), dim3(256), 0, stream, 1,
                              static_cast<const __nv_bfloat16*>(ctx), static_cast<const __nv_bfloat16*>(dctx), g.ldo,
                              g.Sq, g.A, packK, heads, lse, delta, xtab);
   BwdParams p{g.Sq, 0, g.A, g.lens, lse, delta, xtab, nullptr, nullptr, g.status, kTimeoutNs, {g.Skv, g.group, packK},

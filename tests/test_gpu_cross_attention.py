@@ -204,6 +204,10 @@ SHAPES = [
     (200, 333, 12, 4, [333, 65, 0]),
     (257, 514, 4, 4, [514, 1]),
     (300, 80, 16, 2, [80, 40, 17]),
+    (30, 100, 8, 2, [100, 0, 99, 1]),   # one tile holds every head of a key head
+    (1, 17, 128, 1, [17, 0, 16]),
+    (127, 127, 2, 2, [127, 126, 0]),
+    (129, 128, 2, 2, [128, 3]),
 ]
 
 
