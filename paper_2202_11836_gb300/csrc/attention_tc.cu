@@ -751,7 +751,42 @@ __device__ __forceinline__ void softmax_warps_sync() {
   asm volatile("bar.sync 1, 256;" ::: "memory");
 }
 
-template <bool X>
+static_assert(DQ_SMEM >= kSplitAttentionSmem, "clusters that hold 256 columns: see residency.h");
+// A CTA's part of a 128 x 64 fp32 sum that a cluster's CTAs share: 16-byte group g of row r
+// at group g ^ (r & 7) of the row.  Columns 32 half .. of the thread's row r.
+constexpr int PART_BYTES = 128 * 64 * 4;
+__device__ __forceinline__ void put_part(uint8_t* part, int r, int half, bool any, const uint32_t (&o)[32]) {
+  const uint32_t row = ptx::smem_u32(part) + r * 256;
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+    ptx::st_shared_v4(row + (((half * 8 + u) ^ (r & 7)) << 4), any ? o[4 * u] : 0u, any ? o[4 * u + 1] : 0u,
+                      any ? o[4 * u + 2] : 0u, any ? o[4 * u + 3] : 0u);
+}
+// This CTA's 128 / KS rows of the sum, in split order, times sc, as bf16 in 128-byte
+// swizzled rows of `stage`; rows from `live` on of all 128 are zeros.  128 threads.
+template <int KS>
+__device__ __forceinline__ void add_parts(const uint8_t* part, uint8_t* stage, int t, int split, float sc, int live) {
+  constexpr int ROWS = 128 / KS, G = 16 / KS;
+  const int lr = t / KS, sub = t % KS, row = split * ROWS + lr;
+  const uint32_t src = ptx::smem_u32(part) + row * 256, dst = ptx::smem_u32(stage) + lr * 128;
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    const int g = sub + KS * i;
+    float4 x[KS], o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) x[s] = ptx::ld_cluster_f4(ptx::mapa_shared(src + ((g ^ (row & 7)) << 4), s));
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      o.x += x[s].x; o.y += x[s].y; o.z += x[s].z; o.w += x[s].w;
+    }
+    if (row >= live) o = make_float4(0.f, 0.f, 0.f, 0.f);
+    ptx::st_shared_v2(dst + (((g >> 1) ^ (lr & 7)) << 4) + (g & 1) * 8, ptx::pack_bf16(o.x * sc, o.y * sc),
+                      ptx::pack_bf16(o.z * sc, o.w * sc));
+  }
+}
+
+// KS > 1 (X): the CTAs of a cluster share a block's keys and add their parts.
+template <bool X, int KS = 1>
 __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorMap tmQ,
                                                           const __grid_constant__ CUtensorMap tmKV,
                                                           const __grid_constant__ CUtensorMap tmV,  // X
@@ -777,11 +812,12 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
 
   const int pack = X ? p.x.pack : 0;
-  const int qt = blockIdx.x, a = blockIdx.y << pack, b = blockIdx.z;  // (first) head
+  const int qt = blockIdx.x / KS, split = blockIdx.x % KS, a = blockIdx.y << pack, b = blockIdx.z;  // (first) head
   const int S = p.S, H = p.H;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int len = valid_keys(p.lens, b, X ? 0 : 1, X ? p.x.Skv : S, p.status);
-  const int n_kt = (len + BKV - 1) / BKV;
+  const int n_all = (len + BKV - 1) / BKV, j0 = split * n_all / KS;
+  const int n_kt = (split + 1) * n_all / KS - j0;  // this CTA's key tiles
   const int row0 = b * S, q0 = qt * (BQ >> pack);
   const int kvh = X ? a / p.x.group : 0;
   const uint64_t lim = p.timeout_ns;
@@ -834,8 +870,8 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
         uint8_t* kv = smem + DQ_KV_OFF + st * 2 * KV_BYTES;
         ptx::mbar_arrive_expect_tx(&kv_full[st], 2 * KV_BYTES);
         if constexpr (X) {
-          ptx::tma_load_4d(kv, &tmKV, &kv_full[st], 0, kvh, j * BKV, b);
-          ptx::tma_load_4d(kv + KV_BYTES, &tmV, &kv_full[st], 0, kvh, j * BKV, b);
+          ptx::tma_load_4d(kv, &tmKV, &kv_full[st], 0, kvh, (j0 + j) * BKV, b);
+          ptx::tma_load_4d(kv + KV_BYTES, &tmV, &kv_full[st], 0, kvh, (j0 + j) * BKV, b);
         } else {
           ptx::tma_load_2d(kv, &tmKV, &kv_full[st], H + a * HD, row0 + j * BKV);
           ptx::tma_load_2d(kv + KV_BYTES, &tmKV, &kv_full[st], 2 * H + a * HD, row0 + j * BKV);
@@ -929,10 +965,10 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
       ptx::tmem_ld_wait();
       ptx::tc_fence_before();
       ptx::mbar_arrive(s_free);
-      const int kbase = j * BKV + hf * 32;
-      if (X && j * BKV + BKV > len) {  // dS is 0 there, and K anything; S_j and dP_j have read it
+      const int kbase = (j0 + j) * BKV + hf * 32;
+      if (X && (j0 + j) * BKV + BKV > len) {  // dS is 0 there, and K anything; S_j and dP_j have read it
         if (!wait_all(&kv_full[j % DQ_STAGES], (j / DQ_STAGES) & 1)) { ok = false; break; }
-        clear_rows(smem + DQ_KV_OFF + (j % DQ_STAGES) * 2 * KV_BYTES, len - j * BKV, r + hf * 128, NSM_B);
+        clear_rows(smem + DQ_KV_OFF + (j % DQ_STAGES) * 2 * KV_BYTES, len - (j0 + j) * BKV, r + hf * 128, NSM_B);
         ptx::fence_proxy_async_smem();
       }
       uint32_t pk[16];
@@ -973,8 +1009,9 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
       uint32_t o[32];
       ptx::tmem_ld_32x32b_x32(tdQ + lane_base + hf * 32, o);
       ptx::tmem_ld_wait();
+      if constexpr (KS > 1) put_part(smem, r, hf, any, o);  // over Q and dO
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < (KS > 1 ? 0 : 4); ++u) {
         uint32_t w[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -993,19 +1030,38 @@ __global__ void __maxnreg__(80) attn_bwd_dq_tc(const __grid_constant__ CUtensorM
     } else if (!X && p.colpart) {
       red[q4 * 64 + hf * 32 + lane] = 0.f;
     }
-    ptx::fence_proxy_async_smem();  // the staged rows -> the TMA store
-    softmax_warps_sync();
-    if (warp == 2 && lane == 0) {
-      if constexpr (X) ptx::tma_store_4d(&tmOut, smem + DQ_Q_OFF, 0, a, q0, b);
-      else ptx::tma_store_3d(&tmOut, smem + DQ_Q_OFF, a * HD, q0, b);
-      ptx::bulk_commit_group();
+    if constexpr (KS == 1) {
+      ptx::fence_proxy_async_smem();  // the staged rows -> the TMA store
+      softmax_warps_sync();
+      if (warp == 2 && lane == 0) {
+        if constexpr (X) ptx::tma_store_4d(&tmOut, smem + DQ_Q_OFF, 0, a, q0, b);
+        else ptx::tma_store_3d(&tmOut, smem + DQ_Q_OFF, a * HD, q0, b);
+        ptx::bulk_commit_group();
+      }
     }
     if (!X && p.colpart && q4 == 0) {  // the four row quarters, added in order, by the quarter-0 warps
       const int c = hf * 32 + lane;
       const float sum = ((red[c] + red[64 + c]) + red[128 + c]) + red[192 + c];
       p.colpart[(static_cast<int64_t>(b) * gridDim.x + qt) * (3 * H) + a * HD + c] = sum;
     }
-    if (warp == 2 && lane == 0) ptx::bulk_wait_group_read0();  // before the CTA's memory goes
+    if (KS == 1 && warp == 2 && lane == 0) ptx::bulk_wait_group_read0();  // before the CTA's memory goes
+  }
+  if constexpr (KS > 1) {
+    __syncwarp();
+    ptx::cluster_sync();  // every split's part is where it is read from
+    const int t = static_cast<int>(threadIdx.x) - 64, first = q0 + ((split * (BQ / KS)) >> pack);
+    if (t >= 0 && t < NSM_B) {
+      if (t < 128) add_parts<KS>(smem, smem + DQ_KV_OFF, t, split, 0.125f, BQ);
+      ptx::fence_proxy_async_smem();
+      softmax_warps_sync();
+      if (t == 0 && first < S) {
+        ptx::tma_store_4d(&tmOut, smem + DQ_KV_OFF, 0, a, first, b);
+        ptx::bulk_commit_group();
+        ptx::bulk_wait_group_read0();
+      }
+    }
+    __syncwarp();
+    ptx::cluster_sync();  // the peers have read this CTA's part
   }
   ptx::tc_fence_before();
   __syncthreads();
@@ -1062,8 +1118,11 @@ constexpr int KV_BAR_OFF = KV_RED_OFF + 2 * 4 * 64 * 4;
 constexpr int KV_SMEM = KV_BAR_OFF + 128 + 1024;
 static_assert(3 * (KV_SMEM + 1024) > 233472 && 2 * (KV_SMEM + 1024) <= 233472,
               "exactly two dK/dV CTAs per SM");
+static_assert(KV_SMEM >= kSplitAttentionSmem, "clusters that hold 256 columns: see residency.h");
 
-template <bool X>
+// KS > 1 (X): the CTAs of a cluster share the queries of a key tile, for keys that few
+// heads and sequences have and many queries read, and add their parts of dK and dV.
+template <bool X, int KS = 1>
 __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtensorMap tmK,
                                                             const __grid_constant__ CUtensorMap tmV,  // X
                                                             const __grid_constant__ CUtensorMap tmQ,
@@ -1076,14 +1135,14 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
   pdl_wait();
   pdl_trigger();
   extern __shared__ uint8_t smem_raw[];
-  const int kt = blockIdx.x, a = blockIdx.y, b = blockIdx.z;  // X: a is the key head
+  const int kt = blockIdx.x / KS, split = blockIdx.x % KS, a = blockIdx.y, b = blockIdx.z;  // X: a is the key head
   const int S = p.S, H = p.H;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int len = valid_keys(p.lens, b, X ? 0 : 1, X ? p.x.Skv : S, p.status);
   const int row0 = b * S, k0 = kt * BK2;
   const int64_t rs = 3 * static_cast<int64_t>(H);
-  if (X && k0 >= len) {  // as below
-    for (int i = threadIdx.x; i < BK2 * 8; i += NTHR_B) {
+  if (X && k0 >= len) {  // as below (every split of the tile alike)
+    for (int i = threadIdx.x + (split > 0 ? BK2 * 8 : 0); i < BK2 * 8; i += NTHR_B) {
       const int rr = i >> 3, c = i & 7;
       if (k0 + rr < p.x.Skv) {
         const int64_t row = static_cast<int64_t>(b) * p.x.Skv + k0 + rr;
@@ -1122,7 +1181,8 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 2);
   const int pack = X ? p.x.pack : 0, qrows = S << pack;    // rows of queries of a block of 2^pack heads
   const int n_q = (qrows + BQ2 - 1) / BQ2;                  // their tiles
-  const int n_qt = X ? n_q * (p.x.group >> pack) : n_q;     // of every block that reads these keys, in turn
+  const int all_qt = X ? n_q * (p.x.group >> pack) : n_q;   // of every block that reads these keys, in turn
+  const int first_qt = split * all_qt / KS, n_qt = (split + 1) * all_qt / KS - first_qt;  // this CTA's
   const uint64_t lim = p.timeout_ns;
 
   if (threadIdx.x == 0) {
@@ -1177,9 +1237,9 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
       }
     }
     // this (sequence, head)'s X_lse rows, followed by its X_delta rows
-    int block = X ? a * (p.x.group >> pack) : a;  // of heads
+    int block = X ? a * (p.x.group >> pack) + first_qt / n_q : a;  // of heads
     const uint4* xs_b = p.xtab + (static_cast<int64_t>(b) * (p.A >> pack) + block) * 2 * qrows;
-    int issued = 0, t = 0;  // t: the tile within the block
+    int issued = 0, t = first_qt % n_q;  // t: the tile within the block
     for (int i = 0; i < n_qt && lane == 0; ++i) {
       const int st = i % KV_STAGES;
       if (!ptx::mbar_wait(&q_empty[st], ((i / KV_STAGES) & 1) ^ 1u, lim, p.status, kWaitHint)) break;
@@ -1281,7 +1341,7 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
       const bool mine = ptx::mbar_wait(bar, parity, lim, p.status, kWaitHint);
       return __all_sync(0xffffffffu, mine);
     };
-    for (int i = 0, t0 = 0; i < n_qt; ++i, t0 = X && t0 + 1 == n_q ? 0 : t0 + 1) {
+    for (int i = 0, t0 = first_qt % n_q; i < n_qt; ++i, t0 = X && t0 + 1 == n_q ? 0 : t0 + 1) {
       if (!wait_all(st_full, i & 1) || !wait_all(dpt_full, i & 1)) { ok = false; break; }
       ptx::tc_fence_after();
       uint32_t sv[32], dv[32];
@@ -1329,6 +1389,10 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
       ptx::tmem_ld_32x32b_x32(tacc + lane_base, o[0]);
       ptx::tmem_ld_32x32b_x32(tacc + lane_base + 32, o[1]);
       ptx::tmem_ld_wait();
+      if constexpr (KS > 1) {  // over K, V and the ring: dK's part, then dV's
+        put_part(smem + hf * PART_BYTES, r, 0, true, o[0]);
+        put_part(smem + hf * PART_BYTES, r, 1, true, o[1]);
+      }
       if (k0 + q4 * 32 + 32 > len) {  // warp-uniform: rows of keys past the valid length are zero
 #pragma unroll
         for (int c = 0; c < 2; ++c)
@@ -1336,7 +1400,7 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
           for (int j = 0; j < 32; ++j) o[c][j] = key < len ? o[c][j] : 0u;
       }
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int c = 0; c < (KS > 1 ? 0 : 2); ++c)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           uint32_t w[4];
@@ -1360,17 +1424,19 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
       red[(hf * 4 + q4) * 64 + lane] = 0.f;
       red[(hf * 4 + q4) * 64 + 32 + lane] = 0.f;
     }
-    ptx::fence_proxy_async_smem();  // the staged rows -> the TMA store
-    softmax_warps_sync();
-    if (warp == 2 && lane == 0) {
-      if constexpr (X) {
-        ptx::tma_store_4d(&tmOut, smem + KV_K_OFF, 0, a, k0, b);
-        ptx::tma_store_4d(&tmOutV, smem + KV_V_OFF, 0, a, k0, b);
-      } else {
-        ptx::tma_store_3d(&tmOut, smem + KV_K_OFF, H + a * HD, k0, b);
-        ptx::tma_store_3d(&tmOut, smem + KV_V_OFF, 2 * H + a * HD, k0, b);
+    if constexpr (KS == 1) {
+      ptx::fence_proxy_async_smem();  // the staged rows -> the TMA store
+      softmax_warps_sync();
+      if (warp == 2 && lane == 0) {
+        if constexpr (X) {
+          ptx::tma_store_4d(&tmOut, smem + KV_K_OFF, 0, a, k0, b);
+          ptx::tma_store_4d(&tmOutV, smem + KV_V_OFF, 0, a, k0, b);
+        } else {
+          ptx::tma_store_3d(&tmOut, smem + KV_K_OFF, H + a * HD, k0, b);
+          ptx::tma_store_3d(&tmOut, smem + KV_V_OFF, 2 * H + a * HD, k0, b);
+        }
+        ptx::bulk_commit_group();
       }
-      ptx::bulk_commit_group();
     }
     if (!X && p.colpart && q4 == 0) {  // the four row quarters, added in order, by the quarter-0 warps
       const float* rh = red + hf * 4 * 64;
@@ -1379,7 +1445,28 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
       for (int c = lane; c < 64; c += 32)
         dst[c] = ((rh[c] + rh[64 + c]) + rh[128 + c]) + rh[192 + c];
     }
-    if (warp == 2 && lane == 0) ptx::bulk_wait_group_read0();  // before the CTA's memory goes
+    if (KS == 1 && warp == 2 && lane == 0) ptx::bulk_wait_group_read0();  // before the CTA's memory goes
+  }
+  if constexpr (KS > 1) {
+    __syncwarp();
+    ptx::cluster_sync();  // every split's parts are where they are read from
+    const int t = static_cast<int>(threadIdx.x) - 64, first = k0 + split * (BK2 / KS);
+    if (t >= 0 && t < NSM_B) {
+      const int g = t >> 7;  // dK, dV
+      uint8_t* stage = smem + 2 * PART_BYTES;
+      constexpr int STAGE_BYTES = BK2 / KS * 128;
+      add_parts<KS>(smem + g * PART_BYTES, stage + g * STAGE_BYTES, t & 127, split, g == 0 ? 0.125f : 1.f, len - k0);
+      ptx::fence_proxy_async_smem();
+      softmax_warps_sync();
+      if (t == 0 && first < p.x.Skv) {
+        ptx::tma_store_4d(&tmOut, stage, 0, a, first, b);
+        ptx::tma_store_4d(&tmOutV, stage + STAGE_BYTES, 0, a, first, b);
+        ptx::bulk_commit_group();
+        ptx::bulk_wait_group_read0();
+      }
+    }
+    __syncwarp();
+    ptx::cluster_sync();  // the peers have read this CTA's parts
   }
   ptx::tc_fence_before();
   __syncthreads();
@@ -1906,57 +1993,47 @@ namespace attn_tc {
 // delta[b, a, s] = sum over a head of dctx * ctx, for the dQ kernel, and the dK/dV
 // kernel's per-query rows [B][A >> pack][2][Sq << pack]: the log-sum-exp over c =
 // log2(e)/sqrt(D), then delta, negated and split as its comment says.  Eight lanes of 16
-// bytes a head, DELTA_HEADS heads in flight.
-constexpr int DELTA_HEADS = 4;
+// bytes a head.  (Two or four heads of loads in flight a lane were slower at every size but
+// the largest.)
 __global__ void __launch_bounds__(256) attn_delta_cross(const __nv_bfloat16* __restrict__ ctx,
                                                         const __nv_bfloat16* __restrict__ dctx, int64_t ldo, int S,
                                                         int A, int pack, int64_t heads, const float* __restrict__ lse,
                                                         float* __restrict__ delta, uint4* __restrict__ xtab) {
   pdl_wait();
   pdl_trigger();
+  const int64_t i = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 3;
+  if (i >= heads) return;  // (whole groups of eight lanes)
   const int l = threadIdx.x & 7;
-  const int64_t i0 = static_cast<int64_t>(blockIdx.x) * (32 * DELTA_HEADS) + (threadIdx.x >> 3);  // head: i0 + 32 n
-  uint4 x[DELTA_HEADS], y[DELTA_HEADS];
-  float lz[DELTA_HEADS];
-  int64_t b[DELTA_HEADS];
-  int a[DELTA_HEADS], s[DELTA_HEADS];
+  const int64_t row = i / A, b = row / S;
+  const int a = static_cast<int>(i - row * A), s = static_cast<int>(row - b * S);
+  const int64_t at = row * ldo + a * HD + l * 8;
+  const uint4 x = *reinterpret_cast<const uint4*>(ctx + at), y = *reinterpret_cast<const uint4*>(dctx + at);
+  const int64_t sidx = (b * A + a) * S + s;
+  const float lz = l == 0 ? lse[sidx] : 0.f;
+  const __nv_bfloat162* xs = reinterpret_cast<const __nv_bfloat162*>(&x);
+  const __nv_bfloat162* ys = reinterpret_cast<const __nv_bfloat162*>(&y);
+  float acc = 0.f;
 #pragma unroll
-  for (int n = 0; n < DELTA_HEADS; ++n) {
-    const int64_t i = i0 + 32 * n < heads ? i0 + 32 * n : 0, row = i / A;
-    b[n] = row / S;
-    a[n] = static_cast<int>(i - row * A);
-    s[n] = static_cast<int>(row - b[n] * S);
-    const int64_t at = row * ldo + a[n] * HD + l * 8;
-    x[n] = *reinterpret_cast<const uint4*>(ctx + at);
-    y[n] = *reinterpret_cast<const uint4*>(dctx + at);
-    lz[n] = l == 0 ? lse[(b[n] * A + a[n]) * S + s[n]] : 0.f;
+  for (int e = 0; e < 4; ++e) {
+    const float2 u = __bfloat1622float2(xs[e]), w = __bfloat1622float2(ys[e]);
+    acc += u.x * w.x + u.y * w.y;
   }
+  const uint32_t mask = 0xffu << (threadIdx.x & 24);
 #pragma unroll
-  for (int n = 0; n < DELTA_HEADS; ++n) {
-    const __nv_bfloat162* xs = reinterpret_cast<const __nv_bfloat162*>(&x[n]);
-    const __nv_bfloat162* ys = reinterpret_cast<const __nv_bfloat162*>(&y[n]);
-    float acc = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 u = __bfloat1622float2(xs[e]), w = __bfloat1622float2(ys[e]);
-      acc += u.x * w.x + u.y * w.y;
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
-    if (l != 0 || i0 + 32 * n >= heads) continue;
-    delta[(b[n] * A + a[n]) * S + s[n]] = acc;
-    auto row16 = [](float v) {  // -v as [hi, lo, 0, ...] in bf16
-      const __nv_bfloat16 hi = __float2bfloat16_rn(-v);
-      const __nv_bfloat16 lo = __float2bfloat16_rn(-v - __bfloat162float(hi));
-      return make_uint4(static_cast<uint32_t>(__bfloat16_as_ushort(hi)) |
-                            (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16),
-                        0u, 0u, 0u);
-    };
-    uint4* t = xtab + (b[n] * (A >> pack) + (a[n] >> pack)) * 2 * (static_cast<int64_t>(S) << pack) +
-               (static_cast<int64_t>(s[n]) << pack) + (a[n] & ((1 << pack) - 1));
-    t[0] = row16(__fdiv_rn(lz[n], LOG2E * 0.125f));
-    t[static_cast<int64_t>(S) << pack] = row16(acc);
-  }
+  for (int o = 1; o < 8; o <<= 1) acc += __shfl_xor_sync(mask, acc, o);
+  if (l != 0) return;
+  delta[sidx] = acc;
+  auto row16 = [](float v) {  // -v as [hi, lo, 0, ...] in bf16
+    const __nv_bfloat16 hi = __float2bfloat16_rn(-v);
+    const __nv_bfloat16 lo = __float2bfloat16_rn(-v - __bfloat162float(hi));
+    return make_uint4(static_cast<uint32_t>(__bfloat16_as_ushort(hi)) |
+                          (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16),
+                      0u, 0u, 0u);
+  };
+  uint4* t = xtab + (b * (A >> pack) + (a >> pack)) * 2 * (static_cast<int64_t>(S) << pack) +
+             (static_cast<int64_t>(s) << pack) + (a & ((1 << pack) - 1));
+  t[0] = row16(__fdiv_rn(lz, LOG2E * 0.125f));
+  t[static_cast<int64_t>(S) << pack] = row16(acc);
 }
 }  // namespace attn_tc
 
@@ -2026,37 +2103,69 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ct
     if (g.group == 1 << pack && static_cast<int64_t>(g.Sq) << pack <= BQ && g.Skv <= BQ)
       return cross_attention_bwd_short_tc(g, B, pack, ctx, dctx, lse, dq, dk, dv, stream);
   const int packQ = best_pack(g, BQ), packK = best_pack(g, BQ2), hq = 1 << packQ, hk = 1 << packK;
-  const int Akv = g.A / g.group;
+  const int Akv = g.A / g.group, sms = sm_count() > 0 ? sm_count() : 148;
+  const int q_tiles = ceil_div(static_cast<int64_t>(g.Sq) << packQ, BQ), k_tiles = ceil_div(g.Skv, BK2);
+  const int64_t q_ctas = static_cast<int64_t>(q_tiles) * (g.A >> packQ) * B, k_ctas = static_cast<int64_t>(k_tiles) * Akv * B;
+  // what a CTA walks through: key tiles, and query tiles of all heads that read its keys
+  const int q_steps = ceil_div(g.Skv, BKV),
+            k_steps = ceil_div(static_cast<int64_t>(g.Sq) << packK, BQ2) * (g.group >> packK);
+  // Split where few CTAs would walk far, down to two steps each: dK/dV up to two CTAs an
+  // SM, dQ up to 5/4 (it runs beside dK/dV).  us, unsplit and split: 2 x 775 queries, 16
+  // heads on 4, 161 keys 62 and 20; 11 x 953, 9 on 3, 16 keys 71 and 36; 40 queries, 12 on
+  // 4, 945 keys 13.9 and 9.4; 20 x 10, 8 on 4, 1454 keys 37.4 and 33.5.  dQ up to two: 6 x
+  // 197, 12 on 4, 777 keys 24.3 and 29.5; dK/dV up to four: 4 x 256, 4 heads, 1770 keys 18.3
+  // and 27.2.
+  const auto splits = [&](int64_t ctas, int steps, int most, int pack) {  // (a split stores whole queries)
+    int ks = 1;
+    while (ks < 8 && 2 * ks * ctas <= most && steps >= 4 * ks && BQ / (2 * ks) >> pack > 0) ks *= 2;
+    return ks;
+  };
+  const int ksq = splits(q_ctas, q_steps, 5 * sms / 4, packQ), ksk = splits(k_ctas, k_steps, 2 * sms, 0);
   CUtensorMap tq128, to128, tk64, tv64, tdq, tk128, tv128, tq64, to64, tdk, tdv;
   SKY_CHECK(cross_map(&tq128, g.q, g.A, g.Sq, B, g.ldq, hq, BQ >> packQ) &&
                 cross_map(&to128, dctx, g.A, g.Sq, B, g.ldo, hq, BQ >> packQ) &&
-                cross_map(&tdq, dq, g.A, g.Sq, B, g.ldq, hq, BQ >> packQ) &&
+                cross_map(&tdq, dq, g.A, g.Sq, B, g.ldq, hq, BQ / ksq >> packQ) &&
                 cross_map(&tk64, g.k, Akv, g.Skv, B, g.ldk, 1, BKV) && cross_map(&tv64, g.v, Akv, g.Skv, B, g.ldv, 1, BKV) &&
                 cross_map(&tk128, g.k, Akv, g.Skv, B, g.ldk, 1, BK2) && cross_map(&tv128, g.v, Akv, g.Skv, B, g.ldv, 1, BK2) &&
                 cross_map(&tq64, g.q, g.A, g.Sq, B, g.ldq, hk, BQ2 >> packK) &&
                 cross_map(&to64, dctx, g.A, g.Sq, B, g.ldo, hk, BQ2 >> packK) &&
-                cross_map(&tdk, dk, Akv, g.Skv, B, g.ldk, 1, BK2) && cross_map(&tdv, dv, Akv, g.Skv, B, g.ldv, 1, BK2),
+                cross_map(&tdk, dk, Akv, g.Skv, B, g.ldk, 1, BK2 / ksk) && cross_map(&tdv, dv, Akv, g.Skv, B, g.ldv, 1, BK2 / ksk),
             SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the cross attention backward operands");
-  static OncePerDevice once1, once2;
-  const cudaError_t a1 = allow_smem(once1, attn_bwd_dq_tc<true>, DQ_SMEM),
-                    a2 = allow_smem(once2, attn_bwd_dkdv_tc<true>, KV_SMEM);
-  if (a1 != cudaSuccess) return cuda_fail(a1, "cross attention dQ smem attribute");
-  if (a2 != cudaSuccess) return cuda_fail(a2, "cross attention dK/dV smem attribute");
   float* delta = static_cast<float*>(ws);
   uint4* xtab = reinterpret_cast<uint4*>(static_cast<char*>(ws) + cross_delta_bytes(g, B));
   const int64_t heads = static_cast<int64_t>(B) * g.Sq * g.A;
-  cudaError_t e = launch_pdl(attn_delta_cross, dim3(ceil_div(heads, 32 * DELTA_HEADS)), dim3(256), 0, stream, 1,
+  cudaError_t e = launch_pdl(attn_delta_cross, dim3(ceil_div(heads, 32)), dim3(256), 0, stream, 1,
                              static_cast<const __nv_bfloat16*>(ctx), static_cast<const __nv_bfloat16*>(dctx), g.ldo,
                              g.Sq, g.A, packK, heads, lse, delta, xtab);
   BwdParams p{g.Sq, 0, g.A, g.lens, lse, delta, xtab, nullptr, nullptr, g.status, kTimeoutNs, {g.Skv, g.group, packK},
               static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv), g.ldk, g.ldv};
+  const auto with = [](int ks, auto&& go) {
+    return ks == 1   ? go(std::integral_constant<int, 1>{})
+           : ks == 2 ? go(std::integral_constant<int, 2>{})
+           : ks == 4 ? go(std::integral_constant<int, 4>{})
+                     : go(std::integral_constant<int, 8>{});
+  };
   if (e == cudaSuccess)
-    e = launch_pdl(attn_bwd_dkdv_tc<true>, dim3(ceil_div(g.Skv, BK2), Akv, B), dim3(NTHR_B), KV_SMEM, stream, 1, tk128,
-                   tv128, tq64, to64, tdk, tdv, p);
+    e = with(ksk, [&](auto ks) {
+      constexpr int KS = decltype(ks)::value;
+      auto kern = attn_bwd_dkdv_tc<true, KS>;
+      static OncePerDevice once;
+      const cudaError_t attr = allow_smem(once, kern, KV_SMEM);
+      return attr != cudaSuccess ? attr
+                                 : launch_pdl(kern, dim3(k_tiles * KS, Akv, B), dim3(NTHR_B), KV_SMEM, stream, KS, tk128,
+                                              tv128, tq64, to64, tdk, tdv, p);
+    });
   p.x.pack = packQ;
   if (e == cudaSuccess)
-    e = launch_pdl(attn_bwd_dq_tc<true>, dim3(ceil_div(static_cast<int64_t>(g.Sq) << packQ, BQ), g.A >> packQ, B),
-                   dim3(NTHR_B), DQ_SMEM, stream, 1, tq128, tk64, tv64, to128, tdq, p);
+    e = with(ksq, [&](auto ks) {
+      constexpr int KS = decltype(ks)::value;
+      auto kern = attn_bwd_dq_tc<true, KS>;
+      static OncePerDevice once;
+      const cudaError_t attr = allow_smem(once, kern, DQ_SMEM);
+      return attr != cudaSuccess ? attr
+                                 : launch_pdl(kern, dim3(q_tiles * KS, g.A >> packQ, B), dim3(NTHR_B), DQ_SMEM, stream,
+                                              KS, tq128, tk64, tv64, to128, tdq, p);
+    });
   count_launches(3);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core cross attention backward launch");
 }

@@ -243,6 +243,19 @@ def test_large_scores(dtype):
     c.check_backward(c.backward(*c.given()))
 
 
+@pytest.mark.parametrize("sq,skv,heads,kv_heads,lens", [
+    (700, 100, 8, 2, [100, 64]), (900, 16, 9, 3, [16, 3]), (500, 130, 2, 2, [130, 1]), (260, 65, 4, 4, [65, 0]),   # few keys
+    (40, 945, 6, 3, [945, 700]), (1, 1500, 2, 1, [1500, 0]), (17, 700, 32, 1, [700, 450]), (70, 520, 3, 3, [520, 64]),
+    (2000, 2000, 1, 1, [1999]),
+])
+def test_sums_split_over_a_cluster(sq, skv, heads, kv_heads, lens):
+    """Gradients of few keys that many queries read, and of few queries that read many keys."""
+    c = Case(sq, skv, heads, kv_heads, lens).poison()
+    grads = c.backward(*c.given())
+    c.check_backward(grads)
+    assert all(torch.equal(x.buf, y.buf) for x, y in zip(grads, c.backward(*c.given())))
+
+
 def test_forward_feeds_backward():
     """The library's own ctx and lse: within what the forward may be off more."""
     c = Case(150, 220, 6, 3, [220, 100, 0, 7]).poison()
