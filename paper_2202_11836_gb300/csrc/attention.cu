@@ -111,13 +111,6 @@ sky_status attention_bwd_tc(const void* qkv, const void* dctx, const float* lse,
                             int32_t* status, uint64_t timeout_ns, cudaStream_t stream,
                             float* colpart);
 
-// Packed QKV rows as the SIMT kernels take them.
-static attn::Geometry packed_f32(const void* qkv, const int32_t* lens, int S, int H, int A, int32_t* status) {
-  const float* q = static_cast<const float*>(qkv);
-  const int64_t rs = 3 * static_cast<int64_t>(H);
-  return {q, q + H, q + 2 * H, rs, rs, rs, H, S, S, A, 1, H / A, 0, false, lens, 1, status};
-}
-
 sky_status attention_fwd(const void* qkv, const int32_t* lens, int B, int S, int H, int A,
                          sky_dtype dt, void* ctx, float* lse, int32_t* status,
                          cudaStream_t stream) {
@@ -128,8 +121,8 @@ sky_status attention_fwd(const void* qkv, const int32_t* lens, int B, int S, int
   }
   SKY_CHECK(D <= 128, SKY_ERR_UNSUPPORTED, "fp32 attention needs head dim <= 128");
   SKY_CHECK(S <= 3072, SKY_ERR_UNSUPPORTED, "fp32 attention: sequence too long");
-  const cudaError_t e = attn::launch_fwd_simt(packed_f32(qkv, lens, S, H, A, status), B, static_cast<float*>(ctx), lse,
-                                              stream);
+  const cudaError_t e = attn::launch_fwd_self(static_cast<const float*>(qkv), lens, B, S, H, A, static_cast<float*>(ctx),
+                                              lse, status, stream);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "attention forward launch");
 }
 
@@ -172,9 +165,9 @@ sky_status attention_bwd(const void* qkv, const void* ctx, const void* dctx, con
                             stream, colpart);
   }
   SKY_CHECK(D <= 128, SKY_ERR_UNSUPPORTED, "fp32 attention needs head dim <= 128");
-  float* dx = static_cast<float*>(dqkv);
-  const cudaError_t e = attn::launch_bwd_simt(packed_f32(qkv, lens, S, H, A, nullptr), B, static_cast<const float*>(ctx),
-                                              static_cast<const float*>(dctx), lse, delta, dx, dx + H, dx + 2 * H, stream);
+  const cudaError_t e =
+      attn::launch_bwd_self(static_cast<const float*>(qkv), static_cast<const float*>(ctx), static_cast<const float*>(dctx),
+                            lse, lens, B, S, H, A, delta, static_cast<float*>(dqkv), stream);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "attention backward launch");
 }
 

@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(NW * 32) attn_few_mma(const __grid_constant__ 
   const int room = (geo.Skv + CHUNK - 1) / CHUNK;
   int fetched = min(STAGES, room > first ? (room - first + step - 1) / step : 0);
   for (int n = 0; n < fetched; ++n) fetch(n);
-  const int len = attn::valid_keys(geo, b);
+  const int len = attn::valid_keys(geo.lens, b, 0, geo.Skv, geo.status);
   const int chunks = (len + CHUNK - 1) / CHUNK;
   const int mine = chunks > first ? (chunks - first + step - 1) / step : 0;
   uint32_t qa[4][4];
@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(NW * 32) attn_few_simt(const Params p) {
   const int kv = blockIdx.y / blocks, r0 = blockIdx.y % blocks * RB, b = blockIdx.z;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / LK, d = lane % LK * 4;
   pdl_wait();
-  const int len = attn::valid_keys(geo, b);
+  const int len = attn::valid_keys(geo.lens, b, 0, geo.Skv, geo.status);
   float4 q[RB], o[RB];
   float m[RB], l[RB];
 #pragma unroll

@@ -178,8 +178,23 @@ __device__ __forceinline__ float half_warp_sum(float v) {
   return v;
 }
 
-template <typename T, int G>
-__global__ void __launch_bounds__(F_THR) attn_fwd_simt(const Geometry g, T* __restrict__ ctx, float* __restrict__ lse) {
+// SELF: Q, K and V are blocks of the same rows, as many queries as keys, a key head each.
+// Known to the compiler, it is worth 7% of a small forward (3.9 -> 3.5 us at 4 x 32 tokens, 2
+// heads of 64).
+template <bool SELF>
+struct Strides {
+  int H, Skv, group;
+  int64_t q, k, v, o;
+  __device__ explicit Strides(const Geometry& g)
+      : H(static_cast<int>(g.ldo)), Skv(SELF ? g.Sq : g.Skv), group(SELF ? 1 : g.group), q(SELF ? 3 * static_cast<int64_t>(H) : g.ldq),
+        k(SELF ? q : g.ldk), v(SELF ? q : g.ldv), o(SELF ? H : g.ldo) {}
+};
+
+template <bool SELF, typename T, int G>
+__global__ void __launch_bounds__(F_THR, 3) attn_fwd_simt(const Geometry g, const T* __restrict__ gq,
+                                                          const T* __restrict__ gk, const T* __restrict__ gv,
+                                                          const int32_t* __restrict__ lens, T* __restrict__ ctx,
+                                                          float* __restrict__ lse) {
   using ST = Stage<G>;
   constexpr int CC = ST::CC;
   pdl_wait();
@@ -190,13 +205,14 @@ __global__ void __launch_bounds__(F_THR) attn_fwd_simt(const Geometry g, T* __re
   const int tiles = (Sq + FR - 1) / FR;
   const int a = static_cast<int>(blockIdx.x) / tiles, q0 = (static_cast<int>(blockIdx.x) % tiles) * FR, b = blockIdx.y;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int len = valid_keys(g, b), kv = a / g.group;
-  const T* q = static_cast<const T*>(g.q) + static_cast<int64_t>(b) * Sq * g.ldq + a * D;
-  const T* k = static_cast<const T*>(g.k) + static_cast<int64_t>(b) * g.Skv * g.ldk + kv * D;
-  const T* v = static_cast<const T*>(g.v) + static_cast<int64_t>(b) * g.Skv * g.ldv + kv * D;
+  const Strides<SELF> ld(g);
+  const int len = valid_keys(lens, b, SELF ? 1 : 0, ld.Skv, g.status), kv = a / ld.group;
+  const T* q = gq + static_cast<int64_t>(b) * Sq * ld.q + a * D;
+  const T* k = SELF ? q + ld.H : gk + static_cast<int64_t>(b) * ld.Skv * ld.k + kv * D;
+  const T* v = SELF ? q + 2 * ld.H : gv + static_cast<int64_t>(b) * ld.Skv * ld.v + kv * D;
   const float sc = 1.f / sqrtf((float)D);
   float4 own[ST::OWN];
-  load_rows<G>(q, g.ldq, q0, Sq, D, vec, own);
+  load_rows<G>(q, ld.q, q0, Sq, D, vec, own);
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
   float4 o[2][CC] = {};
   for (int k0 = 0; k0 < len; k0 += FC) {
@@ -205,8 +221,8 @@ __global__ void __launch_bounds__(F_THR) attn_fwd_simt(const Geometry g, T* __re
     for (int h = 0; h < ST::BATCHES; ++h) {
       constexpr int R = ST::R;
       float4 kx[ST::PASSES], vx[ST::PASSES];
-      load_rows<G>(k, g.ldk, k0 + R * h, len, D, vec, kx);
-      load_rows<G>(v, g.ldv, k0 + R * h, len, D, vec, vx);
+      load_rows<G>(k, ld.k, k0 + R * h, len, D, vec, kx);
+      load_rows<G>(v, ld.v, k0 + R * h, len, D, vec, vx);
       if (h == 0 && k0 == 0) put_rows<G>(sq, LD, D, own);
       put_rows<G>(sk + R * h * LD, LD, D, kx);
       put_rows<G>(sv + R * h * LD, LD, D, vx);
@@ -244,9 +260,10 @@ __global__ void __launch_bounds__(F_THR) attn_fwd_simt(const Geometry g, T* __re
     __syncwarp();
   }
   pdl_trigger();
-  store_rows<CC>(ctx + static_cast<int64_t>(b) * Sq * g.ldo + a * D, g.ldo, q0, Sq, D, vec, len > 0 ? 1.f / l[0] : 0.f,
-                 len > 0 ? 1.f / l[1] : 0.f, o);
-  if (tx == 0 && lse)
+  const bool any = SELF || len > 0;
+  store_rows<CC>(ctx + static_cast<int64_t>(b) * Sq * ld.o + a * D, ld.o, q0, Sq, D, vec, any ? 1.f / l[0] : 0.f,
+                 any ? 1.f / l[1] : 0.f, o);
+  if (tx == 0 && (SELF || lse))
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       if (q0 + 2 * ty + i < Sq)  // (without a key: -inf)
@@ -261,40 +278,44 @@ __global__ void __launch_bounds__(F_THR) attn_fwd_simt(const Geometry g, T* __re
 // operand of the columns / sqrt(D), dV = P . dO.  Four CTAs an SM (128 registers) are
 // faster up to a head dim of 64 (29.8 us against 34.7 at 4 x 101, 12 heads), above it
 // the registers are (50.6 against 57.0 at 2 x 200, 6 heads of 128).
-template <typename T, int G, int NC>
-__global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geometry g, const T* __restrict__ dctx,
+template <bool SELF, typename T, int G, int NC>
+__global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geometry g, const T* __restrict__ gq,
+                                                      const T* __restrict__ gk, const T* __restrict__ gv,
+                                                      const int32_t* __restrict__ lens, const T* __restrict__ dctx,
                                                       const float* __restrict__ lse, const float* __restrict__ delta,
                                                       T* __restrict__ dq, T* __restrict__ dk, T* __restrict__ dv) {
   using ST = Stage<G, NC>;
   constexpr int CC = ST::CC, TC = ST::ROWS, P_LD = TC + 4;
   pdl_wait();
   extern __shared__ __align__(16) float sm[];
-  const int LD = g.LD, D = g.D, Sq = g.Sq, Skv = g.Skv;
+  const Strides<SELF> ld(g);
+  const int LD = g.LD, D = g.D, Sq = g.Sq, Skv = ld.Skv;
   const bool vec = g.vec;
   float *r0s = sm, *r1s = r0s + FR * LD, *c0s = r1s + FR * LD, *c1s = c0s + TC * LD;
   float *sds = c1s + TC * LD, *sp = sds + FR * P_LD, *sl = sp + FR * P_LD, *sd = sl + TC;
-  const int qtiles = (Sq + FR - 1) / FR, ktiles = (Skv + FR - 1) / FR;
-  const int both = min(qtiles * g.A, ktiles * (g.A / g.group)), x = blockIdx.x;
-  const bool keys = x < 2 * both ? x & 1 : qtiles * g.A < ktiles * (g.A / g.group);  // own rows are keys
-  const int u = x < 2 * both ? x >> 1 : x - both, tiles = keys ? ktiles : qtiles;
+  const int qtiles = (Sq + FR - 1) / FR, ktiles = (Skv + FR - 1) / FR, x = blockIdx.x;
+  const int qunits = qtiles * g.A, kunits = ktiles * (g.A / ld.group), both = SELF ? qunits : min(qunits, kunits);
+  const bool keys = SELF || x < 2 * both ? x & 1 : qunits < kunits;  // own rows are keys
+  const int u = SELF || x < 2 * both ? x >> 1 : x - both, tiles = keys ? ktiles : qtiles;
   const int head = u / tiles, r0 = (u % tiles) * FR, b = blockIdx.y;  // of its kind
-  const int kv = keys ? head : head / g.group, heads = keys ? g.group : 1;
+  const int kv = keys ? head : head / ld.group, heads = keys ? ld.group : 1;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int len = valid_keys(g, b);
-  const T* k = static_cast<const T*>(g.k) + static_cast<int64_t>(b) * Skv * g.ldk + kv * D;
-  const T* v = static_cast<const T*>(g.v) + static_cast<int64_t>(b) * Skv * g.ldv + kv * D;
+  const int len = valid_keys(lens, b, SELF ? 1 : 0, Skv, g.status);
+  const T* self = gq + static_cast<int64_t>(b) * Sq * ld.q + head * D;
+  const T* k = SELF ? self + ld.H : gk + static_cast<int64_t>(b) * Skv * ld.k + kv * D;
+  const T* v = SELF ? self + 2 * ld.H : gv + static_cast<int64_t>(b) * Skv * ld.v + kv * D;
   const float sc = 1.f / sqrtf((float)D), sl2 = sc * 1.4426950408889634f;
   float4 o0[2][CC] = {}, o1[2][CC] = {};
   const int rows = keys ? Skv : Sq, cols = keys ? Sq : len;
   float4 own0[ST::OWN], own1[ST::OWN];
   for (int h = 0; h < heads && (!keys || r0 < len); ++h) {
-    const int a = keys ? kv * g.group + h : head;
-    const T* q = static_cast<const T*>(g.q) + static_cast<int64_t>(b) * Sq * g.ldq + a * D;
-    const T* dO = dctx + static_cast<int64_t>(b) * Sq * g.ldo + a * D;
+    const int a = !SELF && keys ? kv * ld.group + h : head;
+    const T* q = SELF ? self : gq + static_cast<int64_t>(b) * Sq * ld.q + a * D;
+    const T* dO = dctx + static_cast<int64_t>(b) * Sq * ld.o + a * D;
     const float *lse_b = lse + (static_cast<int64_t>(b) * g.A + a) * Sq, *del_b = delta + (static_cast<int64_t>(b) * g.A + a) * Sq;
     if (h == 0) {
-      load_rows<G>(keys ? k : q, keys ? g.ldk : g.ldq, r0, rows, D, vec, own0);
-      load_rows<G>(keys ? v : dO, keys ? g.ldv : g.ldo, r0, rows, D, vec, own1);
+      load_rows<G>(keys ? k : q, keys ? ld.k : ld.q, r0, rows, D, vec, own0);
+      load_rows<G>(keys ? v : dO, keys ? ld.v : ld.o, r0, rows, D, vec, own1);
     }
     float lr[2] = {}, dr[2] = {};
     if (!keys)
@@ -318,8 +339,8 @@ __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geo
       for (int t = 0; t < ST::BATCHES; ++t) {
         constexpr int R = ST::R;
         float4 v0[ST::PASSES], v1[ST::PASSES];
-        load_rows<G>(x0, keys ? g.ldq : g.ldk, c0 + R * t, cols, D, vec, v0);
-        load_rows<G>(x1, keys ? g.ldo : g.ldv, c0 + R * t, cols, D, vec, v1);
+        load_rows<G>(x0, keys ? ld.q : ld.k, c0 + R * t, cols, D, vec, v0);
+        load_rows<G>(x1, keys ? ld.o : ld.v, c0 + R * t, cols, D, vec, v1);
         if (t == 0 && c0 == 0 && h == 0) {
           put_rows<G>(r0s, LD, D, own0);
           put_rows<G>(r1s, LD, D, own1);
@@ -353,9 +374,11 @@ __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geo
     }
   }
   pdl_trigger();
-  T* out = keys ? dk + static_cast<int64_t>(b) * Skv * g.ldk + kv * D : dq + static_cast<int64_t>(b) * Sq * g.ldq + head * D;
-  store_rows<CC>(out, keys ? g.ldk : g.ldq, r0, rows, D, vec, sc, sc, o0);
-  if (keys) store_rows<CC>(dv + static_cast<int64_t>(b) * Skv * g.ldv + kv * D, g.ldv, r0, rows, D, vec, 1.f, 1.f, o1);
+  T* out = dq + static_cast<int64_t>(b) * Sq * ld.q + head * D;
+  T* out_k = SELF ? out + ld.H : dk + static_cast<int64_t>(b) * Skv * ld.k + kv * D;
+  T* out_v = SELF ? out + 2 * ld.H : dv + static_cast<int64_t>(b) * Skv * ld.v + kv * D;
+  store_rows<CC>(keys ? out_k : out, keys ? ld.k : ld.q, r0, rows, D, vec, sc, sc, o0);
+  if (keys) store_rows<CC>(out_v, ld.v, r0, rows, D, vec, 1.f, 1.f, o1);
 }
 
 // Launch shape: the shared row stride (four floats past the head dim, so the 16 lanes of
@@ -376,26 +399,26 @@ bool rows_of_4(const Geometry& g, const void* ctx, const void* x = nullptr, cons
          on(y) && on(z);
 }
 
-template <typename T>
-cudaError_t launch_fwd_simt(Geometry g, int B, T* ctx, float* lse, cudaStream_t stream) {
+template <bool SELF, typename T>
+cudaError_t fwd_simt(Geometry g, int B, T* ctx, float* lse, cudaStream_t stream) {
   g.LD = row_stride(g.D);
   g.vec = rows_of_4<T>(g, ctx);
   const auto go = [&](auto group, auto kern) {  // `group` threads a row: head dims up to four times that
     static OncePerDevice once;
     const cudaError_t e = allow_smem(once, kern, fwd_smem(4 * decltype(group)::value));
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, dim3((unsigned)ceil_div(g.Sq, FR) * g.A, B), dim3(F_THR), fwd_smem(g.D), stream, 1, g, ctx,
-                      lse);
+    return launch_pdl(kern, dim3((unsigned)ceil_div(g.Sq, FR) * g.A, B), dim3(F_THR), fwd_smem(g.D), stream, 1, g,
+                      static_cast<const T*>(g.q), static_cast<const T*>(g.k), static_cast<const T*>(g.v), g.lens, ctx, lse);
   };
   count_launches(1);
-  return g.D <= 32   ? go(Group<8>{}, attn_fwd_simt<T, 8>)
-         : g.D <= 64 ? go(Group<16>{}, attn_fwd_simt<T, 16>)
-                     : go(Group<32>{}, attn_fwd_simt<T, 32>);
+  return g.D <= 32   ? go(Group<8>{}, attn_fwd_simt<SELF, T, 8>)
+         : g.D <= 64 ? go(Group<16>{}, attn_fwd_simt<SELF, T, 16>)
+                     : go(Group<32>{}, attn_fwd_simt<SELF, T, 32>);
 }
 
-template <typename T>
-cudaError_t launch_bwd_simt(Geometry g, int B, const T* ctx, const T* dctx, const float* lse, float* delta, T* dq, T* dk,
-                            T* dv, cudaStream_t stream) {
+template <bool SELF, typename T>
+cudaError_t bwd_simt(Geometry g, int B, const T* ctx, const T* dctx, const float* lse, float* delta, T* dq, T* dk,
+                     T* dv, cudaStream_t stream) {
   const int64_t rows = static_cast<int64_t>(B) * g.Sq;
   const cudaError_t le = launch_pdl(attn_delta<T>, dim3(ceil_div(rows * g.A * 32, 256)), dim3(256), 0, stream, 1, ctx,
                                     dctx, g.Sq, g.ldo, g.A, g.D, rows, delta);
@@ -409,7 +432,8 @@ cudaError_t launch_bwd_simt(Geometry g, int B, const T* ctx, const T* dctx, cons
     static OncePerDevice once;
     const cudaError_t e = allow_smem(once, kern, bwd_smem(4 * G, NC));
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, dim3(blocks, B), dim3(F_THR), bwd_smem(g.D, NC), stream, 1, g, dctx, lse,
+    return launch_pdl(kern, dim3(blocks, B), dim3(F_THR), bwd_smem(g.D, NC), stream, 1, g,
+                      static_cast<const T*>(g.q), static_cast<const T*>(g.k), static_cast<const T*>(g.v), g.lens, dctx, lse,
                       static_cast<const float*>(delta), dq, dk, dv);
   };
   // Up to 16 tokens a 64-column tile is mostly empty: 128 x 8 tokens, 6 heads of 128
@@ -417,18 +441,41 @@ cudaError_t launch_bwd_simt(Geometry g, int B, const T* ctx, const T* dctx, cons
   // (41.1); 64 x 16, 12 of 64 29.8 and 18.3 (70.4).
   const auto width = [&](auto group) {
     constexpr int G = decltype(group)::value;
-    return std::max(g.Sq, g.Skv) <= 16 ? go(group, std::integral_constant<int, 1>{}, attn_bwd_simt<T, G, 1>)
-                                       : go(group, std::integral_constant<int, 4>{}, attn_bwd_simt<T, G, 4>);
+    return std::max(g.Sq, g.Skv) <= 16 ? go(group, std::integral_constant<int, 1>{}, attn_bwd_simt<SELF, T, G, 1>)
+                                       : go(group, std::integral_constant<int, 4>{}, attn_bwd_simt<SELF, T, G, 4>);
   };
   return g.D <= 32 ? width(Group<8>{}) : g.D <= 64 ? width(Group<16>{}) : width(Group<32>{});
 }
 
-template cudaError_t launch_fwd_simt(Geometry, int, float*, float*, cudaStream_t);
-template cudaError_t launch_fwd_simt(Geometry, int, __nv_bfloat16*, float*, cudaStream_t);
-template cudaError_t launch_bwd_simt(Geometry, int, const float*, const float*, const float*, float*, float*, float*,
+template <typename T>
+cudaError_t launch_fwd_simt(const Geometry& g, int B, T* ctx, float* lse, cudaStream_t stream) {
+  return fwd_simt<false>(g, B, ctx, lse, stream);
+}
+template <typename T>
+cudaError_t launch_bwd_simt(const Geometry& g, int B, const T* ctx, const T* dctx, const float* lse, float* delta, T* dq,
+                            T* dk, T* dv, cudaStream_t stream) {
+  return bwd_simt<false>(g, B, ctx, dctx, lse, delta, dq, dk, dv, stream);
+}
+template cudaError_t launch_fwd_simt(const Geometry&, int, float*, float*, cudaStream_t);
+template cudaError_t launch_fwd_simt(const Geometry&, int, __nv_bfloat16*, float*, cudaStream_t);
+template cudaError_t launch_bwd_simt(const Geometry&, int, const float*, const float*, const float*, float*, float*, float*,
                                      float*, cudaStream_t);
-template cudaError_t launch_bwd_simt(Geometry, int, const __nv_bfloat16*, const __nv_bfloat16*, const float*, float*,
+template cudaError_t launch_bwd_simt(const Geometry&, int, const __nv_bfloat16*, const __nv_bfloat16*, const float*, float*,
                                      __nv_bfloat16*, __nv_bfloat16*, __nv_bfloat16*, cudaStream_t);
+
+// Packed QKV rows of H-wide blocks.
+static Geometry packed(const float* q, const int32_t* lens, int S, int H, int A, int32_t* status) {
+  const int64_t rs = 3 * static_cast<int64_t>(H);
+  return {q, q + H, q + 2 * H, rs, rs, rs, H, S, S, A, 1, H / A, 0, false, lens, status};
+}
+cudaError_t launch_fwd_self(const float* qkv, const int32_t* lens, int B, int S, int H, int A, float* ctx, float* lse,
+                            int32_t* status, cudaStream_t stream) {
+  return fwd_simt<true>(packed(qkv, lens, S, H, A, status), B, ctx, lse, stream);
+}
+cudaError_t launch_bwd_self(const float* qkv, const float* ctx, const float* dctx, const float* lse, const int32_t* lens,
+                            int B, int S, int H, int A, float* delta, float* dqkv, cudaStream_t stream) {
+  return bwd_simt<true>(packed(qkv, lens, S, H, A, nullptr), B, ctx, dctx, lse, delta, dqkv, dqkv + H, dqkv + 2 * H, stream);
+}
 
 }  // namespace attn
 }  // namespace sky

@@ -52,6 +52,8 @@
 namespace sky {
 namespace attn_tc {
 
+using attn::valid_keys;
+
 constexpr int BQ = 128, BKV = 64, HD = 64;
 constexpr int Q_BYTES = BQ * HD * 2;    // 16 KiB
 constexpr int KV_BYTES = BKV * HD * 2;  // 8 KiB per K or V tile
@@ -112,16 +114,6 @@ struct FwdParams {
   uint64_t timeout_ns;
   CrossGeometry x;
 };
-
-// The valid keys of sequence b, in [least, S]; a bad length is clamped and reported.
-__device__ __forceinline__ int valid_keys(const int32_t* lens, int b, int least, int S, int32_t* status) {
-  int len = lens[b];
-  if (len < least || len > S) {
-    if (status && threadIdx.x == 0) atomicOr(status, kStatusBadLength);
-    len = len < least ? least : S;
-  }
-  return len;
-}
 
 // Clears rows [from, 64) of a 64-row tile of 128-byte rows (any swizzle: it stays within
 // a row); thread t of n.  The caller fences before the next product reads the tile.

@@ -45,7 +45,7 @@ bool on_grid(const sky_cross_shape& s, const void* p) {
 attn::Geometry geometry(const sky_cross_shape& s, const void* q, const void* k, const void* v, const int32_t* len,
                         int32_t* status) {
   return {q,        k,       v,       s.ldq, s.ldk, s.ldv, s.ldo, s.q_len, s.kv_len, s.heads, s.heads / s.kv_heads,
-          s.head_dim, 0, false, len, 0, status};
+          s.head_dim, 0, false, len, status};
 }
 
 // The most that any choice of kernels takes: pointers, which it depends on, are not known.
