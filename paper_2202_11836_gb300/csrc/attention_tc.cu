@@ -2040,7 +2040,11 @@ bool cross_attention_tc_fits(const attn::Geometry& g, std::initializer_list<cons
 sky_status cross_attention_fwd_tc(const attn::Geometry& g, int B, void* ctx, float* lse, cudaStream_t stream) {
   using namespace attn_tc;
   const int pack = best_pack(g, BQ), hp = 1 << pack, tiles = ceil_div(static_cast<int64_t>(g.Sq) << pack, BQ);
-  const FwdForm form = fwd_form(static_cast<int64_t>(tiles) * (g.A >> pack) * B, ceil_div(g.Skv, BKV));
+  const int64_t ctas = static_cast<int64_t>(tiles) * (g.A >> pack) * B;
+  FwdForm form = fwd_form(ctas, ceil_div(g.Skv, BKV));
+  // (keys of one tile leave nothing for the second buffer, which halves the CTAs an SM: 8 x
+  // 372 queries, 15 heads on 5, 46 keys 4.9 us against 6.7)
+  if (g.Skv <= BKV && ctas > 2 * (sm_count() > 0 ? sm_count() : 148)) form.two = false;
   const int Akv = g.A / g.group;
   CUtensorMap tq, tk, tv, tout;
   SKY_CHECK(cross_map(&tq, g.q, g.A, g.Sq, B, g.ldq, hp, BQ >> pack) &&

@@ -1,0 +1,12 @@
+// The head norms of qk_norm.cuh for fp32, a translation unit of their own to build beside
+// the others.
+#include "qk_norm.cuh"
+
+namespace sky {
+namespace qkn {
+
+template sky_status forward<float>(const sky_qk_norm_shape&, Params&, cudaStream_t);
+template sky_status backward<float>(const sky_qk_norm_shape&, Params&, float*, float*, cudaStream_t);
+
+}  // namespace qkn
+}  // namespace sky

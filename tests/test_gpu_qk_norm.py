@@ -113,7 +113,7 @@ class Case:
 
 SHAPES = [
     # rows, query heads, key heads, dim, values behind the heads
-    (1, 1, 1, 64, 0), (1, 12, 12, 64, 768), (16, 12, 4, 64, 256), (3, 1, 0, 16, 8), (5, 0, 3, 32, 0),
+    (2, 12, 12, 64, 0), (128, 4, 4, 64, 0), (129, 8, 8, 64, 8), (40, 3, 3, 96, 0), (1, 1, 1, 64, 0), (1, 12, 12, 64, 768), (16, 12, 4, 64, 256), (3, 1, 0, 16, 8), (5, 0, 3, 32, 0),
     (7, 17, 9, 48, 16), (33, 9, 3, 80, 0), (101, 12, 4, 96, 384), (64, 6, 6, 128, 0), (19, 5, 2, 176, 0),
     (9, 3, 2, 256, 32), (700, 16, 16, 64, 1024), (5001, 2, 1, 64, 0), (3000, 33, 1, 32, 0), (1, 300, 300, 256, 0),
 ]
