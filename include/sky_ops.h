@@ -125,8 +125,9 @@ typedef struct {
  * bf16 with head_dim 64 and every tensor and row distance on the 16-byte grid
  * runs on the tensor cores; other head dims, up to 128, and other alignments run
  * slower kernels of the same result.
+ * ctx may not overlap q, k or v.
  * Errors: INVALID_ARG (null, sizes, heads no multiple of kv_heads, rows shorter
- * than their heads, a tensor off its type's grid), UNSUPPORTED (head_dim above
+ * than their heads, an argument off its type's grid), UNSUPPORTED (head_dim above
  * 128, batch above 65535, lengths above 2^24, heads above 1024, rows of more
  * than 2^30 values, batch * q_len * heads of 2^33 or more); a length outside [0, kv_len] is clamped and sets bit 0 of
  * *d_status. */
@@ -141,7 +142,12 @@ size_t sky_cross_attention_bwd_workspace_bytes(const sky_cross_shape* shape);
 /* Its backward, from dctx, the forward's inputs and its ctx and lse: dq (rows
  * of ldq), and dk, dv (rows of ldk, ldv), summed over the query heads of each
  * key head; keys past the valid length, and queries without keys, get zeros.
- * Deterministic.  The gradients may not overlap the inputs or each other.
+ * Deterministic.  The gradients may not overlap the inputs or each other (as
+ * memory: dk and dv may be blocks of the same rows), and calls that may overlap
+ * on the GPU need a workspace each.
+ * bf16 on the tensor cores takes P and dS as bf16 operands, as sky_attention_bwd
+ * does, and dot(dctx, ctx) from the bf16 ctx: dq and dk come out 1.3 to 2 times
+ * the error of one rounding.
  * Errors as the forward's; INVALID_ARG for a workspace that is too small or not
  * 16-byte aligned. */
 sky_status sky_cross_attention_bwd(const sky_cross_shape* shape, const void* q, const void* k,
@@ -178,7 +184,7 @@ typedef struct {
  * and must not overlap it otherwise.  Serves a batch of new tokens (a row each)
  * as it does a training batch.
  * Errors: INVALID_ARG (null, sizes, an unknown dtype or rotation, rows shorter
- * than their heads), UNSUPPORTED (head_dim not a multiple of 16 or above 256,
+ * than their heads, gains or positions off their type's grid), UNSUPPORTED (head_dim not a multiple of 16 or above 256,
  * x or y not 16-byte aligned, ldx or ldy not a multiple of 16 bytes, rows of
  * more than 2^24 values). */
 sky_status sky_qk_norm_fwd(const sky_qk_norm_shape* shape, const void* x, const void* q_gain,
@@ -194,6 +200,7 @@ size_t sky_qk_norm_bwd_workspace_bytes(const sky_qk_norm_shape* shape);
  * of ldx; may be dy where ldy == ldx, or x) and the fp32 gain gradients, the
  * sums of dz * xhat over all rows and query (key) heads, to dq_gain and dk_gain
  * ([head_dim]; either may be NULL), in a fixed order (deterministic).
+ * Calls that may overlap on the GPU need a workspace each.
  * Errors as the forward's; INVALID_ARG for a workspace that is too small or not
  * 4-byte aligned. */
 sky_status sky_qk_norm_bwd(const sky_qk_norm_shape* shape, const void* x, const void* dy,

@@ -6,6 +6,7 @@
 //   dQ = dS K / sqrt(D),  dK = sum of dS^T Q / sqrt(D),  dV = sum of P^T dctx
 // over the query heads of a key head.
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "abi.h"
@@ -40,6 +41,11 @@ sky_status check(const sky_cross_shape* s) {
 // others serve what does not meet it).
 bool on_grid(const sky_cross_shape& s, const void* p) {
   return reinterpret_cast<uintptr_t>(p) % (s.dtype == SKY_DTYPE_BF16 ? 2 : 4) == 0;
+}
+bool words(std::initializer_list<const void*> ps) {  // lengths, log-sum-exps, status: 4 bytes
+  for (const void* p : ps)
+    if (reinterpret_cast<uintptr_t>(p) & 3) return false;
+  return true;
 }
 
 attn::Geometry geometry(const sky_cross_shape& s, const void* q, const void* k, const void* v, const int32_t* len,
@@ -89,6 +95,7 @@ sky_status sky_cross_attention_fwd(const sky_cross_shape* shape, const void* q, 
   SKY_CHECK(q && k && v && d_len && ctx, SKY_ERR_INVALID_ARG, "null argument");
   for (const void* p : {q, k, v, static_cast<const void*>(ctx)})
     SKY_CHECK(cross::on_grid(*shape, p), SKY_ERR_INVALID_ARG, "a tensor off its type's grid");
+  SKY_CHECK(cross::words({d_len, lse, d_status}), SKY_ERR_INVALID_ARG, "lengths, lse or status off the 4-byte grid");
   const attn::Geometry g = cross::geometry(*shape, q, k, v, d_len, d_status);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   return shape->dtype == SKY_DTYPE_BF16 ? cross::forward<__nv_bfloat16>(*shape, g, ctx, lse, st)
@@ -112,6 +119,7 @@ sky_status sky_cross_attention_bwd(const sky_cross_shape* shape, const void* q, 
   for (const void* p : {q, k, v, ctx, dctx, static_cast<const void*>(dq), static_cast<const void*>(dk),
                         static_cast<const void*>(dv)})
     SKY_CHECK(cross::on_grid(*shape, p), SKY_ERR_INVALID_ARG, "a tensor off its type's grid");
+  SKY_CHECK(cross::words({d_len, lse, d_status}), SKY_ERR_INVALID_ARG, "lengths, lse or status off the 4-byte grid");
   SKY_CHECK((reinterpret_cast<uintptr_t>(workspace) & 15) == 0, SKY_ERR_INVALID_ARG,
             "workspace must be 16-byte aligned");
   SKY_CHECK(workspace_bytes >= cross::workspace(*shape), SKY_ERR_INVALID_ARG, "workspace too small");

@@ -1,4 +1,6 @@
 // The C ABI of the head norms (kernels: qk_norm.cuh).
+#include <initializer_list>
+
 #include "abi.h"
 #include "qk_norm.cuh"
 
@@ -58,6 +60,16 @@ Params params(const sky_qk_norm_shape& s, const void* q_gain, const void* k_gain
   return p;
 }
 
+// Gains on their type's grid, positions and gain gradients on 4 bytes.
+bool small_on_grid(const sky_qk_norm_shape& s, std::initializer_list<const void*> gains,
+                   std::initializer_list<const void*> words) {
+  for (const void* p : gains)
+    if (reinterpret_cast<uintptr_t>(p) % (s.dtype == SKY_DTYPE_BF16 ? 2 : 4)) return false;
+  for (const void* p : words)
+    if (reinterpret_cast<uintptr_t>(p) & 3) return false;
+  return true;
+}
+
 bool a16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 size_t workspace(const sky_qk_norm_shape& s) {  // 2 rows a CTA, of as many as any plan makes
@@ -80,6 +92,8 @@ sky_status sky_qk_norm_fwd(const sky_qk_norm_shape* shape, const void* x, const 
   SKY_CHECK(x && y, SKY_ERR_INVALID_ARG, "null argument");
   SKY_CHECK(d_pos || shape->rotation == SKY_ROTATE_NONE, SKY_ERR_INVALID_ARG, "a rotation needs positions");
   SKY_CHECK(x != y || shape->ldx == shape->ldy, SKY_ERR_INVALID_ARG, "in place needs ldx == ldy");
+  SKY_CHECK(qkn::small_on_grid(*shape, {q_gain, k_gain}, {d_pos}), SKY_ERR_INVALID_ARG,
+            "gains or positions off their type's grid");
   SKY_CHECK(qkn::a16(x) && qkn::a16(y), SKY_ERR_UNSUPPORTED, "head norm tensors must be 16-byte aligned");
   qkn::Params p = qkn::params(*shape, q_gain, k_gain, d_pos);
   p.x = x;
@@ -102,6 +116,8 @@ sky_status sky_qk_norm_bwd(const sky_qk_norm_shape* shape, const void* x, const 
   SKY_CHECK(x && dy && dx && workspace, SKY_ERR_INVALID_ARG, "null argument");
   SKY_CHECK(d_pos || shape->rotation == SKY_ROTATE_NONE, SKY_ERR_INVALID_ARG, "a rotation needs positions");
   SKY_CHECK(dx != dy || shape->ldx == shape->ldy, SKY_ERR_INVALID_ARG, "in place needs ldx == ldy");
+  SKY_CHECK(qkn::small_on_grid(*shape, {q_gain, k_gain}, {d_pos, dq_gain, dk_gain}), SKY_ERR_INVALID_ARG,
+            "gains, positions or gain gradients off their type's grid");
   SKY_CHECK(qkn::a16(x) && qkn::a16(dy) && qkn::a16(dx), SKY_ERR_UNSUPPORTED,
             "head norm tensors must be 16-byte aligned");
   SKY_CHECK((reinterpret_cast<uintptr_t>(workspace) & 3) == 0, SKY_ERR_INVALID_ARG,

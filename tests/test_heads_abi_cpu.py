@@ -66,6 +66,12 @@ def test_norm_refuses_arguments(lib):
     for i in (0, 1, 5):
         assert bwd(s, *[odd if j == i else a for j, a in enumerate(ok)], need, None) == UNSUPPORTED
     assert bwd(s, *ok[:8], C.c_void_p((1 << 20) + 2), need, None) == INVALID
+    byte, half = C.c_void_p((1 << 20) + 1), C.c_void_p((1 << 20) + 2)
+    for i, off in ((2, byte), (3, byte), (4, half), (6, half), (7, half)):  # gains, positions, gain gradients
+        assert bwd(s, *[off if j == i else a for j, a in enumerate(ok)], need, None) == INVALID
+    for i, off in ((1, byte), (2, byte), (3, half)):
+        assert fwd(s, *[off if j == i else AT for j in range(5)], None) == INVALID
+    assert fwd(norm_shape(dtype=L.SKY_DTYPE_FP32), AT, half, AT, AT, AT, None) == INVALID
     assert bwd(s, *ok, need - 1, None) == INVALID
 
 
@@ -106,6 +112,11 @@ def test_cross_refuses_arguments(lib):
         assert fwd(s, *[None if j == i else AT for j in range(7)], None) == INVALID
     for i in (0, 1, 2, 4):
         assert fwd(s, *[odd if j == i else AT for j in range(7)], None) == INVALID
+    for i in (3, 5, 6):  # lengths, lse, status
+        assert fwd(s, *[odd if j == i else AT for j in range(7)], None) == INVALID
+    for i in (5, 6):
+        assert bwd(s, *[odd if j == i else AT for j in range(11)], need, None, None) == INVALID
+    assert bwd(s, *[AT] * 11, need, odd, None) == INVALID
     assert bwd(None, *[AT] * 11, need, None, None) == INVALID
     for i in range(11):
         assert bwd(s, *[None if j == i else AT for j in range(11)], need, None, None) == INVALID
