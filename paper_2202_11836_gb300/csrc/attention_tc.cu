@@ -1497,7 +1497,7 @@ struct ShortMaps {
 template <bool X>
 __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_constant__ CUtensorMap tmQKV,
                                                                const __grid_constant__ CUtensorMap tmO,
-                                                               const __grid_constant__ CUtensorMap tmC,
+                                                               const __grid_constant__ CUtensorMap tmC,  // not X
                                                                const __grid_constant__ CUtensorMap tmOut,
                                                                const __grid_constant__ ShortMaps tmX,
                                                                const BwdParams p) {
@@ -1525,7 +1525,7 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
     ptx::fence_proxy_async_smem();
     ptx::prefetch_tensormap(&tmQKV);
     ptx::prefetch_tensormap(&tmO);
-    ptx::prefetch_tensormap(&tmC);
+    if (!X) ptx::prefetch_tensormap(&tmC);
   }
   if (warp == 1) {
     ptx::tmem_alloc(tmem_slot, 256);
@@ -1550,10 +1550,9 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
         ptx::tma_load_2d(smem + SH_Q, &tmQKV, qk_full, a * HD, row0);
         ptx::tma_load_2d(smem + SH_K, &tmQKV, qk_full, H + a * HD, row0);
       }
-      ptx::mbar_arrive_expect_tx(ov_full, 3 * Q_BYTES);
+      ptx::mbar_arrive_expect_tx(ov_full, (X ? 2 : 3) * Q_BYTES);
       if constexpr (X) {
         ptx::tma_load_4d(smem + SH_O, &tmO, ov_full, 0, head0, 0, b);
-        ptx::tma_load_4d(smem + SH_DS, &tmC, ov_full, 0, head0, 0, b);
         ptx::tma_load_4d(smem + SH_V, &tmX.v, ov_full, 0, a, 0, b);
       } else {
         ptx::tma_load_2d(smem + SH_O, &tmO, ov_full, a * HD, row0);
@@ -1639,8 +1638,8 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
     // delta = dO . O of the row, from the swizzled tiles (loaded from global memory
     // row by row, 16 bytes a lane, this took 8 us)
     float dl = 0.f;
-    bool ok = wait_all(ov_full);
-    if (ok) {
+    bool ok = X || wait_all(ov_full);
+    if (!X && ok) {
       const uint32_t so = ptx::smem_u32(smem + SH_O) + r * 128, sx = ptx::smem_u32(smem + SH_DS) + r * 128;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -1655,9 +1654,34 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
         }
       }
     }
-    const uint64_t sc2 = pack2(sl2, sl2), nlse = pack2(nlse2, nlse2), ndl = pack2(-dl, -dl);
-    softmax_warps_sync();  // every row's O is read: dS may be written
+    const uint64_t sc2 = pack2(sl2, sl2), nlse = pack2(nlse2, nlse2);
+    if (!X) softmax_warps_sync();  // every row's O is read: dS may be written
     ok = ok && wait_all(sc_full);
+    if constexpr (X) {
+      // delta = sum over the keys of P dP, which the row's two threads have between them:
+      // with few keys what ctx lost to its rounding would be most of dS's error (2.7 to
+      // 3.5e-3 of dQ's norm, 2.3e-3 so), and ctx need not be read
+      if (ok) {
+        ptx::tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {
+          uint32_t sv[32], dv[32];
+          ptx::tmem_ld_32x32b_x32(tS + lane_base + hf * 64 + c, sv);
+          ptx::tmem_ld_32x32b_x32(tdP + lane_base + hf * 64 + c, dv);
+          ptx::tmem_ld_wait();
+          const int left = live ? len - hf * 64 - c : 0;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i < left) dl = fmaf(ptx::ex2_ftz(fmaf(__uint_as_float(sv[i]), sl2, nlse2)), __uint_as_float(dv[i]), dl);
+        }
+      }
+      float* half = reinterpret_cast<float*>(smem + SH_DS);  // (dS is not there yet)
+      half[hf * 128 + r] = dl;
+      softmax_warps_sync();
+      dl = half[r] + half[128 + r];
+      softmax_warps_sync();
+    }
+    const uint64_t ndl = pack2(-dl, -dl);
     if (ok) {
       ptx::tc_fence_after();
       const uint32_t sp = ptx::smem_u32(smem + SH_P) + hf * Q_BYTES + r * 128;
@@ -2069,15 +2093,14 @@ size_t cross_attention_bwd_tc_ws(const attn::Geometry& g, int B) {
 
 // One tile of queries, of all heads that share a key head, and one of keys: everything in
 // one launch.
-static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, int pack, const void* ctx,
-                                               const void* dctx, const float* lse, void* dq, void* dk, void* dv,
-                                               cudaStream_t stream) {
+static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, int pack, const void* dctx,
+                                               const float* lse, void* dq, void* dk, void* dv, cudaStream_t stream) {
   using namespace attn_tc;
   const int hp = 1 << pack, take = BQ >> pack, Akv = g.A / g.group;
-  CUtensorMap tq, to, tc, tdq;
+  CUtensorMap tq, to, tdq;
   ShortMaps x;
   SKY_CHECK(cross_map(&tq, g.q, g.A, g.Sq, B, g.ldq, hp, take) && cross_map(&to, dctx, g.A, g.Sq, B, g.ldo, hp, take) &&
-                cross_map(&tc, ctx, g.A, g.Sq, B, g.ldo, hp, take) && cross_map(&tdq, dq, g.A, g.Sq, B, g.ldq, hp, take) &&
+                cross_map(&tdq, dq, g.A, g.Sq, B, g.ldq, hp, take) &&
                 cross_map(&x.k, g.k, Akv, g.Skv, B, g.ldk, 1, BQ) && cross_map(&x.v, g.v, Akv, g.Skv, B, g.ldv, 1, BQ) &&
                 cross_map(&x.dk, dk, Akv, g.Skv, B, g.ldk, 1, BQ) && cross_map(&x.dv, dv, Akv, g.Skv, B, g.ldv, 1, BQ),
             SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the cross attention backward operands");
@@ -2086,7 +2109,7 @@ static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, i
   if (attr != cudaSuccess) return cuda_fail(attr, "cross attention backward smem attribute");
   const BwdParams p{g.Sq, 0, g.A, g.lens, lse, nullptr, nullptr, nullptr, nullptr, g.status, kTimeoutNs,
                     {g.Skv, g.group, pack}, nullptr, nullptr, 0, 0};
-  const cudaError_t e = launch_pdl(attn_bwd_short_tc<true>, dim3(Akv, B), dim3(SH_THR), SH_SMEM, stream, 1, tq, to, tc,
+  const cudaError_t e = launch_pdl(attn_bwd_short_tc<true>, dim3(Akv, B), dim3(SH_THR), SH_SMEM, stream, 1, tq, to, to,
                                    tdq, x, p);
   count_launches(1);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core cross attention backward launch");
@@ -2097,7 +2120,7 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ct
   using namespace attn_tc;
   for (int pack = 0; pack <= 7; ++pack)
     if (g.group == 1 << pack && static_cast<int64_t>(g.Sq) << pack <= BQ && g.Skv <= BQ)
-      return cross_attention_bwd_short_tc(g, B, pack, ctx, dctx, lse, dq, dk, dv, stream);
+      return cross_attention_bwd_short_tc(g, B, pack, dctx, lse, dq, dk, dv, stream);
   const int packQ = best_pack(g, BQ), packK = best_pack(g, BQ2), hq = 1 << packQ, hk = 1 << packK;
   const int Akv = g.A / g.group, sms = sm_count() > 0 ? sm_count() : 148;
   const int q_tiles = ceil_div(static_cast<int64_t>(g.Sq) << packQ, BQ), k_tiles = ceil_div(g.Skv, BK2);
