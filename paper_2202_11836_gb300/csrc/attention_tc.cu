@@ -2128,19 +2128,18 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ct
   // what a CTA walks through: key tiles, and query tiles of all heads that read its keys
   const int q_steps = ceil_div(g.Skv, BKV),
             k_steps = ceil_div(static_cast<int64_t>(g.Sq) << packK, BQ2) * (g.group >> packK);
-  // Split where few CTAs would walk far, down to two steps each: dK/dV up to 9/4 CTAs an
+  // Split where few CTAs would walk far, down to two steps each: dK/dV up to two CTAs an
   // SM, dQ up to 5/4 (it runs beside dK/dV).  us, unsplit and split: 2 x 775 queries, 16
   // heads on 4, 161 keys 62 and 20; 11 x 953, 9 on 3, 16 keys 71 and 36; 40 queries, 12 on
-  // 4, 945 keys 13.9 and 9.4; 20 x 10, 8 on 4, 1454 keys 37.4 and 33.5; 6 x 197, 12 on 4,
-  // 777 keys 23.9 and 21.2.  dQ up to two: that last shape 24.3 and 29.5 then; dK/dV just
-  // below the limit may lose: 5 x 321, 6 on 2, 456 keys 20.7 and 22.8; up to three: 4 x
-  // 256, 4 heads, 1770 keys 18.4 and 23.1.
+  // 4, 945 keys 13.9 and 9.4; 20 x 10, 8 on 4, 1454 keys 37.4 and 33.5.  dQ up to two: 6 x
+  // 197, 12 on 4, 777 keys 24.3 and 29.5; dK/dV up to four: 4 x 256, 4 heads, 1770 keys 18.3
+  // and 27.2.
   const auto splits = [&](int64_t ctas, int steps, int most, int pack) {  // (a split stores whole queries)
     int ks = 1;
     while (ks < 8 && 2 * ks * ctas <= most && steps >= 4 * ks && BQ / (2 * ks) >> pack > 0) ks *= 2;
     return ks;
   };
-  const int ksq = splits(q_ctas, q_steps, 5 * sms / 4, packQ), ksk = splits(k_ctas, k_steps, 9 * sms / 4, 0);
+  const int ksq = splits(q_ctas, q_steps, 5 * sms / 4, packQ), ksk = splits(k_ctas, k_steps, 2 * sms, 0);
   CUtensorMap tq128, to128, tk64, tv64, tdq, tk128, tv128, tq64, to64, tdk, tdv;
   SKY_CHECK(cross_map(&tq128, g.q, g.A, g.Sq, B, g.ldq, hq, BQ >> packQ) &&
                 cross_map(&to128, dctx, g.A, g.Sq, B, g.ldo, hq, BQ >> packQ) &&
