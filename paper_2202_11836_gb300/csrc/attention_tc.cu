@@ -2133,7 +2133,8 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ct
   // heads on 4, 161 keys 62 and 20; 11 x 953, 9 on 3, 16 keys 71 and 36; 40 queries, 12 on
   // 4, 945 keys 13.9 and 9.4; 20 x 10, 8 on 4, 1454 keys 37.4 and 33.5.  dQ up to two: 6 x
   // 197, 12 on 4, 777 keys 24.3 and 29.5; dK/dV up to four: 4 x 256, 4 heads, 1770 keys 18.3
-  // and 27.2.
+  // and 27.2, up to 9/4: that first shape 24.2 and 21.2 to 24.3, by its lengths, and 5 x 321,
+  // 6 on 2, 456 keys 21.7 and 23.3.
   const auto splits = [&](int64_t ctas, int steps, int most, int pack) {  // (a split stores whole queries)
     int ks = 1;
     while (ks < 8 && 2 * ks * ctas <= most && steps >= 4 * ks && BQ / (2 * ks) >> pack > 0) ks *= 2;
