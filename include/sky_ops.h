@@ -129,8 +129,8 @@ typedef struct {
  * Errors: INVALID_ARG (null, sizes, heads no multiple of kv_heads, rows shorter
  * than their heads, an argument off its type's grid), UNSUPPORTED (head_dim above
  * 128, batch above 65535, lengths above 2^24, heads above 1024, rows of more
- * than 2^30 values, batch * q_len * heads of 2^33 or more); a length outside [0, kv_len] is clamped and sets bit 0 of
- * *d_status. */
+ * than 2^30 values, batch * q_len * heads of 2^33 or more); a length outside
+ * [0, kv_len] is clamped and sets bit 0 of *d_status. */
 sky_status sky_cross_attention_fwd(const sky_cross_shape* shape, const void* q, const void* k,
                                    const void* v, const int32_t* d_len, void* ctx, float* lse,
                                    int32_t* d_status, void* stream);
@@ -181,13 +181,14 @@ typedef struct {
  * query heads and k_gain of the key heads (each [head_dim]; NULL: ones) and R
  * the rotation by the row's position d_pos[row] (int32[rows], any value; may be
  * NULL without a rotation).  Statistics, angles and products are fp32 or finer;
- * angles keep their precision at every position.  y may be x where ldy == ldx,
- * and must not overlap it otherwise.  Serves a batch of new tokens (a row each)
- * as it does a training batch.
+ * angles keep their precision at every position.  A head whose sum of squares
+ * leaves fp32's range comes out as zeros, a head of zeros with eps = 0 as NaN.
+ * y may be x where ldy == ldx, and must not overlap it otherwise.  Serves a batch
+ * of new tokens (a row each) as it does a training batch.
  * Errors: INVALID_ARG (null, sizes, an unknown dtype or rotation, rows shorter
- * than their heads, gains or positions off their type's grid), UNSUPPORTED (head_dim not a multiple of 16 or above 256,
- * x or y not 16-byte aligned, ldx or ldy not a multiple of 16 bytes, rows of
- * more than 2^24 values). */
+ * than their heads, gains or positions off their type's grid), UNSUPPORTED
+ * (head_dim not a multiple of 16 or above 256, x or y not 16-byte aligned, ldx or
+ * ldy not a multiple of 16 bytes, rows of more than 2^24 values). */
 sky_status sky_qk_norm_fwd(const sky_qk_norm_shape* shape, const void* x, const void* q_gain,
                            const void* k_gain, const int32_t* d_pos, void* y, void* stream);
 

@@ -300,7 +300,6 @@ __global__ void __launch_bounds__(THR) qk_norm_fwd(const __grid_constant__ Param
   extern __shared__ __align__(16) uint8_t ring_mem[];
   __shared__ __align__(16) float tab[WARPS * Angles<ROT, LP>::TAB];
   const Place<T, LP, NP, DIM> at(p);
-  
   Angles<ROT, LP> ang(p, tab);
   const float inv = 1.f / static_cast<float>(at.D);
   Ring<T, LP, NP, DIM, 1, STAGES> ring(p, at, ring_mem);
@@ -351,7 +350,6 @@ __global__ void __launch_bounds__(THR) qk_norm_bwd(const __grid_constant__ Param
   __shared__ __align__(8) float sums[ONE ? 2 : 1][ONE ? LP * 16 : 1];
   __shared__ int kind_of[WARPS];
   const Place<T, LP, NP, DIM> at(p);
-  
   Angles<ROT, LP> ang(p, tab);
   const float inv = 1.f / static_cast<float>(at.D);
   Ring<T, LP, NP, DIM, 2, STAGES> ring(p, at, ring_mem);
@@ -381,7 +379,8 @@ __global__ void __launch_bounds__(THR) qk_norm_bwd(const __grid_constant__ Param
         d = fma2(mul2(zh[e], ghi[e]), hi[e], d);
       }
       const float ss = head_sum<LP>(sum2(a, b)), sh = head_sum<LP>(sum2(c, d));
-      const float rs = rsqrtf(ss * inv + p.eps);
+      // (lanes without a head: zeros, whose norm without an eps would be NaN in the gains' sums)
+      const float rs = rsqrtf(ss * inv + (at.live(i) ? p.eps : 1.f));
       const uint64_t r = both(rs), m = both(-(sh * rs * inv));  // - mean of h xhat
 #pragma unroll
       for (int e = 0; e < 4; ++e) {

@@ -32,9 +32,10 @@ def f64(t):
 
 
 class Case:
-    def __init__(self, rows, a, k, dim, dtype, rotation, behind=0, gains=True, far=True, seed=0):
+    def __init__(self, rows, a, k, dim, dtype, rotation, behind=0, gains=True, far=True, seed=0, eps=EPS):
         g = torch.Generator(device="cuda").manual_seed(1000 * rows + 10 * a + dim + seed)
         self.rows, self.a, self.k, self.dim, self.dtype, self.rotation = rows, a, k, dim, dtype, rotation
+        self.eps = eps
         self.t, code, self.half_step = TYPES[dtype]
         self.width = (a + k) * dim
         self.ld = self.width + behind
@@ -47,7 +48,7 @@ class Case:
         self.gain = [(1 + 0.2 * normal(dim)).to(self.t) if gains else None for _ in range(2)]
         hi = 1 << 31 if far else 2048
         self.pos = torch.randint(-hi if far else 0, hi, (rows,), device="cuda", generator=g).to(torch.int32)
-        self.shape = L.SkyQkNormShape(rows, a, k, dim, code, self.ld, self.width, EPS, ROT[rotation], THETA)
+        self.shape = L.SkyQkNormShape(rows, a, k, dim, code, self.ld, self.width, eps, ROT[rotation], THETA)
 
     def forward(self, y=None):
         y = torch.full((self.rows, self.width), MARK, device="cuda", dtype=self.t) if y is None else y
@@ -74,8 +75,8 @@ class Case:
     def want(self):
         x = f64(self.x[:, :self.width]).reshape(self.rows, -1, self.dim)
         pos = f64(self.pos)
-        y = ORC.head_norm(x, self.gain64(), pos, EPS, self.rotation, THETA)
-        dx, terms = ORC.head_norm_backward(x, f64(self.dy).reshape(x.shape), self.gain64(), pos, EPS, self.rotation,
+        y = ORC.head_norm(x, self.gain64(), pos, self.eps, self.rotation, THETA)
+        dx, terms = ORC.head_norm_backward(x, f64(self.dy).reshape(x.shape), self.gain64(), pos, self.eps, self.rotation,
                                            THETA)
         return x, y, dx, terms
 
@@ -93,7 +94,7 @@ class Case:
     def check_backward(self, dx, dq, dk):
         x, _, want, terms = self.want()
         got = f64(dx).reshape(want.shape)
-        rms = np.sqrt((x * x).mean(-1, keepdims=True) + EPS)
+        rms = np.sqrt((x * x).mean(-1, keepdims=True) + self.eps)
         dz = np.abs(f64(self.dy)).reshape(x.shape).max(-1, keepdims=True) * 2 ** 0.5
         h = dz * np.abs(self.gain64()).max(-1)[None, :, None]
         # dx = (h - xhat m) / rms, m a mean of D products; xhat is at most sqrt(D)
@@ -172,6 +173,20 @@ def test_zero_heads_and_no_gain_gradients():
     L.call("sky_qk_norm_bwd", c.shape, P(c.x), P(c.dy), None, None, P(c.pos), P(dx), None, None, P(ws), n, stream())
     torch.cuda.synchronize()
     assert bool(torch.isfinite(dx[:, :c.width]).all())
+
+
+@pytest.mark.parametrize("shape", [(40, 3, 1, 64), (5000, 9, 2, 32), (700, 5, 5, 96), (300, 17, 9, 64)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_eps_of_zero(shape, dtype):
+    """Lanes without a head of their own have zeros to norm, which nothing may take in."""
+    c = Case(*shape, dtype, "halves", far=False, eps=0.0)
+    y = c.forward()
+    dx, dq, dk = c.backward()
+    for t in (y, dx, dq, dk):
+        assert bool(torch.isfinite(t).all())
+    c.check_forward(y)
+    c.check_backward(dx, dq, dk)
 
 
 def test_bad_values_stay_in_their_heads():
