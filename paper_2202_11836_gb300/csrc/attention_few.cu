@@ -1,10 +1,10 @@
 // Cross attention of few query rows: the step of a decoder that writes token by token.
 // The rows of one key head, q_len * group of them (row r: query r / group, head r %
-// group), are at most 16, so a key or value is read for a handful of products and the
-// kernels are bound by those reads.  Keys are split over the warps of a CTA and the CTAs
-// of a cluster, in chunks of 32 dealt out in turn; each warp keeps m, l and O of its
-// chunks (a softmax in one pass), and the parts are joined in the order of warps, then of
-// CTAs: m the largest, l and O scaled to it.
+// group), are at most 16, or 32 over many keys, so a key or value is read for a handful of
+// products and the kernels are bound by those reads.  Keys are split over the warps of a
+// CTA and the CTAs of a cluster, in chunks of 32 dealt out in turn; each warp keeps m, l
+// and O of its chunks (a softmax in one pass), and the parts are joined in the order of
+// warps, then of CTAs: m the largest, l and O scaled to it.
 //
 // What lies behind the valid keys reaches nothing: scores there are replaced by -inf, and
 // V's rows are cleared before a product takes them.
@@ -102,11 +102,12 @@ __device__ void join(const Params& p, float* O, float2* ml, int LD, int len, int
 // transposed), and the stage is free again when they are in registers.  No warp waits
 // for another before the parts are joined.
 //
-// One token of 32 requests, 256..512 keys, 16 heads: 11.7 us, 50 MB at 4.3 TB/s; the
+// One token of 32 requests, 256..512 keys, 16 heads: 11.2 us, 50 MB at 4.5 TB/s; the
 // reads alone would take 7.4, launch, first loads and joining are the rest (2.4 us with
-// three keys).  Long sources pay for the longest: 4 of 5000..20000 keys, 4 key heads, 13.7
+// three keys).  Long sources pay for the longest: 4 of 5000..20000 keys, 4 key heads, 13.3
 // (floor 7.6); a warp takes 0.45 us a chunk, whose latency two stages and three CTAs an SM
-// cover.  Measured against it (us, the two cases): fragments loaded by the lanes
+// cover (told to stay at three, the compiler takes 108 registers for 80: 11.6 and 13.6
+// before).  Measured against that form (us, the two cases): fragments loaded by the lanes
 // themselves with cp.async, 323 instructions a 16-key chunk, 14.9 and 21.0; three stages
 // 15.4 and 18.1 (two CTAs an SM); chunks of 16 11.5 and 14.6; eight warps a CTA 17.4 and
 // 22.2; copies issued under lane == 0 13.3 and 14.5 (their operands then go to uniform
@@ -131,15 +132,17 @@ __device__ __forceinline__ void ldmatrix4t(uint32_t addr, uint32_t (&r)[4]) {
 }
 
 constexpr int STAGES = 2, TILE = CHUNK * 128;  // bytes of a chunk's K or V
-constexpr int MMA_ROWS = 16, MMA_LD = 64 + 4;
+constexpr int MMA_ROWS = 32, MMA_LD = 64 + 4;  // at most
 constexpr int RINGS = NW * STAGES * 2 * TILE, PARTS = (NW * MMA_ROWS * MMA_LD) * 4 + (NW + 1) * MMA_ROWS * 8;
 constexpr int BARS = RINGS > PARTS ? RINGS : PARTS;  // the parts go over the rings
 constexpr int MMA_SMEM = BARS + NW * STAGES * 8 + 1024;
 
-// H: halves of the 16 rows that hold any (1: at most 8 rows)
+// H: blocks of eight rows that hold any, two to a 16-row operand
 template <int H>
-__global__ void __launch_bounds__(NW * 32) attn_few_mma(const __grid_constant__ CUtensorMap tmK,
+__global__ void __launch_bounds__(NW * 32, 3) attn_few_mma(const __grid_constant__ CUtensorMap tmK,
                                                         const __grid_constant__ CUtensorMap tmV, const Params p) {
+  constexpr int M = (H + 1) / 2, ROWS = 16 * M;
+  const auto used = [](int i, int h) { return 2 * i + h < H; };  // half h of operand i
   extern __shared__ uint8_t raw[];
   uint8_t* sm = raw + (((ptx::smem_u32(raw) + 1023u) & ~1023u) - ptx::smem_u32(raw));
   const attn::Geometry& geo = p.g;
@@ -171,18 +174,22 @@ __global__ void __launch_bounds__(NW * 32) attn_few_mma(const __grid_constant__ 
   const int len = attn::valid_keys(geo.lens, b, 0, geo.Skv, geo.status);
   const int chunks = (len + CHUNK - 1) / CHUNK;
   const int mine = chunks > first ? (chunks - first + step - 1) / step : 0;
-  uint32_t qa[4][4];
+  uint32_t qa[M][4][4];
+  float o[M][8][4] = {}, m[M][2], l[M][2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int row = g + 8 * h, q = row / geo.group, a = kv * geo.group + row % geo.group;
-    const __nv_bfloat16* s = static_cast<const __nv_bfloat16*>(geo.q) +
-                             (static_cast<int64_t>(b) * geo.Sq + q) * geo.ldq + a * 64 + 2 * c;
+  for (int i = 0; i < M; ++i)
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      qa[k >> 1][h + 2 * (k & 1)] = h < H && row < p.all_rows ? *reinterpret_cast<const uint32_t*>(s + 8 * k) : 0u;
-  }
-  float o[8][4] = {};
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    for (int h = 0; h < 2; ++h) {
+      const int row = g + 8 * (2 * i + h), q = row / geo.group, a = kv * geo.group + row % geo.group;
+      const __nv_bfloat16* s = static_cast<const __nv_bfloat16*>(geo.q) +
+                               (static_cast<int64_t>(b) * geo.Sq + q) * geo.ldq + a * 64 + 2 * c;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        qa[i][k >> 1][h + 2 * (k & 1)] =
+            used(i, h) && row < p.all_rows ? *reinterpret_cast<const uint32_t*>(s + 8 * k) : 0u;
+      m[i][h] = -INFINITY;
+      l[i][h] = 0.f;
+    }
   __syncwarp();  // the barriers are ready
   // ldmatrix rows of the lane (16-byte piece i of row r is at i ^ (r & 7)): K: key lane %
   // 8 of an 8-key tile, piece lane / 8 (+ 4); V: key lane % 16 of a 16-key step, piece
@@ -201,69 +208,85 @@ __global__ void __launch_bounds__(NW * 32) attn_few_mma(const __grid_constant__ 
       for (int i = left * 8 + lane; i < CHUNK * 8; i += 32) ptx::st_shared_v4(src + TILE + i * 16, 0, 0, 0, 0);
       __syncwarp();
     }
-    float s[CHUNK / 8][4] = {};
+    float s[M][CHUNK / 8][4] = {};
 #pragma unroll
     for (int t = 0; t < CHUNK / 8; ++t) {
       uint32_t x[4], y[4];
       ldmatrix4(src + t * 1024 + krow + (((lane >> 3) ^ (lane & 7)) << 4), x);
       ldmatrix4(src + t * 1024 + krow + (((4 + (lane >> 3)) ^ (lane & 7)) << 4), y);
-      mma16816(s[t], qa[0], x[0], x[1]);
-      mma16816(s[t], qa[1], x[2], x[3]);
-      mma16816(s[t], qa[2], y[0], y[1]);
-      mma16816(s[t], qa[3], y[2], y[3]);
+#pragma unroll
+      for (int i = 0; i < M; ++i) {
+        mma16816(s[i][t], qa[i][0], x[0], x[1]);
+        mma16816(s[i][t], qa[i][1], x[2], x[3]);
+        mma16816(s[i][t], qa[i][2], y[0], y[1]);
+        mma16816(s[i][t], qa[i][3], y[2], y[3]);
+      }
     }
     if (left < CHUNK) {
 #pragma unroll
-      for (int t = 0; t < CHUNK / 8; ++t)
+      for (int i = 0; i < M; ++i)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (8 * t + 2 * c + (i & 1) >= left) s[t][i] = -INFINITY;
+        for (int t = 0; t < CHUNK / 8; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (8 * t + 2 * c + (e & 1) >= left) s[i][t][e] = -INFINITY;
     }
-    float nm[2] = {0.f, 0.f};
+    float nm[M][2], alpha[M][2];
     bool raised = false;
-    float alpha[2] = {1.f, 1.f};
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-      float mx = -INFINITY;
+    for (int i = 0; i < M; ++i)
 #pragma unroll
-      for (int t = 0; t < CHUNK / 8; ++t) mx = fmaxf(mx, fmaxf(s[t][2 * h], s[t][2 * h + 1]));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-      const float mn = fmaxf(fmaxf(m[h], mx * p.scale), -FLT_MAX);
-      raised |= mn > m[h];
-      alpha[h] = exp2f(m[h] - mn);
-      m[h] = mn;
-      nm[h] = -mn;
-    }
+      for (int h = 0; h < 2; ++h) {
+        if (!used(i, h)) continue;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < CHUNK / 8; ++t) mx = fmaxf(mx, fmaxf(s[i][t][2 * h], s[i][t][2 * h + 1]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        const float mn = fmaxf(fmaxf(m[i][h], mx * p.scale), -FLT_MAX);
+        raised |= mn > m[i][h];
+        alpha[i][h] = exp2f(m[i][h] - mn);
+        m[i][h] = mn;
+        nm[i][h] = -mn;
+      }
     if (__any_sync(0xffffffffu, raised)) {
 #pragma unroll
-      for (int h = 0; h < H; ++h) {
-        l[h] *= alpha[h];
+      for (int i = 0; i < M; ++i)
 #pragma unroll
-        for (int d = 0; d < 8; ++d) {
-          o[d][2 * h] *= alpha[h];
-          o[d][2 * h + 1] *= alpha[h];
+        for (int h = 0; h < 2; ++h) {
+          if (!used(i, h)) continue;
+          l[i][h] *= alpha[i][h];
+#pragma unroll
+          for (int d = 0; d < 8; ++d) {
+            o[i][d][2 * h] *= alpha[i][h];
+            o[i][d][2 * h + 1] *= alpha[i][h];
+          }
         }
-      }
     }
 #pragma unroll
     for (int u = 0; u < CHUNK / 16; ++u) {
-      uint32_t pa[4] = {};
+      uint32_t pa[M][4] = {};
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < M; ++i)
 #pragma unroll
-        for (int h = 0; h < H; ++h) {
-          const float e0 = ptx::ex2_ftz(fmaf(s[2 * u + i][2 * h], p.scale, nm[h]));
-          const float e1 = ptx::ex2_ftz(fmaf(s[2 * u + i][2 * h + 1], p.scale, nm[h]));
-          l[h] += e0 + e1;
-          pa[2 * i + h] = ptx::pack_bf16(e0, e1);  // rounded as the tensor cores take it
-        }
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (!used(i, h)) continue;
+            const float e0 = ptx::ex2_ftz(fmaf(s[i][2 * u + t][2 * h], p.scale, nm[i][h]));
+            const float e1 = ptx::ex2_ftz(fmaf(s[i][2 * u + t][2 * h + 1], p.scale, nm[i][h]));
+            l[i][h] += e0 + e1;
+            pa[i][2 * t + h] = ptx::pack_bf16(e0, e1);  // rounded as the tensor cores take it
+          }
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         uint32_t v[4];
         ldmatrix4t(src + u * 2048 + vrow + (((2 * d + (lane >> 4)) ^ (lane & 7)) << 4), v);
-        mma16816(o[2 * d], pa, v[0], v[1]);
-        mma16816(o[2 * d + 1], pa, v[2], v[3]);
+#pragma unroll
+        for (int i = 0; i < M; ++i) {
+          mma16816(o[i][2 * d], pa[i], v[0], v[1]);
+          mma16816(o[i][2 * d + 1], pa[i], v[2], v[3]);
+        }
       }
     }
     __syncwarp();  // the stage is read
@@ -278,18 +301,21 @@ __global__ void __launch_bounds__(NW * 32) attn_few_mma(const __grid_constant__ 
   pdl_trigger();
   __syncthreads();  // every warp's ring is read: the parts go over it
   float* O = reinterpret_cast<float*>(sm);
-  float2* ml = reinterpret_cast<float2*>(O + NW * MMA_ROWS * MMA_LD);
+  float2* ml = reinterpret_cast<float2*>(O + NW * ROWS * MMA_LD);
 #pragma unroll
-  for (int h = 0; h < H; ++h) {
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-    l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-    const int row = warp * MMA_ROWS + g + 8 * h;
+  for (int i = 0; i < M; ++i)
 #pragma unroll
-    for (int d = 0; d < 8; ++d)
-      *reinterpret_cast<float2*>(O + row * MMA_LD + 8 * d + 2 * c) = make_float2(o[d][2 * h], o[d][2 * h + 1]);
-    if (c == 0) ml[row] = make_float2(m[h], l[h]);
-  }
-  join<__nv_bfloat16, MMA_ROWS>(p, O, ml, MMA_LD, len, b, kv, 0);
+    for (int h = 0; h < 2; ++h) {
+      if (!used(i, h)) continue;
+      l[i][h] += __shfl_xor_sync(0xffffffffu, l[i][h], 1);
+      l[i][h] += __shfl_xor_sync(0xffffffffu, l[i][h], 2);
+      const int row = warp * ROWS + g + 8 * (2 * i + h);
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+        *reinterpret_cast<float2*>(O + row * MMA_LD + 8 * d + 2 * c) = make_float2(o[i][d][2 * h], o[i][d][2 * h + 1]);
+      if (c == 0) ml[row] = make_float2(m[i][h], l[i][h]);
+    }
+  join<__nv_bfloat16, ROWS>(p, O, ml, MMA_LD, len, b, kv, 0);
 }
 
 // ------------------------------------------- any type, head dim and alignment
@@ -416,14 +442,18 @@ __global__ void __launch_bounds__(NW * 32) attn_few_simt(const Params p) {
 }  // namespace few
 
 namespace few {
-// The keys of a head over the CTAs of a cluster until there are two an SM, each left more
-// than 128 keys.  us, 512 heads of 256..512 keys: one CTA each 11.7, two 18.8 (they no
-// longer fit at once); 50 heads of 2300: four 6.8, eight 16.4; 114 of 170: one 3.4, two
-// 4.6, four 7.9; 16 heads of 5000..20000: sixteen 13.7.
-int split(int64_t heads, int Skv) {
+// The keys of a head over the CTAs of a cluster: doubled up to `most` fourths of a CTA an
+// SM, each left more than `keys` of them.  Twice 5/4 CTAs an SM are what still fits at once
+// with three an SM.  us: 512 heads of 256..512 keys unsplit 11.2, in two 18; 256 heads of 512
+// (16 rows) 6.9 and 13.7, 78 of 10300 13.6 and 18.5 (in two and four); 50 of 2300 in four 6.8,
+// in eight 16.4.  A cluster costs 1 to 3 us to start and join, so it is left alone for short
+// keys: 48 heads of 442 unsplit 3.8, in two 4.3; 8 of 1167 8.8 in two, four.  The CUDA cores
+// take 3 us for a chunk that takes the others 0.5, so shorter shares pay there: 12 heads of
+// 300 in two 5.0, unsplit 7.9; 192 of 512 in two 12.6, unsplit 17.5; 32 of 600 13.7 and 30.
+int split(int64_t heads, int Skv, int keys, int most) {
   const int sms = sm_count() > 0 ? sm_count() : 148;
   int ctas = 1;
-  while (ctas < 16 && ctas * heads < 2 * sms && Skv > 256 * ctas) ctas *= 2;
+  while (ctas < 16 && 4 * ctas * heads < most * sms && Skv > keys * ctas) ctas *= 2;
   return ctas;
 }
 
@@ -452,7 +482,7 @@ cudaError_t few_simt(const attn::Geometry& g, int B, T* ctx, float* lse, cudaStr
     const int heads = Akv * ((rows + RB - 1) / RB);
     static OncePerDevice wide;
     return launch(wide, attn_few_simt<T, decltype(lanes)::value, RB>,
-                  dim3(split(static_cast<int64_t>(heads) * B, g.Skv), heads, B), 0, stream, p);
+                  dim3(split(static_cast<int64_t>(heads) * B, g.Skv, 128, 8), heads, B), 0, stream, p);
   };
   const auto block = [&](auto lanes) {
     return rows == 1 ? go(lanes, std::integral_constant<int, 1>{}) : go(lanes, std::integral_constant<int, 4>{});
@@ -463,13 +493,18 @@ cudaError_t few_simt(const attn::Geometry& g, int B, T* ctx, float* lse, cudaStr
 }
 }  // namespace few
 
+// Up to 32 rows where the keys are many: the tiles' kernel splits them over four CTAs at
+// most.  us, 32 rows, 128-row tiles and this: 4 heads of 20000 keys 42 and 12.6, 24 of 3000
+// 10.3 and 9.1, 128 of 3000 22.8 and 22.4; of 1100 keys 7.1 and 7.0, 12.7 and 13.2; 128 of
+// 700 8.2 and 11.2.
 bool cross_attention_few_fits(const attn::Geometry& g) {
-  return static_cast<int64_t>(g.Sq) * g.group <= few::MMA_ROWS;
+  const int64_t rows = static_cast<int64_t>(g.Sq) * g.group;
+  return rows <= few::MMA_ROWS / 2 || (rows <= few::MMA_ROWS && g.Skv >= 2048);
 }
 
 sky_status cross_attention_few(const attn::Geometry& g, int B, void* ctx, float* lse, cudaStream_t stream) {
   using namespace few;
-  const int Akv = g.A / g.group, ctas = split(static_cast<int64_t>(Akv) * B, g.Skv);
+  const int Akv = g.A / g.group, ctas = split(static_cast<int64_t>(Akv) * B, g.Skv, 512, 5);
   const Params p{g, g.Sq * g.group, scale(g.D), ctx, lse};
   CUtensorMap tk, tv;
   SKY_CHECK(attn_tc::cross_map(&tk, g.k, Akv, g.Skv, B, g.ldk, 1, CHUNK) &&
@@ -481,7 +516,9 @@ sky_status cross_attention_few(const attn::Geometry& g, int B, void* ctx, float*
     const cudaError_t e = allow_smem(once, kern, MMA_SMEM);
     return e != cudaSuccess ? e : launch(wide, kern, dim3(ctas, Akv, B), MMA_SMEM, stream, tk, tv, p);
   };
-  const cudaError_t e = p.all_rows <= 8 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, 2>{});
+  const cudaError_t e = p.all_rows <= 8    ? go(std::integral_constant<int, 1>{})
+                        : p.all_rows <= 16 ? go(std::integral_constant<int, 2>{})
+                                           : go(std::integral_constant<int, 4>{});
   count_launches(1);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "few-row cross attention launch");
 }

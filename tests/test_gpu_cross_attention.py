@@ -292,6 +292,7 @@ def test_lengths_outside_are_clamped_and_reported():
 @pytest.mark.parametrize("sq,heads,kv_heads,skv,lens", [
     (1, 16, 16, 512, [512, 256, 300, 1, 0, 511]), (1, 16, 4, 2500, [2500, 1300]), (2, 8, 1, 1031, [1031, 0, 5]),
     (4, 4, 4, 333, [333, 32, 33]), (1, 1, 1, 5000, [4999]), (3, 10, 2, 700, [700, 16, 15, 17]), (1, 32, 1, 260, [260]),
+    (17, 2, 2, 2100, [2100, 0, 1999]), (8, 12, 4, 2048, [2048, 1, 33]), (32, 1, 1, 3001, [3001]), (1, 25, 1, 4100, [4100, 7]),
 ])
 def test_few_query_rows(sq, heads, kv_heads, skv, lens, dtype):
     c = Case(sq, skv, heads, kv_heads, lens, dtype=dtype).poison()
