@@ -8,6 +8,7 @@
 
 #include "attention_simt.h"
 #include "common.cuh"
+#include "ptx.cuh"
 #include "row4.cuh"
 
 namespace sky {
@@ -141,6 +142,17 @@ __device__ __forceinline__ void accumulate(const float* w, const float* cols, in
     }
   }
 }
+template <typename T>
+__device__ __forceinline__ void store_to(T* p, int d, int D, bool vec, const float4& v) {  // p: value d of a row
+  if (vec) {
+    store4(p, v);
+  } else {
+    p[0] = from_f32<T>(v.x);
+    if (d + 1 < D) p[1] = from_f32<T>(v.y);
+    if (d + 2 < D) p[2] = from_f32<T>(v.z);
+    if (d + 3 < D) p[3] = from_f32<T>(v.w);
+  }
+}
 template <int CC, typename T>
 __device__ __forceinline__ void store_rows(T* X, int64_t ld, int r0, int rows, int D, bool vec, float scale0,
                                            float scale1, const float4 (&o)[2][CC]) {
@@ -155,15 +167,7 @@ __device__ __forceinline__ void store_rows(T* X, int64_t ld, int r0, int rows, i
       const int d = 4 * tx + 64 * cc;
       if (d >= D) continue;
       const float4 v = make_float4(o[i][cc].x * sc, o[i][cc].y * sc, o[i][cc].z * sc, o[i][cc].w * sc);
-      T* p = X + static_cast<int64_t>(r) * ld + d;
-      if (vec) {
-        store4(p, v);
-      } else {
-        p[0] = from_f32<T>(v.x);
-        if (d + 1 < D) p[1] = from_f32<T>(v.y);
-        if (d + 2 < D) p[2] = from_f32<T>(v.z);
-        if (d + 3 < D) p[3] = from_f32<T>(v.w);
-      }
+      store_to(X + static_cast<int64_t>(r) * ld + d, d, D, vec, v);
     }
   }
 }
@@ -278,12 +282,23 @@ __global__ void __launch_bounds__(F_THR, 3) attn_fwd_simt(const Geometry g, cons
 // operand of the columns / sqrt(D), dV = P . dO.  Four CTAs an SM (128 registers) are
 // faster up to a head dim of 64 (29.8 us against 34.7 at 4 x 101, 12 heads), above it
 // the registers are (50.6 against 57.0 at 2 x 200, 6 heads of 128).
-template <bool SELF, typename T, int G, int NC>
+//
+// Not SELF: where a block has many columns and there are few blocks, the CTAs of a cluster
+// share its columns and add their parts.
+struct Splits {
+  int ks;           // CTAs of a cluster; 1: none, blocks of the two kinds alternate
+  bool keys_first;  // the kind with the longer blocks comes first
+  bool whole[2];    // whether the first kind's blocks, and the second's, are left whole
+};
+enum Kind { SELF_ATTENTION, CROSS, CROSS_SPLIT };
+template <Kind KIND, typename T, int G, int NC>
 __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geometry g, const T* __restrict__ gq,
                                                       const T* __restrict__ gk, const T* __restrict__ gv,
                                                       const int32_t* __restrict__ lens, const T* __restrict__ dctx,
                                                       const float* __restrict__ lse, const float* __restrict__ delta,
-                                                      T* __restrict__ dq, T* __restrict__ dk, T* __restrict__ dv) {
+                                                      T* __restrict__ dq, T* __restrict__ dk, T* __restrict__ dv,
+                                                      const Splits sp) {
+  constexpr bool SELF = KIND == SELF_ATTENTION, SPLIT = KIND == CROSS_SPLIT;
   using ST = Stage<G, NC>;
   constexpr int CC = ST::CC, TC = ST::ROWS, P_LD = TC + 4;
   pdl_wait();
@@ -292,40 +307,68 @@ __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geo
   const int LD = g.LD, D = g.D, Sq = g.Sq, Skv = ld.Skv;
   const bool vec = g.vec;
   float *r0s = sm, *r1s = r0s + FR * LD, *c0s = r1s + FR * LD, *c1s = c0s + TC * LD;
-  float *sds = c1s + TC * LD, *sp = sds + FR * P_LD, *sl = sp + FR * P_LD, *sd = sl + TC;
-  const int qtiles = (Sq + FR - 1) / FR, ktiles = (Skv + FR - 1) / FR, x = blockIdx.x;
-  const int qunits = qtiles * g.A, kunits = ktiles * (g.A / ld.group), both = SELF ? qunits : min(qunits, kunits);
-  const bool keys = SELF || x < 2 * both ? x & 1 : qunits < kunits;  // own rows are keys
-  const int u = SELF || x < 2 * both ? x >> 1 : x - both, tiles = keys ? ktiles : qtiles;
-  const int head = u / tiles, r0 = (u % tiles) * FR, b = blockIdx.y;  // of its kind
+  float *sds = c1s + TC * LD, *sps = sds + FR * P_LD, *sl = sps + FR * P_LD, *sd = sl + TC;
+  const int qtiles = (Sq + FR - 1) / FR, ktiles = (Skv + FR - 1) / FR;
+  const int qunits = qtiles * g.A, kunits = ktiles * (g.A / ld.group);
+  // its place: kind, number within the kind, and part of the columns
+  int x = blockIdx.x, split = 0, splits = 1;
+  bool keys;  // own rows are keys
+  if (SELF) {
+    keys = x & 1;
+    x >>= 1;
+  } else if (!SPLIT) {
+    const int both = min(qunits, kunits);
+    keys = x < 2 * both ? x & 1 : qunits < kunits;
+    x = x < 2 * both ? x >> 1 : x - both;
+  } else {  // clusters of one kind, then of the other: a block each, or one of every CTA
+    const int n = sp.keys_first ? kunits : qunits, first = sp.whole[0] ? (n + sp.ks - 1) / sp.ks * sp.ks : n * sp.ks;
+    const bool second = x >= first;
+    keys = second != sp.keys_first;
+    if (second) x -= first;
+    if (!sp.whole[second]) {
+      splits = sp.ks;
+      split = x % splits;
+      x /= splits;
+    } else if (x >= (keys ? kunits : qunits)) {
+      return;
+    }
+  }
+  const int tiles = keys ? ktiles : qtiles;
+  const int head = x / tiles, r0 = (x % tiles) * FR, b = blockIdx.y;  // of its kind
   const int kv = keys ? head : head / ld.group, heads = keys ? ld.group : 1;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int len = valid_keys(lens, b, SELF ? 1 : 0, Skv, g.status);
-  const T* self = gq + static_cast<int64_t>(b) * Sq * ld.q + head * D;
+  const T* self = gq + static_cast<int64_t>(b) * Sq * ld.q + head * D;  // (of queries)
   const T* k = SELF ? self + ld.H : gk + static_cast<int64_t>(b) * Skv * ld.k + kv * D;
   const T* v = SELF ? self + 2 * ld.H : gv + static_cast<int64_t>(b) * Skv * ld.v + kv * D;
   const float sc = 1.f / sqrtf((float)D), sl2 = sc * 1.4426950408889634f;
   float4 o0[2][CC] = {}, o1[2][CC] = {};
   const int rows = keys ? Skv : Sq, cols = keys ? Sq : len;
   float4 own0[ST::OWN], own1[ST::OWN];
-  for (int h = 0; h < heads && (!keys || r0 < len); ++h) {
-    const int a = !SELF && keys ? kv * ld.group + h : head;
-    const T* q = SELF ? self : gq + static_cast<int64_t>(b) * Sq * ld.q + a * D;
-    const T* dO = dctx + static_cast<int64_t>(b) * Sq * ld.o + a * D;
-    const float *lse_b = lse + (static_cast<int64_t>(b) * g.A + a) * Sq, *del_b = delta + (static_cast<int64_t>(b) * g.A + a) * Sq;
-    if (h == 0) {
-      load_rows<G>(keys ? k : q, keys ? ld.k : ld.q, r0, rows, D, vec, own0);
-      load_rows<G>(keys ? v : dO, keys ? ld.v : ld.o, r0, rows, D, vec, own1);
-    }
-    float lr[2] = {}, dr[2] = {};
+  const int ctiles = (cols + TC - 1) / TC, all = keys && r0 >= len ? 0 : heads * ctiles;
+  const int begin = SPLIT ? split * all / splits : 0, end = SPLIT ? (split + 1) * all / splits : all;
+  float lr[2] = {}, dr[2] = {};
+  if (begin < end) {
+    const T* dO = dctx + static_cast<int64_t>(b) * Sq * ld.o + head * D;  // (of queries)
+    load_rows<G>(keys ? k : self, keys ? ld.k : ld.q, r0, rows, D, vec, own0);
+    load_rows<G>(keys ? v : dO, keys ? ld.v : ld.o, r0, rows, D, vec, own1);
     if (!keys)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int r = min(r0 + 2 * ty + i, Sq - 1);
-        lr[i] = lse_b[r];
-        dr[i] = del_b[r];
+        const int64_t r = (static_cast<int64_t>(b) * g.A + head) * Sq + min(r0 + 2 * ty + i, Sq - 1);
+        lr[i] = lse[r];
+        dr[i] = delta[r];
       }
-    for (int c0 = 0; c0 < cols; c0 += TC) {
+  }
+  int h = SPLIT && begin < end ? begin / ctiles : 0, from = SPLIT ? begin - h * ctiles : 0;
+  for (int left = end - begin; left > 0; ++h, from = 0, left = SELF ? 0 : left) {  // a head's tiles
+    const int a = !SELF && keys ? kv * ld.group + h : head, to = SPLIT ? min(ctiles, from + left) : ctiles;
+    const T* q = SELF ? self : gq + static_cast<int64_t>(b) * Sq * ld.q + a * D;
+    const T* dO = dctx + static_cast<int64_t>(b) * Sq * ld.o + a * D;
+    const float *lse_b = lse + (static_cast<int64_t>(b) * g.A + a) * Sq, *del_b = delta + (static_cast<int64_t>(b) * g.A + a) * Sq;
+    const bool first = SELF || left == end - begin;
+    left -= to - from;
+    for (int c0 = from * TC; c0 < to * TC; c0 += TC) {
       __syncthreads();
       // columns: queries (Q, dO; all S) or keys (K, V; the valid ones)
       const T *x0 = keys ? q : k, *x1 = keys ? dO : v;
@@ -341,7 +384,7 @@ __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geo
         float4 v0[ST::PASSES], v1[ST::PASSES];
         load_rows<G>(x0, keys ? ld.q : ld.k, c0 + R * t, cols, D, vec, v0);
         load_rows<G>(x1, keys ? ld.o : ld.v, c0 + R * t, cols, D, vec, v1);
-        if (t == 0 && c0 == 0 && h == 0) {
+        if (t == 0 && first && c0 == from * TC) {
           put_rows<G>(r0s, LD, D, own0);
           put_rows<G>(r1s, LD, D, own1);
         }
@@ -364,12 +407,12 @@ __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geo
           const bool live = c0 + cl < cols && (!keys || r0 + 2 * ty + i < len);
           const float p = live ? exp2f(fmaf(s[i][c], sl2, -(keys ? sl[cl] : lr[i]))) : 0.f;
           sds[(2 * ty + i) * P_LD + cl] = live ? p * (dp[i][c] - (keys ? sd[cl] : dr[i])) : 0.f;
-          if (keys) sp[(2 * ty + i) * P_LD + cl] = p;
+          if (keys) sps[(2 * ty + i) * P_LD + cl] = p;
         }
       __syncwarp();
       const int n = min(TC, cols - c0);
       accumulate<CC, P_LD>(sds, c0s, LD, D, n, o0);
-      if (keys) accumulate<CC, P_LD>(sp, c1s, LD, D, n, o1);
+      if (keys) accumulate<CC, P_LD>(sps, c1s, LD, D, n, o1);
       __syncwarp();
     }
   }
@@ -377,8 +420,40 @@ __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geo
   T* out = dq + static_cast<int64_t>(b) * Sq * ld.q + head * D;
   T* out_k = SELF ? out + ld.H : dk + static_cast<int64_t>(b) * Skv * ld.k + kv * D;
   T* out_v = SELF ? out + 2 * ld.H : dv + static_cast<int64_t>(b) * Skv * ld.v + kv * D;
-  store_rows<CC>(keys ? out_k : out, keys ? ld.k : ld.q, r0, rows, D, vec, sc, sc, o0);
-  if (keys) store_rows<CC>(out_v, ld.v, r0, rows, D, vec, 1.f, 1.f, o1);
+  if (!SPLIT || splits == 1) {
+    store_rows<CC>(keys ? out_k : out, keys ? ld.k : ld.q, r0, rows, D, vec, sc, sc, o0);
+    if (keys) store_rows<CC>(out_v, ld.v, r0, rows, D, vec, 1.f, 1.f, o1);
+    return;
+  }
+  // the parts, over the columns' tiles, and FR / splits rows of their sum, in split order
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int cc = 0; cc < CC; ++cc) {
+      const int d = 4 * tx + 64 * cc;
+      if (d >= D) continue;
+      *reinterpret_cast<float4*>(c0s + (2 * ty + i) * LD + d) = o0[i][cc];
+      if (keys) *reinterpret_cast<float4*>(c1s + (2 * ty + i) * LD + d) = o1[i][cc];
+    }
+  ptx::cluster_sync();
+  const int groups = (D + 3) / 4, mine = FR / splits;
+  for (int e = threadIdx.x; e < mine * groups; e += F_THR) {
+    const int lr_ = split * mine + e / groups, d = e % groups * 4, r = r0 + lr_;
+    if (r >= rows) continue;
+    for (int which = 0; which < (keys ? 2 : 1); ++which) {
+      const uint32_t at = ptx::smem_u32((which ? c1s : c0s) + lr_ * LD + d);
+      float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c = 0; c < splits; ++c) {
+        const float4 w = ptx::ld_cluster_f4(ptx::mapa_shared(at, c));
+        u.x += w.x; u.y += w.y; u.z += w.z; u.w += w.w;
+      }
+      if (!which) u = make_float4(u.x * sc, u.y * sc, u.z * sc, u.w * sc);
+      const int64_t ldr = !keys ? ld.q : which ? ld.v : ld.k;
+      store_to((!keys ? out : which ? out_v : out_k) + r * ldr + d, d, D, vec, u);
+    }
+  }
+  ptx::cluster_sync();  // the peers have read this CTA's part
 }
 
 // Launch shape: the shared row stride (four floats past the head dim, so the 16 lanes of
@@ -416,6 +491,34 @@ cudaError_t fwd_simt(Geometry g, int B, T* ctx, float* lse, cudaStream_t stream)
                      : go(Group<32>{}, attn_fwd_simt<SELF, T, 32>);
 }
 
+// The columns of the kind that has more of them, and of the other where it has more than is
+// then left to a CTA, are split while the longest block takes about as long as the SMs'
+// share of all work: to a step each where the CTAs all fit at once, two where they take up
+// to four rounds.  us, whole and split, heads of 64 unless stated: 6 queries of 6 heads of
+// 128 on 2, 1650 keys 182 and 40; 9 x 468, 4 on 1, 6 keys 199 and 51; 2 x 182, 8 on 2, 38
+// keys 105 and 28; 3 x 51, one of 128, 340 keys 41 and 19; 2 x 605, 6 of 128, 37 keys 124
+// and 54.  Beyond these limits: 2 x 57, 12 of 128 on 6, 177 keys (a step each, more than a
+// round) 34 and 43; 10 x 490, 6 of 32, 69 keys (eight rounds) 97 and 248; 116, 24 of 128 on
+// 6, 1453 keys (balanced whole) 370 and 435.  Tiles of 16 columns are left whole.
+Splits bwd_splits(const Geometry& g, int B, unsigned* blocks) {
+  const int64_t units[2] = {static_cast<int64_t>(ceil_div(g.Sq, FR)) * g.A,
+                            static_cast<int64_t>(ceil_div(g.Skv, FR)) * (g.A / g.group)};  // queries, keys
+  const int steps[2] = {ceil_div(g.Skv, FC), ceil_div(g.Sq, FC) * g.group};
+  const bool keys = steps[1] > steps[0];
+  const int64_t room = static_cast<int64_t>(sm_count() > 0 ? sm_count() : 148) * (g.D > 64 ? 2 : 4);
+  const int64_t all = (units[0] * steps[0] + units[1] * steps[1]) * B;
+  Splits sp{1, keys, {true, true}};
+  for (int ks = 2; ks <= 8 && steps[keys] >= ks && std::max(g.Sq, g.Skv) > 16; ks *= 2) {
+    const bool whole = steps[!keys] <= ceil_div(steps[keys], ks);  // the shorter kind
+    const int64_t n = ks * (units[keys] + (whole ? ceil_div(units[!keys], ks) : units[!keys]));
+    if (n * B > 4 * room || (n * B > room && steps[keys] < 2 * ks)) break;
+    if (9 * room * ceil_div(steps[keys], ks / 2) < 8 * all) break;
+    sp = {ks, keys, {false, whole}};
+    *blocks = static_cast<unsigned>(n);
+  }
+  return sp;
+}
+
 template <bool SELF, typename T>
 cudaError_t bwd_simt(Geometry g, int B, const T* ctx, const T* dctx, const float* lse, float* delta, T* dq, T* dk,
                      T* dv, cudaStream_t stream) {
@@ -426,23 +529,28 @@ cudaError_t bwd_simt(Geometry g, int B, const T* ctx, const T* dctx, const float
   if (le != cudaSuccess) return le;
   g.LD = row_stride(g.D);
   g.vec = rows_of_4<T>(g, dctx, dq, dk, dv);
-  const unsigned blocks = (unsigned)ceil_div(g.Sq, FR) * g.A + (unsigned)ceil_div(g.Skv, FR) * (g.A / g.group);
+  Splits sp{1, false, {true, true}};
+  unsigned blocks = (unsigned)ceil_div(g.Sq, FR) * g.A + (unsigned)ceil_div(g.Skv, FR) * (g.A / g.group);
+  if (!SELF) sp = bwd_splits(g, B, &blocks);
   const auto go = [&](auto group, auto nc, auto kern) {
     constexpr int G = decltype(group)::value, NC = decltype(nc)::value;
-    static OncePerDevice once;
-    const cudaError_t e = allow_smem(once, kern, bwd_smem(4 * G, NC));
+    static OncePerDevice once[2];  // (both cross kinds have the same type)
+    const cudaError_t e = allow_smem(once[sp.ks > 1], kern, bwd_smem(4 * G, NC));
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, dim3(blocks, B), dim3(F_THR), bwd_smem(g.D, NC), stream, 1, g,
+    return launch_pdl(kern, dim3(blocks, B), dim3(F_THR), bwd_smem(g.D, NC), stream, sp.ks, g,
                       static_cast<const T*>(g.q), static_cast<const T*>(g.k), static_cast<const T*>(g.v), g.lens, dctx, lse,
-                      static_cast<const float*>(delta), dq, dk, dv);
+                      static_cast<const float*>(delta), dq, dk, dv, sp);
   };
   // Up to 16 tokens a 64-column tile is mostly empty: 128 x 8 tokens, 6 heads of 128
   // 52.4 us with it, 27.8 with 16 columns (a warp a row 28.8); 12 of 64 45.2 and 25.5
   // (41.1); 64 x 16, 12 of 64 29.8 and 18.3 (70.4).
   const auto width = [&](auto group) {
     constexpr int G = decltype(group)::value;
-    return std::max(g.Sq, g.Skv) <= 16 ? go(group, std::integral_constant<int, 1>{}, attn_bwd_simt<SELF, T, G, 1>)
-                                       : go(group, std::integral_constant<int, 4>{}, attn_bwd_simt<SELF, T, G, 4>);
+    constexpr Kind WHOLE = SELF ? SELF_ATTENTION : CROSS;
+    if constexpr (!SELF)
+      if (sp.ks > 1) return go(group, std::integral_constant<int, 4>{}, attn_bwd_simt<CROSS_SPLIT, T, G, 4>);
+    return std::max(g.Sq, g.Skv) <= 16 ? go(group, std::integral_constant<int, 1>{}, attn_bwd_simt<WHOLE, T, G, 1>)
+                                       : go(group, std::integral_constant<int, 4>{}, attn_bwd_simt<WHOLE, T, G, 4>);
   };
   return g.D <= 32 ? width(Group<8>{}) : g.D <= 64 ? width(Group<16>{}) : width(Group<32>{});
 }

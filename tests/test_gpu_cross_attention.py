@@ -256,6 +256,21 @@ def test_sums_split_over_a_cluster(sq, skv, heads, kv_heads, lens):
     assert all(torch.equal(x.buf, y.buf) for x, y in zip(grads, c.backward(*c.given())))
 
 
+@pytest.mark.parametrize("sq,skv,heads,kv_heads,lens,dim,shift,dtype", [
+    (6, 1650, 6, 2, [1650, 0, 582], 128, 0, "fp32"), (468, 6, 4, 1, [6, 0, 5], 64, 0, "fp32"),
+    (182, 38, 8, 2, [38, 19], 64, 0, "fp32"), (51, 340, 1, 1, [340, 65, 1], 33, 1, "fp32"),
+    (53, 700, 3, 3, [700, 64], 20, 0, "fp32"), (130, 17, 5, 1, [17, 16], 32, 0, "fp32"),
+    (10, 300, 4, 2, [300, 129, 0], 80, 0, "bf16"), (150, 70, 6, 2, [70, 0], 64, 1, "bf16"),
+    (600, 530, 2, 2, [530], 32, 0, "fp32"), (17, 17, 16, 1, [17, 3], 64, 0, "fp32"),
+])
+def test_columns_split_on_the_cuda_cores(sq, skv, heads, kv_heads, lens, dim, shift, dtype):
+    """The same where the tensor cores do not serve: one kind's blocks, or both kinds', in parts."""
+    c = Case(sq, skv, heads, kv_heads, lens, dtype=dtype, dim=dim, beside=shift, shift=shift).poison()
+    grads = c.backward(*c.given())
+    c.check_backward(grads)
+    assert all(torch.equal(x.buf, y.buf) for x, y in zip(grads, c.backward(*c.given())))
+
+
 def test_forward_feeds_backward():
     """The library's own ctx and lse: within what the forward may be off more."""
     c = Case(150, 220, 6, 3, [220, 100, 0, 7]).poison()
