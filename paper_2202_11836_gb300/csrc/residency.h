@@ -8,8 +8,8 @@
 // their shared memory could want more than its 512 columns.  So they must not
 // fit:
 //   the split attention forward, and the dQ and dK/dV kernels where they are split
-//   (256 columns, two CTAs an SM), take so much shared memory that two of their CTAs
-//   leave no room for a cluster product's;
+//   (256 columns), take so much shared memory that two of their CTAs leave no room for
+//   a third of them or for a cluster product's;
 //   cluster products (at most 128 columns) take at least kClusterProductSmem.
 // (The persistent product takes a whole SM, and everything else that allocates
 // finishes by itself.)
@@ -19,9 +19,10 @@ namespace sky {
 
 constexpr int kSmemPerSM = 233472, kSmemPerCta = 1024;  // of an SM; reserved for a CTA
 constexpr int kClusterProductSmem = 80 * 1024;          // dynamic shared memory, at least
-constexpr int kSplitAttentionSmem = 73 * 1024;
+constexpr int kSplitAttentionSmem = 77 * 1024;          // dynamic shared memory, at least
 static_assert(2 * (kSplitAttentionSmem + kSmemPerCta) + kClusterProductSmem + kSmemPerCta > kSmemPerSM,
               "two split attention CTAs and a cluster product on an SM");
+static_assert(3 * (kSplitAttentionSmem + kSmemPerCta) > kSmemPerSM, "three split attention CTAs on an SM");
 static_assert(2 * (kSplitAttentionSmem + kSmemPerCta) <= kSmemPerSM, "two split attention CTAs on an SM");
 
 }  // namespace sky
