@@ -146,9 +146,8 @@ size_t sky_cross_attention_bwd_workspace_bytes(const sky_cross_shape* shape);
  * memory: dk and dv may be blocks of the same rows), and calls that may overlap
  * on the GPU need a workspace each.
  * bf16 on the tensor cores takes P and dS as bf16 operands, as sky_attention_bwd
- * does, and dot(dctx, ctx) from the bf16 ctx where a key head's queries or its
- * keys are more than 128: dq and dk come out 1.3 to 2 times the error of one
- * rounding.
+ * does, and where keys or queries are many dot(dctx, ctx) from the bf16 ctx: dq
+ * and dk come out 1.3 to 2 times the error of one rounding.
  * Errors as the forward's; INVALID_ARG for a workspace that is too small or not
  * 16-byte aligned. */
 sky_status sky_cross_attention_bwd(const sky_cross_shape* shape, const void* q, const void* k,

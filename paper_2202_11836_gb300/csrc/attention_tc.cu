@@ -1488,13 +1488,16 @@ constexpr int SH_SMEM = SH_BAR + 128;
 constexpr int SH_THR = 320;  // warp 0 TMA, warp 1 MMA issue, warps 2..9 softmax
 static_assert(2 * (SH_SMEM + 1024) <= 233472, "two CTAs per SM");
 
-// X: a key head's queries, S of each of the 2^pack heads that share it, are the tile's
-// rows; maps of Q, K, V and of dQ, dK, dV.
+// X: keys up to 128.  A CTA has a tile of the queries that read a key head: 128 >> pack
+// queries of 2^pack heads.  KS > 1: the CTAs of a cluster have KS tiles between them, which
+// are all (of the last ones, rows past the queries are zeros and add nothing), and add
+// their parts of dK and dV.  Maps of Q, K, V and of dQ, dK, dV.
 struct ShortMaps {
   CUtensorMap k, v, dk, dv;
 };
+static_assert(SH_SMEM >= kSplitAttentionSmem, "clusters that hold 256 columns: see residency.h");
 
-template <bool X>
+template <bool X, int KS = 1>
 __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_constant__ CUtensorMap tmQKV,
                                                                const __grid_constant__ CUtensorMap tmO,
                                                                const __grid_constant__ CUtensorMap tmC,  // not X
@@ -1509,9 +1512,14 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
   uint64_t* g_full = pds_full + 1;   // dV, dK, dQ complete
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(g_full + 1);
 
-  const int a = blockIdx.x, b = blockIdx.y;
-  const int pack = X ? p.x.pack : 0, head0 = a << pack;
-  const int S = p.S << pack, H = p.H;  // rows of the tile that hold a query
+  const int a = blockIdx.x / KS, split = blockIdx.x % KS, b = blockIdx.y;  // X: a is the key head
+  const int pack = X ? p.x.pack : 0;
+  const int tiles = KS > 1 ? ((p.S << pack) + BQ - 1) / BQ : 1, block = split / tiles;  // of heads
+  const int q0 = KS > 1 ? (split - block * tiles) * (BQ >> pack) : 0;
+  const int head0 = X ? a * p.x.group + (block << pack) : a;
+  // rows of the tile that hold a query (none behind the last block)
+  const bool has = KS == 1 || (block << pack) < p.x.group;
+  const int S = KS > 1 ? (has ? min(BQ, (p.S - q0) << pack) : 0) : p.S << pack, H = p.H;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row0 = b * S;
   const uint64_t lim = p.timeout_ns;
@@ -1544,7 +1552,7 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
     if (lane == 0) {
       ptx::mbar_arrive_expect_tx(qk_full, 2 * Q_BYTES);
       if constexpr (X) {
-        ptx::tma_load_4d(smem + SH_Q, &tmQKV, qk_full, 0, head0, 0, b);
+        ptx::tma_load_4d(smem + SH_Q, &tmQKV, qk_full, 0, has ? head0 : 0, has ? q0 : p.S, b);
         ptx::tma_load_4d(smem + SH_K, &tmX.k, qk_full, 0, a, 0, b);
       } else {
         ptx::tma_load_2d(smem + SH_Q, &tmQKV, qk_full, a * HD, row0);
@@ -1552,7 +1560,7 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
       }
       ptx::mbar_arrive_expect_tx(ov_full, (X ? 2 : 3) * Q_BYTES);
       if constexpr (X) {
-        ptx::tma_load_4d(smem + SH_O, &tmO, ov_full, 0, head0, 0, b);
+        ptx::tma_load_4d(smem + SH_O, &tmO, ov_full, 0, has ? head0 : 0, has ? q0 : p.S, b);
         ptx::tma_load_4d(smem + SH_V, &tmX.v, ov_full, 0, a, 0, b);
       } else {
         ptx::tma_load_2d(smem + SH_O, &tmO, ov_full, a * HD, row0);
@@ -1630,7 +1638,7 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
     const bool live = r < S;
     const float nlse2 =
         !live ? 0.f
-        : X   ? -p.lse[(static_cast<int64_t>(b) * p.A + head0 + (r & ((1 << pack) - 1))) * p.S + (r >> pack)]
+        : X   ? -p.lse[(static_cast<int64_t>(b) * p.A + head0 + (r & ((1 << pack) - 1))) * p.S + q0 + (r >> pack)]
               : -p.lse[(static_cast<int64_t>(b) * p.A + a) * S + r];
     auto wait_all = [&](uint64_t* bar) {
       return __all_sync(0xffffffffu, ptx::mbar_wait(bar, 0, lim, p.status, kWaitHint));
@@ -1741,6 +1749,10 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
         uint32_t o[32];
         ptx::tmem_ld_32x32b_x32((is_q ? tdQ : (hf == 0 ? tdK : tdV)) + lane_base + col, o);
         ptx::tmem_ld_wait();
+        if (KS > 1 && !is_q) {  // over P and dS (without a query no product was made)
+          put_part(smem + SH_P + hf * PART_BYTES, r, c, S > 0, o);
+          continue;
+        }
         if (X && (is_q ? len == 0 : r >= len)) {  // queries without keys; keys past the valid length
 #pragma unroll
           for (int i = 0; i < 32; ++i) o[i] = 0u;
@@ -1771,9 +1783,11 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
     softmax_warps_sync();
     if (warp == 2 && lane == 0) {
       if constexpr (X) {
-        ptx::tma_store_4d(&tmOut, smem + SH_Q, 0, head0, 0, b);
-        ptx::tma_store_4d(&tmX.dk, smem + SH_K, 0, a, 0, b);
-        ptx::tma_store_4d(&tmX.dv, smem + SH_V, 0, a, 0, b);
+        if (S > 0) ptx::tma_store_4d(&tmOut, smem + SH_Q, 0, head0, q0, b);
+        if (KS == 1) {
+          ptx::tma_store_4d(&tmX.dk, smem + SH_K, 0, a, 0, b);
+          ptx::tma_store_4d(&tmX.dv, smem + SH_V, 0, a, 0, b);
+        }
       } else {
         ptx::tma_store_3d(&tmOut, smem + SH_Q, a * HD, 0, b);
         ptx::tma_store_3d(&tmOut, smem + SH_K, H + a * HD, 0, b);
@@ -1788,6 +1802,27 @@ __global__ void __launch_bounds__(SH_THR, 2) attn_bwd_short_tc(const __grid_cons
       p.colpart[static_cast<int64_t>(b) * 3 * H + g * H + a * HD + c] = ((x[0] + x[64]) + x[128]) + x[192];
     }
     if (warp == 2 && lane == 0) ptx::bulk_wait_group_read0();  // before the CTA's memory goes
+  }
+  if constexpr (KS > 1) {
+    __syncwarp();
+    ptx::cluster_sync();  // every tile's parts are where they are read from
+    const int t = static_cast<int>(threadIdx.x) - 64, first = split * (BQ / KS);
+    if (t >= 0) {
+      const int g = t >> 7;  // dK, dV, over K and its neighbour
+      constexpr int STAGE_BYTES = BQ / KS * 128;
+      add_parts<KS>(smem + SH_P + g * PART_BYTES, smem + SH_K + g * STAGE_BYTES, t & 127, split, g == 0 ? 0.125f : 1.f,
+                    len);
+      ptx::fence_proxy_async_smem();
+      softmax_warps_sync();
+      if (t == 0 && first < p.x.Skv) {
+        ptx::tma_store_4d(&tmX.dk, smem + SH_K, 0, a, first, b);
+        ptx::tma_store_4d(&tmX.dv, smem + SH_K + STAGE_BYTES, 0, a, first, b);
+        ptx::bulk_commit_group();
+        ptx::bulk_wait_group_read0();
+      }
+    }
+    __syncwarp();
+    ptx::cluster_sync();  // the peers have read this CTA's parts
   }
   ptx::tc_fence_before();
   __syncthreads();
@@ -1858,10 +1893,10 @@ bool cross_map(CUtensorMap* map, const void* base, int heads, int rows, int B, i
 namespace {
 // log2 of the heads that share a query tile of `rows` rows: the fewest tiles, then the
 // fewest heads.
-int best_pack(const attn::Geometry& g, int rows) {
+int best_pack(const attn::Geometry& g, int rows, int most = 5) {
   int best = 0;
   int64_t least = 0;
-  for (int p = 0; p <= 5 && g.group % (1 << p) == 0; ++p) {
+  for (int p = 0; p <= most && g.group % (1 << p) == 0; ++p) {
     const int64_t tiles = ((static_cast<int64_t>(g.Sq) << p) + rows - 1) / rows * (g.A >> p);
     if (p == 0 || tiles < least) {
       best = p;
@@ -2091,9 +2126,9 @@ size_t cross_attention_bwd_tc_ws(const attn::Geometry& g, int B) {
   return cross_delta_bytes(g, B) + static_cast<size_t>(B) * g.A * g.Sq * 2 * attn_tc::XROW_BYTES;
 }
 
-// One tile of queries, of all heads that share a key head, and one of keys: everything in
-// one launch.
-static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, int pack, const void* dctx,
+// One tile of keys, and up to ks of the queries that read a key head: everything in one
+// launch, a tile a CTA.
+static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, int pack, int ks, const void* dctx,
                                                const float* lse, void* dq, void* dk, void* dv, cudaStream_t stream) {
   using namespace attn_tc;
   const int hp = 1 << pack, take = BQ >> pack, Akv = g.A / g.group;
@@ -2102,15 +2137,23 @@ static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, i
   SKY_CHECK(cross_map(&tq, g.q, g.A, g.Sq, B, g.ldq, hp, take) && cross_map(&to, dctx, g.A, g.Sq, B, g.ldo, hp, take) &&
                 cross_map(&tdq, dq, g.A, g.Sq, B, g.ldq, hp, take) &&
                 cross_map(&x.k, g.k, Akv, g.Skv, B, g.ldk, 1, BQ) && cross_map(&x.v, g.v, Akv, g.Skv, B, g.ldv, 1, BQ) &&
-                cross_map(&x.dk, dk, Akv, g.Skv, B, g.ldk, 1, BQ) && cross_map(&x.dv, dv, Akv, g.Skv, B, g.ldv, 1, BQ),
+                cross_map(&x.dk, dk, Akv, g.Skv, B, g.ldk, 1, BQ / ks) &&
+                cross_map(&x.dv, dv, Akv, g.Skv, B, g.ldv, 1, BQ / ks),
             SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the cross attention backward operands");
-  static OncePerDevice once;
-  const cudaError_t attr = allow_smem(once, attn_bwd_short_tc<true>, SH_SMEM);
-  if (attr != cudaSuccess) return cuda_fail(attr, "cross attention backward smem attribute");
   const BwdParams p{g.Sq, 0, g.A, g.lens, lse, nullptr, nullptr, nullptr, nullptr, g.status, kTimeoutNs,
                     {g.Skv, g.group, pack}, nullptr, nullptr, 0, 0};
-  const cudaError_t e = launch_pdl(attn_bwd_short_tc<true>, dim3(Akv, B), dim3(SH_THR), SH_SMEM, stream, 1, tq, to, to,
-                                   tdq, x, p);
+  const auto go = [&](auto c) {
+    constexpr int KS = decltype(c)::value;
+    static OncePerDevice once;
+    const cudaError_t e = allow_smem(once, attn_bwd_short_tc<true, KS>, SH_SMEM);
+    return e != cudaSuccess ? e
+                            : launch_pdl(attn_bwd_short_tc<true, KS>, dim3(Akv * KS, B), dim3(SH_THR), SH_SMEM, stream,
+                                         KS, tq, to, to, tdq, x, p);
+  };
+  const cudaError_t e = ks == 1   ? go(std::integral_constant<int, 1>{})
+                        : ks == 2 ? go(std::integral_constant<int, 2>{})
+                        : ks == 4 ? go(std::integral_constant<int, 4>{})
+                                  : go(std::integral_constant<int, 8>{});
   count_launches(1);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core cross attention backward launch");
 }
@@ -2118,9 +2161,18 @@ static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, i
 sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ctx, const void* dctx, const float* lse,
                                   void* dq, void* dk, void* dv, void* ws, cudaStream_t stream) {
   using namespace attn_tc;
-  for (int pack = 0; pack <= 7; ++pack)
-    if (g.group == 1 << pack && static_cast<int64_t>(g.Sq) << pack <= BQ && g.Skv <= BQ)
-      return cross_attention_bwd_short_tc(g, B, pack, dctx, lse, dq, dk, dv, stream);
+  if (g.Skv <= BQ) {
+    const int pack = best_pack(g, BQ, 7);
+    const int64_t tiles = static_cast<int64_t>(ceil_div(static_cast<int64_t>(g.Sq) << pack, BQ)) * (g.group >> pack);
+    const int ks = tiles > 4 ? 8 : tiles > 2 ? 4 : static_cast<int>(tiles);
+    // (us, three launches and one: 2 x 205 queries, 3 heads on 1, 18 keys 11.0 and 8.3; 2 x 447,
+    // 2 heads, 16 keys 12.0 and 8.2; 7 x 474, 7 heads, 22 keys 16.8 and 12.5.  Clusters of four
+    // and eight in more than one round: 25 x 137, 12 on 6, 105 keys 25.5 and 29.5; 32 x 1024,
+    // 16 heads, 100 keys 147 and 180)
+    const int sms = sm_count() > 0 ? sm_count() : 148;
+    if (tiles <= 8 && (ks <= 2 || static_cast<int64_t>(ks) * (g.A / g.group) * B <= 2 * sms))
+      return cross_attention_bwd_short_tc(g, B, pack, ks, dctx, lse, dq, dk, dv, stream);
+  }
   const int packQ = best_pack(g, BQ), packK = best_pack(g, BQ2), hq = 1 << packQ, hk = 1 << packK;
   const int Akv = g.A / g.group, sms = sm_count() > 0 ? sm_count() : 148;
   const int q_tiles = ceil_div(static_cast<int64_t>(g.Sq) << packQ, BQ), k_tiles = ceil_div(g.Skv, BK2);

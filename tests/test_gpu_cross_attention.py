@@ -271,6 +271,19 @@ def test_columns_split_on_the_cuda_cores(sq, skv, heads, kv_heads, lens, dim, sh
     assert all(torch.equal(x.buf, y.buf) for x, y in zip(grads, c.backward(*c.given())))
 
 
+@pytest.mark.parametrize("sq,skv,heads,kv_heads,lens", [
+    (500, 100, 1, 1, [100, 0, 17]), (1024, 128, 2, 2, [128, 1]), (1000, 3, 3, 3, [3, 2, 0]), (40, 90, 6, 2, [90, 16]),
+    (70, 33, 12, 2, [33, 32, 0]), (5, 50, 24, 2, [50, 49]), (129, 128, 2, 1, [128, 127]), (300, 64, 4, 2, [64, 63, 1]),
+    (1025, 20, 1, 1, [20]), (1, 128, 320, 1, [128, 5]), (131, 77, 5, 1, [77, 0]), (640, 97, 2, 2, [97, 96]),
+])
+def test_few_keys_of_many_queries(sq, skv, heads, kv_heads, lens):
+    """One tile of keys and up to eight of queries, which add their parts; and more than that."""
+    c = Case(sq, skv, heads, kv_heads, lens, beside=8).poison()
+    grads = c.backward(*c.given())
+    c.check_backward(grads)
+    assert all(torch.equal(x.buf, y.buf) for x, y in zip(grads, c.backward(*c.given())))
+
+
 def test_forward_feeds_backward():
     """The library's own ctx and lse: within what the forward may be off more."""
     c = Case(150, 220, 6, 3, [220, 100, 0, 7]).poison()
