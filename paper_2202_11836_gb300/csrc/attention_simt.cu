@@ -194,8 +194,17 @@ struct Strides {
         k(SELF ? q : g.ldk), v(SELF ? q : g.ldv), o(SELF ? H : g.ldo) {}
 };
 
+// CTAs an SM that the registers are kept to: three of head dims above 64, whose shared memory
+// lets no more fit, four up to 64; up to 32 the compiler's own choice (80 registers) for self
+// attention and five for cross attention.  Three for all gave the compiler 141 to 154
+// registers, and many CTAs waited for a place (us, three and these): 8 x 512 tokens, 2 heads
+// of 64 88 and 56; 32 x 512, 8 of 32 615 and 506; 4 x 32, 2 of 64 3.6 and 3.7; 8 x 300 over
+// 512, 8 on 4 of 64 109 and 91, of 32 80 and 69.
+template <bool SELF, int G>
+constexpr int kFwdCtas = G > 16 ? 3 : G > 8 ? 4 : SELF ? 0 : 5;
+
 template <bool SELF, typename T, int G>
-__global__ void __launch_bounds__(F_THR, 3) attn_fwd_simt(const Geometry g, const T* __restrict__ gq,
+__global__ void __launch_bounds__(F_THR, kFwdCtas<SELF, G>) attn_fwd_simt(const Geometry g, const T* __restrict__ gq,
                                                           const T* __restrict__ gk, const T* __restrict__ gv,
                                                           const int32_t* __restrict__ lens, T* __restrict__ ctx,
                                                           float* __restrict__ lse) {
@@ -221,7 +230,8 @@ __global__ void __launch_bounds__(F_THR, 3) attn_fwd_simt(const Geometry g, cons
   float4 o[2][CC] = {};
   for (int k0 = 0; k0 < len; k0 += FC) {
     __syncthreads();
-#pragma unroll
+// (self attention batch by batch: 4 x 200 tokens, 6 heads of 128 52.9 us unrolled, 49.7 so)
+#pragma unroll (SELF ? 1 : ST::BATCHES)
     for (int h = 0; h < ST::BATCHES; ++h) {
       constexpr int R = ST::R;
       float4 kx[ST::PASSES], vx[ST::PASSES];
