@@ -322,9 +322,8 @@ __global__ void __launch_bounds__(NTHR, FwdShape<NS>::CTAS) attn_fwd_tc(const __
       mask_half(0);
       mx = half_max(0, mx) * sl2;
       if (j == 0) {
-        // (a split whose first keys' scores are all -inf adds nothing, as those keys
-        // would behind others)
-        m = KS > 1 ? fmaxf(mx, -FLT_MAX) : mx;
+        // (finite also where the first tile's scores are all -inf: those keys add nothing)
+        m = fmaxf(mx, -FLT_MAX);
       } else if (__any_sync(0xffffffffu, mx > m + kRescaleLog2)) {
         // O holds P_{j-1} V_{j-1} (one buffer: S_j was issued behind it)
         if (NS == 2) {
