@@ -2040,50 +2040,235 @@ sky_status attention_bwd_tc(const void* qkv, const void* dctx, const float* lse,
 
 // ------------------------------------------------------- cross attention
 namespace attn_tc {
-// delta[b, a, s] = sum over a head of dctx * ctx, for the dQ kernel, and the dK/dV
-// kernel's per-query rows [B][A >> pack][2][Sq << pack]: the log-sum-exp over c =
-// log2(e)/sqrt(D), then delta, negated and split as its comment says.  Eight lanes of 16
-// bytes a head.  (Two or four heads of loads in flight a lane were slower at every size but
-// the largest.)
-__global__ void __launch_bounds__(256) attn_delta_cross(const __nv_bfloat16* __restrict__ ctx,
-                                                        const __nv_bfloat16* __restrict__ dctx, int64_t ldo, int S,
-                                                        int A, int pack, int64_t heads, const float* __restrict__ lse,
-                                                        float* __restrict__ delta, uint4* __restrict__ xtab) {
-  pdl_wait();
-  pdl_trigger();
-  const int64_t i = (blockIdx.x * static_cast<int64_t>(blockDim.x) + threadIdx.x) >> 3;
-  if (i >= heads) return;  // (whole groups of eight lanes)
-  const int l = threadIdx.x & 7;
-  const int64_t row = i / A, b = row / S;
-  const int a = static_cast<int>(i - row * A), s = static_cast<int>(row - b * S);
-  const int64_t at = row * ldo + a * HD + l * 8;
-  const uint4 x = *reinterpret_cast<const uint4*>(ctx + at), y = *reinterpret_cast<const uint4*>(dctx + at);
-  const int64_t sidx = (b * A + a) * S + s;
-  const float lz = l == 0 ? lse[sidx] : 0.f;
-  const __nv_bfloat162* xs = reinterpret_cast<const __nv_bfloat162*>(&x);
-  const __nv_bfloat162* ys = reinterpret_cast<const __nv_bfloat162*>(&y);
-  float acc = 0.f;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 u = __bfloat1622float2(xs[e]), w = __bfloat1622float2(ys[e]);
-    acc += u.x * w.x + u.y * w.y;
+// delta[b, a, s] = sum over the keys of P dP, for the dQ kernel, and the dK/dV kernel's
+// per-query rows [B][A >> pack][2][Sq << pack]: the log-sum-exp over c = log2(e)/sqrt(D),
+// then delta, negated and split as its comment says.
+//
+// dot(dctx, ctx) is the same sum, but of a ctx rounded to bf16 it is off by up to 2^-9
+// sum |dctx ctx|, the same for every key of the row: that does not shrink with dS, and a
+// mean of V, which leaves the exact dq alone, makes it as large as one likes (V of mean 4
+// over 512 keys: dq off by 1.3e-2 of its norm).  So S and dP are formed here once more, two of
+// the five products, and the sum stays in 32 bits.
+//
+// One CTA per 128 query rows as in the dQ kernel, but nothing goes back.  Two forms, as of the
+// forward: two buffers of S and dP (NS = 2, 256 TMEM columns, two CTAs an SM, eight warps of
+// half a row a thread), so that the products of tile j + 1 run beside the exponentials of
+// tile j; or one, with a whole row a thread, and four CTAs an SM, for many CTAs, whose first
+// loads and last sums overlap then.  KS > 1: the CTAs of a cluster share a block's keys.
+template <int NS>
+struct DeltaShape {
+  static constexpr int STAGES = NS == 1 ? 1 : 3, SUMS = 128 * NS;  // K/V ring; threads that sum
+  static constexpr int THR = 64 + SUMS;                            // warp 0 TMA, warp 1 MMA issue
+  static constexpr int Q_OFF = 0, DO_OFF = Q_BYTES, KV_OFF = 2 * Q_BYTES;
+  static constexpr int BAR_OFF = KV_OFF + STAGES * 2 * KV_BYTES, RED_OFF = BAR_OFF + 256;
+  static constexpr int SMEM = RED_OFF + BQ * 8 + 1024;
+  static constexpr int CTAS = NS == 1 ? 4 : 2, TMEM_COLS = 128 * NS;
+  static_assert(CTAS * (SMEM + kSmemPerCta) <= kSmemPerSM);
+};
+static_assert(DeltaShape<2>::SMEM >= kSplitAttentionSmem, "clusters that hold 256 columns: see residency.h");
+
+struct DeltaParams {
+  int S, A, Skv, group, pack, packK;  // pack: of the tiles here; packK: of the rows for dK/dV
+  const int32_t* lens;
+  const float* lse;
+  float* delta;
+  uint4* xtab;
+  int32_t* status;
+  uint64_t timeout_ns;
+};
+
+__device__ __forceinline__ uint4 table_row(float v) {  // -v as [hi, lo, 0, ...] in bf16
+  const __nv_bfloat16 hi = __float2bfloat16_rn(-v);
+  const __nv_bfloat16 lo = __float2bfloat16_rn(-v - __bfloat162float(hi));
+  return make_uint4(static_cast<uint32_t>(__bfloat16_as_ushort(hi)) |
+                        (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16),
+                    0u, 0u, 0u);
+}
+
+template <int KS, int NS>
+__global__ void __launch_bounds__(DeltaShape<NS>::THR, DeltaShape<NS>::CTAS) attn_delta_cross(
+                                                              const __grid_constant__ CUtensorMap tmQ,
+                                                              const __grid_constant__ CUtensorMap tmK,
+                                                              const __grid_constant__ CUtensorMap tmV,
+                                                              const __grid_constant__ CUtensorMap tmO,
+                                                              const DeltaParams p) {
+  using SH = DeltaShape<NS>;
+  static_assert(KS == 1 || NS == 2);
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw_addr = ptx::smem_u32(smem_raw);
+  uint8_t* smem = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
+  uint64_t* qd_full = reinterpret_cast<uint64_t*>(smem + SH::BAR_OFF);
+  uint64_t* kv_full = qd_full + 1;
+  uint64_t* kv_empty = kv_full + SH::STAGES;
+  uint64_t* s_full = kv_empty + SH::STAGES;  // [NS] S_j, dP_j complete
+  uint64_t* s_free = s_full + NS;           // [NS] and read
+  uint64_t* done = s_free + NS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  float2* red = reinterpret_cast<float2*>(smem + SH::RED_OFF);  // of a row: both halves of its keys
+
+  const int pack = p.pack, S = p.S;
+  const int qt = blockIdx.x / KS, split = blockIdx.x % KS, a = blockIdx.y << pack, b = blockIdx.z;  // (first) head
+  const int q0 = qt * (BQ >> pack), kvh = a / p.group;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint64_t lim = p.timeout_ns;
+  if (threadIdx.x == 0) {
+    ptx::mbar_init(qd_full, 1);
+    for (int s = 0; s < SH::STAGES; ++s) {
+      ptx::mbar_init(&kv_full[s], 1);
+      ptx::mbar_init(&kv_empty[s], 1);
+    }
+    for (int s = 0; s < NS; ++s) {
+      ptx::mbar_init(&s_full[s], 1);
+      ptx::mbar_init(&s_free[s], SH::SUMS);
+    }
+    ptx::mbar_init(done, 1);
+    ptx::fence_mbar_init();
+    ptx::fence_proxy_async_smem();
+    ptx::prefetch_tensormap(&tmQ);
+    ptx::prefetch_tensormap(&tmO);
+    ptx::prefetch_tensormap(&tmK);
+    ptx::prefetch_tensormap(&tmV);
   }
-  const uint32_t mask = 0xffu << (threadIdx.x & 24);
+  if (warp == 1) {
+    ptx::tmem_alloc(tmem_slot, SH::TMEM_COLS);
+    ptx::tmem_relinquish();
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tmem_slot;  // S_j at 128 (j % NS), dP_j 64 columns behind
+  pdl_wait();
+  const int len = valid_keys(p.lens, b, 0, p.Skv, p.status);
+  const int n_all = (len + BKV - 1) / BKV, j0 = split * n_all / KS;
+  const int n_kt = (split + 1) * n_all / KS - j0;  // this CTA's key tiles
+
+  if (warp == 0) {
+    if (lane == 0) {
+      ptx::mbar_arrive_expect_tx(qd_full, 2 * Q_BYTES);
+      ptx::tma_load_4d(smem + SH::Q_OFF, &tmQ, qd_full, 0, a, q0, b);
+      ptx::tma_load_4d(smem + SH::DO_OFF, &tmO, qd_full, 0, a, q0, b);
+      int issued = 0;
+      for (int j = 0; j < n_kt; ++j) {
+        const int st = j % SH::STAGES;
+        if (!ptx::mbar_wait(&kv_empty[st], ((j / SH::STAGES) & 1) ^ 1u, lim, p.status, kWaitHint)) break;
+        uint8_t* kv = smem + SH::KV_OFF + st * 2 * KV_BYTES;
+        ptx::mbar_arrive_expect_tx(&kv_full[st], 2 * KV_BYTES);
+        ptx::tma_load_4d(kv, &tmK, &kv_full[st], 0, kvh, (j0 + j) * BKV, b);
+        ptx::tma_load_4d(kv + KV_BYTES, &tmV, &kv_full[st], 0, kvh, (j0 + j) * BKV, b);
+        ++issued;
+      }
+      // bounded waits for the copies still in flight
+      ptx::mbar_wait(qd_full, 0, lim, p.status, kWaitHint);
+      for (int j = issued - 1; j >= 0 && j >= issued - SH::STAGES; --j)
+        ptx::mbar_wait(&kv_full[j % SH::STAGES], (j / SH::STAGES) & 1, lim, p.status, kWaitHint);
+    }
+  } else if (warp == 1) {
+    constexpr uint32_t idS = ptx::idesc_bf16_f32(BQ, BKV, false, false);
+    const bool issuer = ptx::elect_one();
+    const uint64_t dq = ptx::smem_desc_sw128(ptx::smem_u32(smem + SH::Q_OFF), 16, 1024);
+    const uint64_t dd = ptx::smem_desc_sw128(ptx::smem_u32(smem + SH::DO_OFF), 16, 1024);
+    const uint64_t dk0 = ptx::smem_desc_sw128(ptx::smem_u32(smem + SH::KV_OFF), 16, 1024);
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, ptx::mbar_wait(bar, parity, lim, p.status, kWaitHint));
+    };
+    const bool ok = wait(qd_full, 0);
+    for (int j = 0; j < n_kt && ok; ++j) {
+      if (j >= NS && !wait(&s_free[j % NS], (j / NS - 1) & 1)) break;
+      if (!wait(&kv_full[j % SH::STAGES], (j / SH::STAGES) & 1)) break;
+      ptx::tc_fence_after();
+      if (issuer) {
+        const uint64_t dk = dk0 + static_cast<uint64_t>((j % SH::STAGES) * (2 * KV_BYTES >> 4));
+        const uint32_t tS = tmem + (j % NS) * 128;
 #pragma unroll
-  for (int o = 1; o < 8; o <<= 1) acc += __shfl_xor_sync(mask, acc, o);
-  if (l != 0) return;
-  delta[sidx] = acc;
-  auto row16 = [](float v) {  // -v as [hi, lo, 0, ...] in bf16
-    const __nv_bfloat16 hi = __float2bfloat16_rn(-v);
-    const __nv_bfloat16 lo = __float2bfloat16_rn(-v - __bfloat162float(hi));
-    return make_uint4(static_cast<uint32_t>(__bfloat16_as_ushort(hi)) |
-                          (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16),
-                      0u, 0u, 0u);
-  };
-  uint4* t = xtab + (b * (A >> pack) + (a >> pack)) * 2 * (static_cast<int64_t>(S) << pack) +
-             (static_cast<int64_t>(s) << pack) + (a & ((1 << pack) - 1));
-  t[0] = row16(__fdiv_rn(lz, LOG2E * 0.125f));
-  t[static_cast<int64_t>(S) << pack] = row16(acc);
+        for (int kk = 0; kk < HD / 16; ++kk) ptx::tc_mma_f16(tS, dq + kk * 2, dk + kk * 2, idS, kk > 0 ? 1u : 0u);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk)
+          ptx::tc_mma_f16(tS + 64, dd + kk * 2, dk + (KV_BYTES >> 4) + kk * 2, idS, kk > 0 ? 1u : 0u);
+        ptx::tc_commit(&s_full[j % NS]);
+        ptx::tc_commit(&kv_empty[j % SH::STAGES]);
+      }
+      __syncwarp();
+    }
+    if (issuer) ptx::tc_commit(done);
+    __syncwarp();
+    ptx::mbar_wait(done, 0, lim, p.status, kWaitHint);
+  } else {
+    const int q4 = warp & 3, hf = (warp - 2) >> 2;  // two buffers: keys [32 hf, 32 hf + 32) of a tile
+    const int r = q4 * 32 + lane;                   // query row = TMEM lane
+    const int q = q0 + (r >> pack), head = a + (r & ((1 << pack) - 1));
+    const uint32_t lane_base = static_cast<uint32_t>(q4 * 32) << 16;
+    const float sl2 = LOG2E * 0.125f;
+    const int64_t sidx = (static_cast<int64_t>(b) * p.A + head) * S + (q < S ? q : 0);
+    const float lz = q < S ? p.lse[sidx] : 0.f;
+    const uint64_t sc2 = pack2(sl2, sl2), nlse = pack2(-lz, -lz);
+    uint64_t acc[2] = {0, 0};  // pairs of zeros
+    for (int j = 0; j < n_kt; ++j) {
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&s_full[j % NS], (j / NS) & 1, lim, p.status, kWaitHint))) break;
+      ptx::tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < 3 - NS; ++c) {
+        const int key = NS == 2 ? hf * 32 : c * 32;
+        uint32_t sv[32], dv[32];
+        const uint32_t t = tmem + (j % NS) * 128 + lane_base + key;
+        ptx::tmem_ld_32x32b_x32(t, sv);
+        ptx::tmem_ld_32x32b_x32(t + 64, dv);
+        ptx::tmem_ld_wait();
+        if (c == 2 - NS) {
+          ptx::tc_fence_before();
+          ptx::mbar_arrive(&s_free[j % NS]);
+        }
+        const int left = len - (j0 + j) * BKV - key;  // valid keys of these
+        if (left < 32) {  // warp-uniform: only in the last tile; what lies behind may be anything
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i >= left) {
+              sv[i] = 0xff800000u;  // -inf: P = 0
+              dv[i] = 0u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+          const float2 x = unpack2(fma2(pack2(__uint_as_float(sv[i]), __uint_as_float(sv[i + 1])), sc2, nlse));
+          acc[(i >> 1) & 1] = fma2(pack2(ptx::ex2_ftz(x.x), ptx::ex2_ftz(x.y)),
+                                   pack2(__uint_as_float(dv[i]), __uint_as_float(dv[i + 1])), acc[(i >> 1) & 1]);
+        }
+      }
+    }
+    pdl_trigger();
+    const float2 sum = unpack2(add2(acc[0], acc[1]));
+    if (NS == 2) reinterpret_cast<float*>(red + r)[hf] = sum.x + sum.y;
+    else red[r] = sum;
+  }
+  ptx::tc_fence_before();
+  if constexpr (KS > 1) {
+    __syncwarp();
+    ptx::cluster_sync();  // every split's sums are where they are read from
+  } else {
+    __syncthreads();
+  }
+  if (warp == 1) {
+    ptx::tc_fence_after();
+    ptx::tmem_dealloc(tmem, SH::TMEM_COLS);
+  }
+  // This CTA's 128 / KS rows: the halves of every split, in order
+  constexpr int ROWS = BQ / KS;
+  const int t = static_cast<int>(threadIdx.x) - 64, r = split * ROWS + t, q = q0 + (r >> pack);
+  if (t >= 0 && t < ROWS && q < S) {
+    float d = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const float2 x = KS > 1 ? ptx::ld_cluster_f2(ptx::mapa_shared(ptx::smem_u32(red + r), s)) : red[r];
+      d += x.x + x.y;
+    }
+    const int head = a + (r & ((1 << pack) - 1));
+    const int64_t sidx = (static_cast<int64_t>(b) * p.A + head) * S + q, qrows = static_cast<int64_t>(S) << p.packK;
+    p.delta[sidx] = d;
+    uint4* row = p.xtab + (static_cast<int64_t>(b) * (p.A >> p.packK) + (head >> p.packK)) * 2 * qrows +
+                 (static_cast<int64_t>(q) << p.packK) + (head & ((1 << p.packK) - 1));
+    row[0] = table_row(__fdiv_rn(p.lse[sidx], LOG2E * 0.125f));
+    row[qrows] = table_row(d);
+  }
+  if constexpr (KS > 1) ptx::cluster_sync();  // the peers have read this CTA's sums
 }
 }  // namespace attn_tc
 
@@ -2157,8 +2342,8 @@ static sky_status cross_attention_bwd_short_tc(const attn::Geometry& g, int B, i
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "tensor-core cross attention backward launch");
 }
 
-sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ctx, const void* dctx, const float* lse,
-                                  void* dq, void* dk, void* dv, void* ws, cudaStream_t stream) {
+sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* dctx, const float* lse, void* dq, void* dk,
+                                  void* dv, void* ws, cudaStream_t stream) {
   using namespace attn_tc;
   if (g.Skv <= BQ) {
     const int pack = best_pack(g, BQ, 7);
@@ -2192,6 +2377,7 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ct
     return ks;
   };
   const int ksq = splits(q_ctas, q_steps, 5 * sms / 4, packQ), ksk = splits(k_ctas, k_steps, 2 * sms, 0);
+  const int ksd = splits(q_ctas, q_steps, 2 * sms, 0);  // delta
   CUtensorMap tq128, to128, tk64, tv64, tdq, tk128, tv128, tq64, to64, tdk, tdv;
   SKY_CHECK(cross_map(&tq128, g.q, g.A, g.Sq, B, g.ldq, hq, BQ >> packQ) &&
                 cross_map(&to128, dctx, g.A, g.Sq, B, g.ldo, hq, BQ >> packQ) &&
@@ -2204,10 +2390,6 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ct
             SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed for the cross attention backward operands");
   float* delta = static_cast<float*>(ws);
   uint4* xtab = reinterpret_cast<uint4*>(static_cast<char*>(ws) + cross_delta_bytes(g, B));
-  const int64_t heads = static_cast<int64_t>(B) * g.Sq * g.A;
-  cudaError_t e = launch_pdl(attn_delta_cross, dim3(ceil_div(heads, 32)), dim3(256), 0, stream, 1,
-                             static_cast<const __nv_bfloat16*>(ctx), static_cast<const __nv_bfloat16*>(dctx), g.ldo,
-                             g.Sq, g.A, packK, heads, lse, delta, xtab);
   BwdParams p{g.Sq, 0, g.A, g.lens, lse, delta, xtab, nullptr, nullptr, g.status, kTimeoutNs, {g.Skv, g.group, packK},
               static_cast<__nv_bfloat16*>(dk), static_cast<__nv_bfloat16*>(dv), g.ldk, g.ldv};
   const auto with = [](int ks, auto&& go) {
@@ -2216,6 +2398,18 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ct
            : ks == 4 ? go(std::integral_constant<int, 4>{})
                      : go(std::integral_constant<int, 8>{});
   };
+  const DeltaParams dp{g.Sq, g.A, g.Skv, g.group, packQ, packK, g.lens, lse, delta, xtab, g.status, kTimeoutNs};
+  const auto delta_by = [&](auto splits, auto bufs) {
+    constexpr int KS = decltype(splits)::value, NS = decltype(bufs)::value;
+    using SH = DeltaShape<NS>;
+    static OncePerDevice once;
+    const cudaError_t attr = allow_smem(once, attn_delta_cross<KS, NS>, SH::SMEM);
+    return attr != cudaSuccess ? attr
+                               : launch_pdl(attn_delta_cross<KS, NS>, dim3(q_tiles * KS, g.A >> packQ, B), dim3(SH::THR),
+                                            SH::SMEM, stream, KS, tq128, tk64, tv64, to128, dp);
+  };
+  cudaError_t e = q_ctas > 2 * sms ? delta_by(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{})
+                                   : with(ksd, [&](auto ks) { return delta_by(ks, std::integral_constant<int, 2>{}); });
   if (e == cudaSuccess)
     e = with(ksk, [&](auto ks) {
       constexpr int KS = decltype(ks)::value;

@@ -21,7 +21,7 @@ bool cross_attention_tc_fits(const attn::Geometry& g, std::initializer_list<cons
 sky_status cross_attention_fwd_tc(const attn::Geometry& g, int B, void* ctx, float* lse, cudaStream_t stream);
 // Scratch of the backward (16-byte aligned): delta, then the dK/dV kernel's per-query rows.
 size_t cross_attention_bwd_tc_ws(const attn::Geometry& g, int B);
-sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* ctx, const void* dctx, const float* lse,
-                                  void* dq, void* dk, void* dv, void* ws, cudaStream_t stream);
+sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* dctx, const float* lse, void* dq, void* dk,
+                                  void* dv, void* ws, cudaStream_t stream);
 
 }  // namespace sky

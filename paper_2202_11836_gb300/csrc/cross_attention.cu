@@ -72,8 +72,8 @@ sky_status forward(const sky_cross_shape& s, const attn::Geometry& g, void* ctx,
 template <typename T>
 sky_status backward(const sky_cross_shape& s, const attn::Geometry& g, const void* ctx, const void* dctx,
                     const float* lse, void* dq, void* dk, void* dv, void* ws, cudaStream_t st) {
-  if (std::is_same<T, __nv_bfloat16>::value && cross_attention_tc_fits(g, {g.q, g.k, g.v, ctx, dctx, dq, dk, dv}))
-    return cross_attention_bwd_tc(g, s.batch, ctx, dctx, lse, dq, dk, dv, ws, st);
+  if (std::is_same<T, __nv_bfloat16>::value && cross_attention_tc_fits(g, {g.q, g.k, g.v, dctx, dq, dk, dv}))
+    return cross_attention_bwd_tc(g, s.batch, dctx, lse, dq, dk, dv, ws, st);
   const cudaError_t e =
       attn::launch_bwd_simt(g, s.batch, static_cast<const T*>(ctx), static_cast<const T*>(dctx), lse,
                             static_cast<float*>(ws), static_cast<T*>(dq), static_cast<T*>(dk), static_cast<T*>(dv), st);

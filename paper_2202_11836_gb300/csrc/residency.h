@@ -7,8 +7,8 @@
 // holding what the other's peer needs on another SM, if the CTAs that fit an SM by
 // their shared memory could want more than its 512 columns.  So they must not
 // fit:
-//   the attention kernels where they are split over a cluster (the forward, dQ, dK/dV,
-//   the one-launch backward: 256 columns) take so much shared memory that two of their
+//   the attention kernels where they are split over a cluster (the forward, delta, dQ,
+//   dK/dV, the one-launch backward: 256 columns) take so much shared memory that two of their
 //   CTAs leave no room for a third or for a cluster product's;
 //   cluster products (at most 128 columns) take at least kClusterProductSmem.
 // (The persistent product takes a whole SM, and everything else that allocates
