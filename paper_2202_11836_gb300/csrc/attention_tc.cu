@@ -2180,10 +2180,10 @@ __global__ void __launch_bounds__(DeltaShape<NS>::THR, DeltaShape<NS>::CTAS) att
         const uint64_t dk = dk0 + static_cast<uint64_t>((j % SH::STAGES) * (2 * KV_BYTES >> 4));
         const uint32_t tS = tmem + (j % NS) * 128;
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) ptx::tc_mma_f16(tS, dq + kk * 2, dk + kk * 2, idS, kk > 0 ? 1u : 0u);
-#pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk)
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          ptx::tc_mma_f16(tS, dq + kk * 2, dk + kk * 2, idS, kk > 0 ? 1u : 0u);
           ptx::tc_mma_f16(tS + 64, dd + kk * 2, dk + (KV_BYTES >> 4) + kk * 2, idS, kk > 0 ? 1u : 0u);
+        }
         ptx::tc_commit(&s_full[j % NS]);
         ptx::tc_commit(&kv_empty[j % SH::STAGES]);
       }
