@@ -1088,10 +1088,11 @@ constexpr int KV_Q_OFF = 2 * KV2_BYTES;
 constexpr int KV_O_OFF = KV_Q_OFF + KV_STAGES * QO2_BYTES;
 // The per-query terms enter the score products as one more K = 16 step:
 // S^T - lse2 / c = [K | E] [Q | X_lse]^T and dP^T - delta = [V | E] [dO | X_delta]^T,
-// with c = log2(e)/sqrt(D), E the 128 x 16 matrix whose first two columns are
-// ones, and X the 64 x 16 per-tile matrix whose first two columns hold the
-// negated term split into a bf16 high part and a bf16 low part (exact to
-// about 2^-17 relative).  The softmax threads then need no per-query loads.
+// with c = log2(e)/sqrt(D), E the 128 x 16 matrix whose first three columns are
+// ones, and X the 64 x 16 per-tile matrix whose first columns hold the negated
+// term split into bf16 parts: two of self attention's (exact to about 2^-17
+// relative), three of cross attention's (2^-25; what two lose is 1% of P where the
+// log-sum-exp is 2000).  The softmax threads then need no per-query loads.
 // E and X are K-major without swizzling, built from 8-row x 16-byte core
 // matrices: a row's K columns 0..7 are 16 contiguous bytes (row groups 128
 // bytes apart), and columns 8..15, all zero, come from one shared zero block
@@ -1196,10 +1197,10 @@ __global__ void __maxnreg__(80) attn_bwd_dkdv_tc(const __grid_constant__ CUtenso
     ptx::tmem_alloc(tmem_slot, 256);
     ptx::tmem_relinquish();
   }
-  // E: rows [1, 1, 0 x 6] (bf16); the X ring and the zero block: zeros
+  // E: rows [1, 1, 1, 0 x 5] (bf16); the X ring and the zero block: zeros
   for (int w = threadIdx.x; w < (KV_RED_OFF - KV_E_OFF) / 16; w += NTHR_B)
     *reinterpret_cast<uint4*>(smem + KV_E_OFF + w * 16) =
-        make_uint4(w < BK2 ? 0x3F803F80u : 0u, 0u, 0u, 0u);
+        make_uint4(w < BK2 ? 0x3F803F80u : 0u, w < BK2 ? 0x3F80u : 0u, 0u, 0u);
   ptx::fence_proxy_async_smem();
   ptx::tc_fence_before();
   __syncthreads();
@@ -2077,12 +2078,13 @@ struct DeltaParams {
   uint64_t timeout_ns;
 };
 
-__device__ __forceinline__ uint4 table_row(float v) {  // -v as [hi, lo, 0, ...] in bf16
+__device__ __forceinline__ uint4 table_row(float v) {  // -v as [hi, mid, lo, 0, ...] in bf16
   const __nv_bfloat16 hi = __float2bfloat16_rn(-v);
-  const __nv_bfloat16 lo = __float2bfloat16_rn(-v - __bfloat162float(hi));
+  const float rest = -v - __bfloat162float(hi);
+  const __nv_bfloat16 mid = __float2bfloat16_rn(rest), lo = __float2bfloat16_rn(rest - __bfloat162float(mid));
   return make_uint4(static_cast<uint32_t>(__bfloat16_as_ushort(hi)) |
-                        (static_cast<uint32_t>(__bfloat16_as_ushort(lo)) << 16),
-                    0u, 0u, 0u);
+                        (static_cast<uint32_t>(__bfloat16_as_ushort(mid)) << 16),
+                    __bfloat16_as_ushort(lo), 0u, 0u);
 }
 
 template <int KS, int NS>

@@ -80,3 +80,35 @@ def test_mean_of_v_and_peaked_scores(sq, skv, heads, kv_heads, lens, mean, scale
 @pytest.mark.parametrize("B,sq,skv,heads,kv_heads", [(3, 20, 2000, 16, 4), (1, 5, 3000, 2, 1), (2, 129, 500, 3, 1)])
 def test_keys_of_few_rows(B, sq, skv, heads, kv_heads):
     check(Case(sq, skv, heads, kv_heads, [skv - 61 * b for b in range(B)]).poison(), 2)
+
+
+@pytest.mark.parametrize("sq,skv,heads,kv_heads,lens", [(200, 300, 2, 2, [300, 129]), (90, 700, 3, 1, [700]),
+                                                        (1100, 120, 1, 1, [120])])
+def test_scores_in_the_thousands(sq, skv, heads, kv_heads, lens):
+    """Rows that one key takes whole, at scores up to 3100: P is 1 there, as far as dV has the
+    log-sum-exp.
+
+    A head's first value is in q an integer from 32 to 63, in k a multiple of 8 up to 384, of the
+    last key 392; its second in q a multiple of 1/16 below 8, in k 1; the others are 0.  So the
+    scores are exact, of 19 bits, and every other at least 32 below the last key's, P there
+    below e^-32.  That key's P is off by the log-sum-exp's rounding and the accumulator's, 3 x 2^-24
+    of it, times ln 2, less than the half step 2^-9 below 1 (asserted), so it rounds to 1: dv is a
+    sum of dctx rounded once.  (With the log-sum-exp to 2^-18 P would be off by 0.6 to 1.2e-2.)"""
+    c = Case(sq, skv, heads, kv_heads, lens)
+    g = np.random.default_rng(sq)
+    q, k = np.zeros(c.q.get().shape, np.float32), np.zeros(c.k.get().shape, np.float32)
+    q[..., 0] = g.integers(32, 64, q.shape[:-1])
+    q[..., 1] = g.integers(0, 128, q.shape[:-1]) / 16
+    k[..., 0], k[..., 1] = (np.arange(skv) % 49 * 8)[None, :, None], 1
+    for b, n in enumerate(lens):
+        k[b, n - 1, :, 0] = 392
+    c.q.set(q)
+    c.k.set(k)
+    qq, kk, vv, dd = c.inputs()
+    _, z = ORC.cross_attention(qq, kk, vv, lens)
+    assert np.log(2.0) * 3 * U * np.abs(z).max() + 2.0 ** -21 < 2.0 ** -9
+    want = ORC.cross_attention_backward(qq, kk, vv, dd, lens)[2]
+    rows = sq * (heads // kv_heads)
+    most = np.abs(dd).sum(1).reshape(len(lens), kv_heads, -1, c.dim).sum(2)[:, None]
+    off = np.abs(f64(c.backward(*c.given())[2].get()) - want)
+    assert (off <= H * np.abs(want) + ((rows + 8) * U + np.exp(-30.0)) * most).all(), off.max()
