@@ -14,7 +14,8 @@
 namespace sky {
 namespace attn {
 
-// delta[b, a, s] = sum_d dctx * ctx: one warp per (row, head), rows of ldo.
+// delta[b, a, s] = sum_d dctx * ctx: one warp per (row, head), rows of ldo.  (fp32; bf16:
+// attn_delta_keys)
 template <typename T>
 __global__ void attn_delta(const T* __restrict__ ctx, const T* __restrict__ dctx, int S, int64_t ldo,
                            int A, int D, int64_t rows, float* __restrict__ delta) {
@@ -466,10 +467,93 @@ __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geo
   ptx::cluster_sync();  // the peers have read this CTA's part
 }
 
+// delta of bf16 storage: the sum over the keys of P dP.  dot(dctx, ctx) is the same sum, but of
+// a rounded ctx it is off by up to 2^-9 sum |dctx ctx|, the same for every key of the row,
+// which a mean of V makes larger than dS.  Own rows are queries, columns keys, as for dQ; the
+// CTAs of a cluster share a block's columns.  Two of the backward's seven products once more
+// (us, from the rounded ctx and this): 4 x 200 over 333, 8 heads on 2 of 128 210 and 264; 8 x
+// 300 over 512, 8 on 4 of 32 265 and 320; 10 over 3000, 4 on 1 of 128 61 and 96.
+template <typename T, int G>
+__global__ void __launch_bounds__(F_THR, G > 16 ? 2 : 4) attn_delta_keys(const Geometry g, const T* __restrict__ gq,
+                                                                         const T* __restrict__ gk, const T* __restrict__ gv,
+                                                                         const int32_t* __restrict__ lens,
+                                                                         const T* __restrict__ dctx,
+                                                                         const float* __restrict__ lse,
+                                                                         float* __restrict__ delta, int splits) {
+  using ST = Stage<G>;
+  pdl_wait();
+  extern __shared__ __align__(16) float sm[];
+  const int LD = g.LD, D = g.D, Sq = g.Sq;
+  float *r0s = sm, *r1s = r0s + FR * LD, *c0s = r1s + FR * LD, *c1s = c0s + FC * LD, *part = c1s + FC * LD;
+  const int tiles = (Sq + FR - 1) / FR, split = static_cast<int>(blockIdx.x) % splits, x = static_cast<int>(blockIdx.x) / splits;
+  const int a = x / tiles, q0 = (x % tiles) * FR, b = blockIdx.y, kv = a / g.group;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int len = valid_keys(lens, b, 0, g.Skv, g.status);
+  const T* q = gq + static_cast<int64_t>(b) * Sq * g.ldq + a * D;
+  const T* dO = dctx + static_cast<int64_t>(b) * Sq * g.ldo + a * D;
+  const T* k = gk + static_cast<int64_t>(b) * g.Skv * g.ldk + kv * D;
+  const T* v = gv + static_cast<int64_t>(b) * g.Skv * g.ldv + kv * D;
+  const int64_t at = (static_cast<int64_t>(b) * g.A + a) * Sq;
+  const float sl2 = 1.f / sqrtf((float)D) * 1.4426950408889634f;
+  const int all = (len + FC - 1) / FC, begin = split * all / splits, end = (split + 1) * all / splits;
+  float lr[2], d[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) lr[i] = lse[at + min(q0 + 2 * ty + i, Sq - 1)];
+  if (begin < end) {
+    float4 own0[ST::OWN], own1[ST::OWN];
+    load_rows<G>(q, g.ldq, q0, Sq, D, g.vec, own0);
+    load_rows<G>(dO, g.ldo, q0, Sq, D, g.vec, own1);
+    put_rows<G>(r0s, LD, D, own0);
+    put_rows<G>(r1s, LD, D, own1);
+  }
+  for (int c0 = begin * FC; c0 < end * FC; c0 += FC) {
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < ST::BATCHES; ++t) {
+      constexpr int R = ST::R;
+      float4 v0[ST::PASSES], v1[ST::PASSES];
+      load_rows<G>(k, g.ldk, c0 + R * t, len, D, g.vec, v0);
+      load_rows<G>(v, g.ldv, c0 + R * t, len, D, g.vec, v1);
+      put_rows<G>(c0s + R * t * LD, LD, D, v0);
+      put_rows<G>(c1s + R * t * LD, LD, D, v1);
+    }
+    __syncthreads();
+    float s[2][4], dp[2][4];
+    scores(r0s, c0s, LD, D, s);
+    scores(r1s, c1s, LD, D, dp);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        if (c0 + tx + 16 * c < len) d[i] = fmaf(exp2f(fmaf(s[i][c], sl2, -lr[i])), dp[i][c], d[i]);
+  }
+  pdl_trigger();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    d[i] = half_warp_sum(d[i]);
+    if (tx == 0) part[2 * ty + i] = d[i];
+  }
+  if (splits > 1) ptx::cluster_sync();
+  else __syncthreads();
+  const int r = 2 * static_cast<int>(threadIdx.x);
+  if (split == 0 && r < FR) {  // two rows a thread, in split order
+    float2 sum = *reinterpret_cast<const float2*>(part + r);
+    for (int c = 1; c < splits; ++c) {
+      const float2 w = ptx::ld_cluster_f2(ptx::mapa_shared(ptx::smem_u32(part + r), c));
+      sum.x += w.x;
+      sum.y += w.y;
+    }
+    if (q0 + r < Sq) delta[at + q0 + r] = sum.x;
+    if (q0 + r + 1 < Sq) delta[at + q0 + r + 1] = sum.y;
+  }
+  if (splits > 1) ptx::cluster_sync();  // the first CTA has read the sums
+}
+
 // Launch shape: the shared row stride (four floats past the head dim, so the 16 lanes of
 // a score product read different banks) and the bytes it makes.
 constexpr int row_stride(int D) { return (D + 3) / 4 * 4 + 4; }
 constexpr int fwd_smem(int D) { return ((FR + 2 * FC) * row_stride(D) + FR * FP_LD) * 4; }
+constexpr int delta_smem(int D) { return ((2 * FR + 2 * FC) * row_stride(D) + FR) * 4; }
 constexpr int bwd_smem(int D, int NC) {
   return ((2 * FR + 32 * NC) * row_stride(D) + 2 * FR * (16 * NC + 4) + 32 * NC) * 4;
 }
@@ -529,16 +613,40 @@ Splits bwd_splits(const Geometry& g, int B, unsigned* blocks) {
   return sp;
 }
 
+// A block's keys over a cluster while the CTAs all fit at once and each keeps two tiles.
+template <typename T>
+cudaError_t delta_keys(const Geometry& g, int B, const T* dctx, const float* lse, float* delta, cudaStream_t stream) {
+  const int64_t blocks = static_cast<int64_t>(ceil_div(g.Sq, FR)) * g.A;
+  const int64_t room = static_cast<int64_t>(sm_count() > 0 ? sm_count() : 148) * (g.D > 64 ? 2 : 4);
+  int ks = 1;
+  while (ks < 8 && 2 * ks * blocks * B <= room && ceil_div(g.Skv, FC) >= 4 * ks) ks *= 2;
+  const auto go = [&](auto group) {
+    constexpr int G = decltype(group)::value;
+    static OncePerDevice once;
+    const cudaError_t e = allow_smem(once, attn_delta_keys<T, G>, delta_smem(4 * G));
+    if (e != cudaSuccess) return e;
+    return launch_pdl(attn_delta_keys<T, G>, dim3(static_cast<unsigned>(blocks * ks), B), dim3(F_THR), delta_smem(g.D),
+                      stream, ks, g, static_cast<const T*>(g.q), static_cast<const T*>(g.k), static_cast<const T*>(g.v),
+                      g.lens, dctx, lse, delta, ks);
+  };
+  return g.D <= 32 ? go(Group<8>{}) : g.D <= 64 ? go(Group<16>{}) : go(Group<32>{});
+}
+
 template <bool SELF, typename T>
 cudaError_t bwd_simt(Geometry g, int B, const T* ctx, const T* dctx, const float* lse, float* delta, T* dq, T* dk,
                      T* dv, cudaStream_t stream) {
-  const int64_t rows = static_cast<int64_t>(B) * g.Sq;
-  const cudaError_t le = launch_pdl(attn_delta<T>, dim3(ceil_div(rows * g.A * 32, 256)), dim3(256), 0, stream, 1, ctx,
-                                    dctx, g.Sq, g.ldo, g.A, g.D, rows, delta);
-  count_launches(2);
-  if (le != cudaSuccess) return le;
   g.LD = row_stride(g.D);
   g.vec = rows_of_4<T>(g, dctx, dq, dk, dv);
+  cudaError_t le;
+  if constexpr (std::is_same<T, float>::value) {
+    const int64_t rows = static_cast<int64_t>(B) * g.Sq;
+    le = launch_pdl(attn_delta<T>, dim3(ceil_div(rows * g.A * 32, 256)), dim3(256), 0, stream, 1, ctx, dctx, g.Sq, g.ldo,
+                    g.A, g.D, rows, delta);
+  } else {
+    le = delta_keys(g, B, dctx, lse, delta, stream);
+  }
+  count_launches(2);
+  if (le != cudaSuccess) return le;
   Splits sp{1, false, {true, true}};
   unsigned blocks = (unsigned)ceil_div(g.Sq, FR) * g.A + (unsigned)ceil_div(g.Skv, FR) * (g.A / g.group);
   if (!SELF) sp = bwd_splits(g, B, &blocks);

@@ -82,6 +82,15 @@ def test_keys_of_few_rows(B, sq, skv, heads, kv_heads):
     check(Case(sq, skv, heads, kv_heads, [skv - 61 * b for b in range(B)]).poison(), 2)
 
 
+@pytest.mark.parametrize("mean", [0, 4])
+@pytest.mark.parametrize("sq,skv,heads,kv_heads,lens,dim,shift", [
+    (64, 300, 4, 2, [300, 129, 0], 128, 0), (37, 200, 3, 3, [200, 1], 64, 1), (130, 90, 2, 1, [90, 64], 32, 0),
+    (9, 1500, 2, 1, [1500, 65, 7], 80, 0), (16, 16, 4, 4, [16, 3], 33, 1), (3, 3000, 1, 1, [2999], 20, 0),
+])
+def test_mean_of_v_on_the_cuda_cores(sq, skv, heads, kv_heads, lens, dim, shift, mean):
+    check(Case(sq, skv, heads, kv_heads, lens, dim=dim, beside=shift, shift=shift).poison(), mean)
+
+
 @pytest.mark.parametrize("sq,skv,heads,kv_heads,lens", [(200, 300, 2, 2, [300, 129]), (90, 700, 3, 1, [700]),
                                                         (1100, 120, 1, 1, [120])])
 def test_scores_in_the_thousands(sq, skv, heads, kv_heads, lens):
