@@ -54,9 +54,12 @@ attn::Geometry geometry(const sky_cross_shape& s, const void* q, const void* k, 
           s.head_dim, 0, false, len, status};
 }
 
-// The most that any choice of kernels takes: pointers, which it depends on, are not known.
+// delta, 4 bytes a row and head, and where the shape allows the tensor-core kernels (the
+// pointers, which may rule them out still, are not known) their table rows, 32 more.
 size_t workspace(const sky_cross_shape& s) {
-  return cross_attention_bwd_tc_ws(geometry(s, nullptr, nullptr, nullptr, nullptr, nullptr), s.batch);
+  const attn::Geometry g = geometry(s, nullptr, nullptr, nullptr, nullptr, nullptr);
+  if (s.dtype == SKY_DTYPE_BF16 && cross_attention_tc_fits(g, {})) return cross_attention_bwd_tc_ws(g, s.batch);
+  return (static_cast<size_t>(s.batch) * s.heads * s.q_len * sizeof(float) + 15) & ~size_t{15};
 }
 
 template <typename T>
