@@ -181,7 +181,8 @@ typedef struct {
  * the rotation by the row's position d_pos[row] (int32[rows], any value; may be
  * NULL without a rotation).  Statistics, angles and products are fp32 or finer;
  * angles keep their precision at every position.  A head whose sum of squares
- * leaves fp32's range comes out as zeros, a head of zeros with eps = 0 as NaN.
+ * overflows fp32 comes out as zeros; with eps = 0 one whose sum is 0 in fp32 (values
+ * below about 1e-23) comes out infinite or NaN, as a head of zeros does.
  * y may be x where ldy == ldx, and must not overlap it otherwise.  Serves a batch
  * of new tokens (a row each) as it does a training batch.
  * Errors: INVALID_ARG (null, sizes, an unknown dtype or rotation, rows shorter

@@ -54,7 +54,8 @@ Params params(const sky_qk_norm_shape& s, const void* q_gain, const void* k_gain
       if (i > 0 && i % 16 == 0) coarse = std::pow(s.theta, -2.0 * i / s.head_dim);
       const double f = coarse * fine[i % 16] / 6.283185307179586476925;
       double whole;  // (whole turns a position change nothing; they arise for theta < 1)
-      p.turn[i] = static_cast<uint64_t>(std::modf(f, &whole) * 18446744073709551616.0);
+      // (to nearest; below 1 a double is at most 1 - 2^-53, so 2^64 is never reached)
+      p.turn[i] = static_cast<uint64_t>(std::nearbyint(std::modf(f, &whole) * 18446744073709551616.0));
     }
   }
   return p;

@@ -27,7 +27,8 @@
 // Angles.  pos * frequency in fp32 is off by whole turns' fractions at far positions
 // (2^-24 of 10^6 radians is 0.06).  So the host gives each frequency as a fraction of a
 // turn in 64-bit fixed point, and pos * F modulo 2^64 is the turned fraction exactly, up
-// to |pos| 2^-65 of a turn and what the double on the host lost.  Its top 32 bits, as a
+// to |pos| 2^-65 of a turn and what the doubles on the host lost, a few 2^-53 of the
+// frequency: 2^-50 |pos| radians in all.  Its top 32 bits, as a
 // signed fraction, go to sincospif.  Lane i computes angles i, i + 32, ... of the token
 // once for all heads of the warp, and they are shared through shared memory.
 #pragma once
