@@ -1,12 +1,13 @@
 """Every form of the cross attention forward, chosen by the sizes that choose it: two
 score buffers, one, one for keys of a single tile, keys split over two and four CTAs, few
-rows on the tensor cores and on the CUDA cores, 16-row blocks there.  Bounds and layout
-are those of test_gpu_cross_attention.
+rows on the tensor cores and on the CUDA cores, 16-row blocks there; rows whose offsets pass
+2^31 values; calls on several streams and threads at once.  Bounds and layout are those of
+test_gpu_cross_attention.
 """
-import numpy as np
+import threading
+
 import pytest
 
-from oracle import heads_f64 as ORC
 from paper_2202_11836_gb300 import _lib as L
 from test_gpu_cross_attention import Case, P, stream
 
@@ -31,6 +32,105 @@ FORMS = {
     "few rows, CUDA cores": (2, 700, 6, 2, [700, 65, 129], "fp32"),
     "CUDA cores": (150, 200, 4, 2, [200, 65, 130], "fp32"),
 }
+
+
+# lengths that leave splits without a tile, end a tile, and are 0 and 1, by form
+RAGGED = {
+    "two buffers": [0, 1, 64, 300], "one buffer": [200, 0, 1, 63, 64, 65, 128, 191, 192],
+    "one buffer, four heads a tile": [0, 200, 1, 63, 64, 65, 127, 128, 129, 2, 130],
+    "four splits": [945, 0, 1, 64, 65, 128], "four splits, whole heads": [0, 800, 65],
+    "two splits": [1600, 0, 1, 64, 65, 128, 1599, 700, 63, 1], "two splits, two heads a tile": [0, 1600, 1, 64, 63, 65, 127, 129, 999, 2],
+    "few rows": [0, 2500, 1, 32, 33], "few rows, 32": [2100, 0, 1], "few rows, CUDA cores": [1, 0, 700],
+    "CUDA cores": [0, 1, 200],
+}
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_ragged_lengths_with_anything_behind(form):
+    sq, skv, heads, kv_heads, _, dtype = FORMS[form]
+    c = Case(sq, skv, heads, kv_heads, RAGGED[form], dtype=dtype, beside=8).poison()
+    ctx, lse = c.forward()
+    c.check_forward(ctx, lse)
+    again, lse2 = c.forward()
+    assert torch.equal(ctx.buf, again.buf) and torch.equal(lse, lse2)
+    assert torch.equal(c.forward(with_lse=False)[0].buf, ctx.buf)
+
+
+@pytest.mark.parametrize("heads,kv_heads,B", [(16, 16, 9), (32, 8, 11)])
+def test_keys_of_one_tile_under_many_blocks(heads, kv_heads, B):
+    """One buffer by its own rule: a single tile of keys and more than two blocks an SM."""
+    c = Case(300 if heads == 16 else 150, 40, heads, kv_heads, [40, 0, 1, 39, 33, 32, 31, 40, 2, 17, 40][:B], beside=8).poison()
+    ctx, lse = c.forward()
+    c.check_forward(ctx, lse)
+
+
+@pytest.mark.parametrize("sq,skv,heads,kv_heads,lens,dim,shift,apart", [
+    (6, 7, 2, 2, [7, 5], 64, 0, 3 << 26),     # few rows; one launch backward
+    (6, 7, 2, 1, [7, 5], 64, 1, 3 << 26),     # CUDA cores
+    (20, 135, 1, 1, [130], 64, 0, 1 << 24),   # tiles; three launches backward
+    (9, 135, 1, 1, [135], 32, 0, 1 << 24),    # CUDA cores, 16-row blocks
+])
+def test_rows_past_32_bit_offsets(sq, skv, heads, kv_heads, lens, dim, shift, apart):
+    c = Case(sq, skv, heads, kv_heads, lens, dim=dim, beside=apart, shift=shift)
+    assert (len(lens) * max(sq, skv) - 1) * min(c.ld) > 1 << 31
+    near = Case(sq, skv, heads, kv_heads, lens, dim=dim, beside=8 if shift == 0 else 1, shift=shift)
+    for x in ("q", "k", "v", "dctx"):
+        getattr(near, x).set(getattr(c, x).get().contiguous())
+
+    def alike(x, y):
+        return torch.equal(x.get(), y.get()) and x.untouched()
+    (ctx, lse), (want, want_lse) = c.forward(), near.forward()
+    assert alike(ctx, want) and torch.equal(lse, want_lse)
+    for got, ref in zip(c.backward(ctx, lse), near.backward(want, want_lse)):
+        assert alike(got, ref)
+    near.check_forward(want, want_lse)
+
+
+@pytest.mark.parametrize("threads", [False, True])
+def test_calls_at_once(threads):
+    """Forwards and backwards of every kind on six streams, a workspace each, from one thread
+    or from six: the bits of calls made alone."""
+    shapes = [(40, 945, 6, 3, [945, 300], "bf16", 64), (300, 200, 16, 16, [200, 65, 128], "bf16", 64),
+              (1, 2500, 8, 2, [2500, 65], "bf16", 64), (700, 100, 8, 2, [100, 64], "bf16", 64),
+              (50, 340, 2, 2, [340, 65], "fp32", 64), (33, 150, 4, 2, [150, 80], "bf16", 128)]
+    cases = [Case(*s[:5], dtype=s[5], dim=s[6]) for s in shapes]
+    alone = []
+    for c in cases:
+        ctx, lse = c.forward()
+        alone.append((ctx, lse, c.backward(ctx, lse)))
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [(c.new["ctx"](), torch.empty_like(a[1]), [c.new[n]() for n in ("dq", "dk", "dv")],
+             torch.empty(L.lib().sky_cross_attention_bwd_workspace_bytes(c.shape), dtype=torch.uint8, device="cuda"))
+            for c, a in zip(cases, alone)]
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(i, rounds):
+        try:
+            torch.cuda.set_device(0)
+            c, (ctx, lse, grads, ws), st = cases[i], outs[i], streams[i].cuda_stream
+            for _ in range(rounds):
+                L.call("sky_cross_attention_fwd", c.shape, c.q.ptr(), c.k.ptr(), c.v.ptr(), P(c.d_len), ctx.ptr(), P(lse),
+                       None, st)
+                L.call("sky_cross_attention_bwd", c.shape, c.q.ptr(), c.k.ptr(), c.v.ptr(), ctx.ptr(), c.dctx.ptr(), P(lse),
+                       P(c.d_len), *[g.ptr() for g in grads], P(ws), ws.numel(), None, st)
+        except Exception as e:  # noqa: BLE001  (of another thread: told below)
+            failed.append(e)
+    if threads:
+        ts = [threading.Thread(target=work, args=(i, 20)) for i in range(len(cases))]
+        for t in ts:
+            t.start()
+        for t in ts:
+            t.join()
+    else:
+        for _ in range(20):
+            for i in range(len(cases)):
+                work(i, 1)
+    torch.cuda.synchronize()
+    assert not failed
+    for (ctx, lse, grads), (c2, l2, g2, _) in zip(alone, outs):
+        assert torch.equal(ctx.buf, c2.buf) and torch.equal(lse, l2)
+        assert all(torch.equal(x.buf, y.buf) for x, y in zip(grads, g2))
 
 
 @pytest.mark.parametrize("form", FORMS)
