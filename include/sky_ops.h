@@ -124,7 +124,9 @@ typedef struct {
  * computed once and kept, kv_len being the room that they have.
  * bf16 with head_dim 64 and every tensor and row distance on the 16-byte grid
  * runs on the tensor cores; other head dims, up to 128, and other alignments run
- * slower kernels of the same result.
+ * slower kernels, whose products are fp32 throughout.  The tensor cores take P as a
+ * bf16 operand: ctx is then off by what its own rounding and P's are, 2.2e-3 of its
+ * norm where one rounding is 1.7e-3; lse stays fp32.
  * ctx may not overlap q, k or v.
  * Errors: INVALID_ARG (null, sizes, heads no multiple of kv_heads, rows shorter
  * than their heads, an argument off its type's grid), UNSUPPORTED (head_dim above
@@ -146,8 +148,9 @@ size_t sky_cross_attention_bwd_workspace_bytes(const sky_cross_shape* shape);
  * memory: dk and dv may be blocks of the same rows), and calls that may overlap
  * on the GPU need a workspace each.
  * bf16 on the tensor cores takes P and dS as bf16 operands, as sky_attention_bwd
- * does, and where keys or queries are many dot(dctx, ctx) from the bf16 ctx: dq
- * and dk come out 1.3 to 2 times the error of one rounding.
+ * does: gradients are off by what their own rounding and the operands' are, about
+ * 1.4 times one rounding.  dot(dctx, ctx) is formed for bf16 from P and dctx v^T in
+ * 32 bits (only fp32 reads ctx), so a mean of v or peaked scores do not add to that.
  * Errors as the forward's; INVALID_ARG for a workspace that is too small or not
  * 16-byte aligned. */
 sky_status sky_cross_attention_bwd(const sky_cross_shape* shape, const void* q, const void* k,

@@ -36,7 +36,7 @@ __device__ __forceinline__ int valid_keys(const int32_t* lens, int b, int least,
 // T: float or __nv_bfloat16.  lse may be null.
 template <typename T>
 cudaError_t launch_fwd_simt(const Geometry& g, int B, T* ctx, float* lse, cudaStream_t stream);
-// delta: [B][A][Sq] floats of scratch.
+// delta: [B][A][Sq] floats of scratch.  ctx: read for fp32 only.
 template <typename T>
 cudaError_t launch_bwd_simt(const Geometry& g, int B, const T* ctx, const T* dctx, const float* lse, float* delta, T* dq,
                             T* dk, T* dv, cudaStream_t stream);

@@ -705,7 +705,7 @@ struct BwdParams {
   const int32_t* lens;
   const float* lse;
   const float* delta;
-  const uint4* xtab;  // dK/dV per-query rows: [B*A][2][S] x 16 bytes (attn_delta_bf16)
+  const uint4* xtab;  // dK/dV per-query rows: [B*A][2][S] x 16 bytes (the delta pre-passes)
   __nv_bfloat16* dqkv;
   // optional: column sums of the stored dQKV, one row per 128-row tile of a
   // sequence: colpart[b * ceil(S/128) + tile][3H]
@@ -2379,7 +2379,10 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* dc
     return ks;
   };
   const int ksq = splits(q_ctas, q_steps, 5 * sms / 4, packQ), ksk = splits(k_ctas, k_steps, 2 * sms, 0);
-  const int ksd = splits(q_ctas, q_steps, 2 * sms, 0);  // delta
+  // delta as dQ, of whose rows it stores none.  us, unsplit and split: 40 queries, 12 on 4, 945
+  // keys 14.9 and 11.9; 20, 2 heads, 1219 keys 16.1 and 11.1; 4 x 256, 4 heads, 1770 keys 27.6
+  // and 21.5; up to two CTAs an SM: 4 x 256, 16 heads, 512 keys 20.8 and 21.3.
+  const int ksd = splits(q_ctas, q_steps, 5 * sms / 4, 0);
   CUtensorMap tq128, to128, tk64, tv64, tdq, tk128, tv128, tq64, to64, tdk, tdv;
   SKY_CHECK(cross_map(&tq128, g.q, g.A, g.Sq, B, g.ldq, hq, BQ >> packQ) &&
                 cross_map(&to128, dctx, g.A, g.Sq, B, g.ldo, hq, BQ >> packQ) &&
@@ -2410,6 +2413,10 @@ sky_status cross_attention_bwd_tc(const attn::Geometry& g, int B, const void* dc
                                : launch_pdl(attn_delta_cross<KS, NS>, dim3(q_tiles * KS, g.A >> packQ, B), dim3(SH::THR),
                                             SH::SMEM, stream, KS, tq128, tk64, tv64, to128, dp);
   };
+  // One buffer once two CTAs an SM no longer hold all (us, two buffers and one: 32 x 1024 over
+  // 100, 16 heads 161 and 154; 11 x 953, 9 on 3, 16 keys 39.5 and 37.1; 16 x 512 over 512, 16
+  // heads 96.9 and 96.7), two up to there (2 x 2048, 8 heads 84.6 and 99.2; 4 x 512 over 1024, 16
+  // heads 49.5 and 59.0; 8 x 256 over 200, 16 heads 20.0 and 21.4).
   cudaError_t e = q_ctas > 2 * sms ? delta_by(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{})
                                    : with(ksd, [&](auto ks) { return delta_by(ks, std::integral_constant<int, 2>{}); });
   if (e == cudaSuccess)

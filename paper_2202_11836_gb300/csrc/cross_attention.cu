@@ -2,7 +2,7 @@
 // sky_cross_attention_* and its choice of kernels.  Per sequence b and query head a,
 // with the key head a / (heads / kv_heads):
 //   P = softmax_j(Q K^T / sqrt(D)) over the valid keys j < len[b],  ctx = P V,
-// and with delta = rowsum(dctx ctx), dP = dctx V^T, dS = P (dP - delta)
+// and with dP = dctx V^T, delta = rowsum(P dP) = rowsum(dctx ctx), dS = P (dP - delta)
 //   dQ = dS K / sqrt(D),  dK = sum of dS^T Q / sqrt(D),  dV = sum of P^T dctx
 // over the query heads of a key head.
 #include <algorithm>

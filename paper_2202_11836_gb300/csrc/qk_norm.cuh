@@ -481,7 +481,9 @@ auto pick(const sky_qk_norm_shape& s, F&& f) {
 
 // CTAs an SM.  8192 tokens of 32 heads of 64, us: forward 12.3 with three, 14.7 with two
 // (and four stages); backward 22 with one, 26 with two of 128 registers, whose main loop
-// is as fast (19.6 and 19.8) but leaves twice the partial rows to add.
+// is as fast (19.6 and 19.8) but leaves twice the partial rows to add.  (Three is what that
+// forward's 78 registers let fit.  Forms of more, such as pairs and head dims from 80 on, and
+// fp32 in two passes, whose rings take 96 KiB, fit two, and run the plan in two rounds.)
 inline int max_ctas(bool bwd) {
   const int sms = sm_count() > 0 ? sm_count() : 148;
   return sms * (bwd ? 1 : 3);

@@ -151,6 +151,38 @@ def test_first_keys_that_score_minus_infinity(form):
     d.check_forward(*c.forward())
 
 
+class Behind:
+    """The rows from `n` on of a gradient of keys."""
+
+    def __init__(self, rows, n):
+        self.rows, self.n = rows, n
+
+    def get(self):
+        return self.rows.get()[:, self.n:]
+
+
+@pytest.mark.parametrize("sq,skv,heads,kv_heads,lens,dtype,dim", [
+    (200, 300, 4, 2, [300, 65, 129], "bf16", 64), (40, 945, 6, 3, [945, 65, 66], "bf16", 64),
+    (900, 120, 2, 2, [120, 65], "bf16", 64), (30, 120, 2, 2, [120, 65], "bf16", 64),  # many queries; one launch
+    (50, 200, 2, 1, [200, 66], "bf16", 96), (50, 200, 2, 1, [200, 66], "fp32", 64),
+])
+def test_gradients_behind_keys_that_score_minus_infinity(sq, skv, heads, kv_heads, lens, dtype, dim):
+    """Those keys' own gradients are 0, and the others' and the queries' as without them."""
+    c = Case(sq, skv, heads, kv_heads, lens, dtype=dtype, dim=dim)
+    d = Case(sq, skv - 64, heads, kv_heads, [n - 64 for n in lens], dtype=dtype, dim=dim)
+    q, k = c.q.get().clone(), c.k.get().clone()
+    q[..., 0] = q[..., 0].abs() + 4.0
+    for x, y in ((d.q, q), (d.k, k[:, 64:]), (d.v, c.v.get()[:, 64:]), (d.dctx, c.dctx.get())):
+        x.set(y.contiguous())
+    k[:, :64, :, 0] = -3e38
+    c.q.set(q)
+    c.k.set(k)
+    ctx, lse = d.given()
+    dq, dk, dv = c.backward(c.new["ctx"]().set(ctx.get().contiguous()), lse)
+    assert not bool(dk.get()[:, :64].any()) and not bool(dv.get()[:, :64].any())
+    d.check_backward((dq, Behind(dk, 64), Behind(dv, 64)))
+
+
 @pytest.mark.parametrize("B,S,heads", [(2, 200, 2), (9, 300, 16), (1, 900, 2)])
 def test_first_keys_that_score_minus_infinity_in_self_attention(B, S, heads):
     """The same over packed QKV rows: two buffers, one, four splits."""
