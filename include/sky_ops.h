@@ -149,8 +149,9 @@ size_t sky_cross_attention_bwd_workspace_bytes(const sky_cross_shape* shape);
  * on the GPU need a workspace each.
  * bf16 on the tensor cores takes P and dS as bf16 operands, as sky_attention_bwd
  * does: gradients are off by what their own rounding and the operands' are, 2.3 to
- * 2.6e-3 of their norm where one rounding is 1.7e-3.  dot(dctx, ctx) is formed for bf16 from P and dctx v^T in
- * 32 bits (only fp32 reads ctx), so a mean of v or peaked scores do not add to that.
+ * 2.6e-3 of their norm where one rounding is 1.7e-3.  For bf16 dot(dctx, ctx) is
+ * formed from P and dctx v^T in 32 bits (only fp32 reads ctx), so neither a mean of v
+ * nor peaked scores add to that.
  * Errors as the forward's; INVALID_ARG for a workspace that is too small or not
  * 16-byte aligned. */
 sky_status sky_cross_attention_bwd(const sky_cross_shape* shape, const void* q, const void* k,

@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(F_THR, G > 16 ? 1 : 4) attn_bwd_simt(const Geo
 }
 
 // delta of bf16 storage: the sum over the keys of P dP.  dot(dctx, ctx) is the same sum, but of
-// a rounded ctx it is off by up to 2^-9 sum |dctx ctx|, the same for every key of the row,
+// a rounded ctx it is off by up to 2^-8 sum |dctx ctx|, the same for every key of the row,
 // which a mean of V makes larger than dS.  Own rows are queries, columns keys, as for dQ; the
 // CTAs of a cluster share a block's columns.  Two of the backward's seven products once more
 // (us, from the rounded ctx and this): 4 x 200 over 333, 8 heads on 2 of 128 210 and 264; 8 x

@@ -2045,10 +2045,10 @@ namespace attn_tc {
 // per-query rows [B][A >> pack][2][Sq << pack]: the log-sum-exp over c = log2(e)/sqrt(D),
 // then delta, negated and split as its comment says.
 //
-// dot(dctx, ctx) is the same sum, but of a ctx rounded to bf16 it is off by up to 2^-9
+// dot(dctx, ctx) is the same sum, but of a ctx rounded to bf16 it is off by up to 2^-8
 // sum |dctx ctx|, the same for every key of the row: that does not shrink with dS, and a
 // mean of V, which leaves the exact dq alone, makes it as large as one likes (V of mean 4
-// over 512 keys: dq off by 1.3e-2 of its norm).  So S and dP are formed here once more, two of
+// over 512 keys: dq off by 1.2e-2 of its norm).  So S and dP are formed here once more, two of
 // the five products, and the sum stays in 32 bits.
 //
 // One CTA per 128 query rows as in the dQ kernel, but nothing goes back.  Two forms, as of the
