@@ -1,5 +1,4 @@
-"""ctypes binding of libsky_slice.so: the C ABI of include/sky_slice.h and
-include/sky_ops.h under the same names.
+"""ctypes binding of libsky_slice.so: the C ABI of include/*.h under the same names.
 
 The binding only marshals arguments (pointers, sizes, enums); every step of
 the encoder slice runs in the library's CUDA kernels.  Loading fails loudly
@@ -19,6 +18,9 @@ SKY_DTYPE_BF16, SKY_DTYPE_FP32 = 0, 1
 SKY_GEMM_XWT, SKY_GEMM_XW, SKY_GEMM_XTW = 0, 1, 2
 SKY_EPI_STORE, SKY_EPI_BIAS_GELU, SKY_EPI_GELU_BWD = 0, 1, 2
 SKY_ROTATE_NONE, SKY_ROTATE_HALVES, SKY_ROTATE_PAIRS = 0, 1, 2
+SKY_ROUTE_OVER_ALL, SKY_ROUTE_OVER_CHOSEN = 0, 1
+SKY_STATE_FP32, SKY_STATE_8BIT = 0, 1
+SKY_STATE_BLOCK = 256
 SKY_NUM_PARAMS = 12
 
 
@@ -85,6 +87,33 @@ class SkyQkNormShape(C.Structure):
                 ("theta", C.c_double)]
 
 
+class SkyRouteShape(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("experts", C.c_int32), ("top_k", C.c_int32),
+                ("dtype", C.c_int), ("weights", C.c_int)]
+
+
+class SkyRowsShape(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("top_k", C.c_int32), ("width", C.c_int32),
+                ("dtype", C.c_int)]
+
+
+class SkyGroupedShape(C.Structure):
+    _fields_ = [("groups", C.c_int32), ("rows", C.c_int32), ("out", C.c_int32), ("in_", C.c_int32),
+                ("dtype", C.c_int)]
+
+
+class SkyAdamwTensor(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("p", C.c_void_p),
+                ("n", C.c_int64), ("decay", C.c_int32)]
+
+
+class SkyAdamwConfig(C.Structure):
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
+                ("weight_decay", C.c_float), ("step", C.c_int64), ("grad_dtype", C.c_int),
+                ("states", C.c_int)]
+
+
 _VP, _I32, _SZ = C.c_void_p, C.c_int32, C.c_size_t
 _SIGNATURES = {
     "sky_slice_create": (C.c_int, [C.POINTER(SkySliceConfig), C.POINTER(_VP)]),
@@ -141,6 +170,19 @@ _SIGNATURES = {
     "sky_slice_optimizer_init": (C.c_int, [_VP, C.POINTER(SkyOptimizerConfig)]),
     "sky_slice_optimizer_step": (C.c_int, [_VP, C.c_float, _VP]),
     "sky_slice_get_optimizer_state": (C.c_int, [_VP, _I32, _I32, C.POINTER(_VP)]),
+    "sky_route_workspace_bytes": (_SZ, [C.POINTER(SkyRouteShape)]),
+    "sky_route_fwd": (C.c_int, [C.POINTER(SkyRouteShape)] + [_VP] * 6 + [_SZ, _VP, _VP]),
+    "sky_route_bwd": (C.c_int, [C.POINTER(SkyRouteShape)] + [_VP] * 5),
+    "sky_dispatch_fwd": (C.c_int, [C.POINTER(SkyRowsShape)] + [_VP] * 4),
+    "sky_dispatch_bwd": (C.c_int, [C.POINTER(SkyRowsShape)] + [_VP] * 4),
+    "sky_combine_fwd": (C.c_int, [C.POINTER(SkyRowsShape)] + [_VP] * 5),
+    "sky_combine_bwd": (C.c_int, [C.POINTER(SkyRowsShape)] + [_VP] * 7),
+    "sky_grouped_gemm_workspace_bytes": (_SZ, [C.c_int, C.POINTER(SkyGroupedShape), C.c_int]),
+    "sky_grouped_gemm": (C.c_int, [C.c_int, C.POINTER(SkyGroupedShape), _VP, _VP, _VP, _VP, C.c_int,
+                                   C.c_int] + [_VP] * 4 + [_SZ, _VP, _VP]),
+    "sky_grouped_column_sum": (C.c_int, [C.POINTER(SkyGroupedShape)] + [_VP] * 5),
+    "sky_adamw_step": (C.c_int, [C.POINTER(SkyAdamwConfig), C.POINTER(SkyAdamwTensor), _I32, _VP,
+                                 _VP]),
     "sky_alloc_even": (C.c_int, [_I32, _I32, C.POINTER(_I32)]),
     "sky_alloc_coarse": (C.c_int, [C.POINTER(SkyAllocProblem), C.POINTER(_I32)]),
     "sky_alloc_finetune": (C.c_int, [C.POINTER(SkyAllocProblem), _I32, C.POINTER(_I32),

@@ -1,0 +1,34 @@
+// The products grouped by expert (sky_experts.h): what their kernels share.
+#pragma once
+#include <cuda_runtime.h>
+
+#include "../../include/sky_experts.h"
+
+namespace sky {
+namespace grouped {
+
+// A call, checked.  Weights are [groups][out][in]; group g owns the rows
+// [offset[g], offset[g + 1]) of the ragged matrices.
+//   XWT: A [rows, in],  B weights,      C [rows, out]
+//   XW:  A [rows, out], B weights,      C [rows, in]
+//   XTW: A [rows, out], B [rows, in],   C fp32 [groups][out][in]
+struct Call {
+  sky_gemm_form form;
+  int groups, rows, out, in;
+  const int32_t* offset;
+  const void *A, *B;
+  void* C;
+  sky_epilogue epi;
+  const void *bias, *aux;
+  void* aux_out;
+  void* ws;
+  size_t ws_bytes;
+  int32_t* status;
+};
+
+// fp32 arithmetic on the CUDA cores (grouped_f32.cu).
+template <typename T>
+sky_status launch_simt(const Call& c, cudaStream_t st);
+
+}  // namespace grouped
+}  // namespace sky

@@ -1,0 +1,133 @@
+// Products grouped by expert in fp32 arithmetic on the CUDA cores: the tiles of gemm_f32.cu,
+// each over the rows of one group.  Bound as those are, by the FMA pipe or, with few rows, by
+// the latency of a slab; the number of tiles is known on the device only, so the grid holds as
+// many as the rows may make and those that are too many leave at once.
+#include <cuda_fp16.h>
+
+#include <type_traits>
+
+#include "common.cuh"
+#include "f32_tile.cuh"
+#include "grouped.cuh"
+#include "grouped.h"
+#include "ptx.cuh"
+
+namespace sky {
+namespace grouped {
+namespace {
+
+using gemm::F_THREADS;
+using gemm::TK;
+using gemm::TM;
+using gemm::TN;
+
+struct Params {
+  Call c;
+  int m_tiles, n_tiles, ks;  // m_tiles: XTW only
+};
+
+// GELU' is kept as the dense products keep it: fp16 beside bf16, else fp32.
+template <typename T> struct Slope { using type = float; };
+template <> struct Slope<__nv_bfloat16> { using type = __half; };
+__device__ __forceinline__ float slope_value(float s) { return s; }
+__device__ __forceinline__ float slope_value(__half s) { return __half2float(s); }
+__device__ __forceinline__ void set_slope(float* s, float v) { *s = v; }
+__device__ __forceinline__ void set_slope(__half* s, float v) { *s = __float2half_rn(v); }
+
+template <typename T, int FORM, bool VEC>
+__global__ void __launch_bounds__(F_THREADS) grouped_simt(const __grid_constant__ Params p) {
+  using S = typename Slope<T>::type;
+  const Call& c = p.c;
+  pdl_wait();
+  const int split = static_cast<int>(blockIdx.x) % p.ks, tile = static_cast<int>(blockIdx.x) / p.ks;
+  if (blockIdx.x == 0) check_offsets(c.offset, c.groups, c.rows, c.status);
+  const T *A = static_cast<const T*>(c.A), *B = static_cast<const T*>(c.B);
+  gemm::F32Operands<T> o;
+  int m0, n0, g;
+  int64_t row0 = 0;
+  if constexpr (FORM == SKY_GEMM_XTW) {
+    g = tile / (p.m_tiles * p.n_tiles);
+    const int in_group = tile % (p.m_tiles * p.n_tiles);
+    m0 = in_group / p.n_tiles * TM;
+    n0 = in_group % p.n_tiles * TN;
+    const int2 r = group_rows(c.offset, g, c.rows);
+    o = {A + static_cast<int64_t>(r.x) * c.out, B + static_cast<int64_t>(r.x) * c.in, c.out, c.in, c.out, c.in, r.y - r.x};
+  } else {
+    const Found f = find_tile(c.offset, c.groups, c.rows, tile / p.n_tiles, [](int n) { return (n + TM - 1) / TM; });
+    if (f.group < 0) return;  // (every CTA of a cluster)
+    g = f.group;
+    m0 = f.tile * TM;
+    n0 = tile % p.n_tiles * TN;
+    row0 = f.lo;
+    const int K = FORM == SKY_GEMM_XWT ? c.in : c.out, N = FORM == SKY_GEMM_XWT ? c.out : c.in;
+    o = {A + row0 * K, B + static_cast<int64_t>(g) * c.out * c.in, K, c.in, f.hi - f.lo, N, K};
+  }
+  if (p.ks > 1) ptx::cluster_arrive();  // this CTA runs: its peers may write its shared memory
+  const int slabs = (o.K + TK - 1) / TK;
+  const int s0 = static_cast<int>(static_cast<int64_t>(split) * slabs / p.ks);
+  const int s1 = static_cast<int>(static_cast<int64_t>(split + 1) * slabs / p.ks);
+  auto finish = [&](int m, int n, float v) {
+    if (m >= o.M || n >= o.N) return;
+    if constexpr (FORM == SKY_GEMM_XTW) {
+      static_cast<float*>(c.C)[(static_cast<int64_t>(g) * c.out + m) * c.in + n] = v;
+    } else {
+      const int64_t off = (row0 + m) * o.N + n;
+      if (FORM == SKY_GEMM_XWT && c.bias) v += to_f32<T>(static_cast<const T*>(c.bias)[static_cast<int64_t>(g) * c.out + n]);
+      if (c.epi == SKY_EPI_GELU_BWD) v *= slope_value(static_cast<const S*>(c.aux)[off]);
+      if (c.epi == SKY_EPI_BIAS_GELU) {
+        set_slope(static_cast<S*>(c.aux_out) + off, gelu_grad_f(v));
+        v = gelu_f(v);
+      }
+      static_cast<T*>(c.C)[off] = from_f32<T>(v);
+    }
+  };
+  gemm::f32_tile<FORM != SKY_GEMM_XTW, FORM == SKY_GEMM_XWT, VEC>(o, m0, n0, p.ks, split, s0, s1, finish);
+}
+
+template <typename T, int FORM>
+sky_status launch(const Call& c, cudaStream_t st) {
+  const int sms = sm_count();
+  SKY_CHECK(sms > 0, SKY_ERR_CUDA, "no CUDA device");
+  Params p{};
+  p.c = c;
+  const int N = FORM == SKY_GEMM_XWT ? c.out : c.in;
+  p.n_tiles = ceil_div(N, TN);
+  p.m_tiles = FORM == SKY_GEMM_XTW ? ceil_div(c.out, TM) : 0;
+  // tiles of rows: every group that has any may end inside one
+  const int64_t m_tiles = FORM == SKY_GEMM_XTW ? static_cast<int64_t>(c.groups) * p.m_tiles
+                                               : c.rows / TM + static_cast<int64_t>(std::min(c.groups, c.rows));
+  const int64_t tiles = m_tiles * p.n_tiles;
+  // splits as gemm_f32.cu makes them, by the slabs of a mean group
+  const int K = FORM == SKY_GEMM_XWT ? c.in : FORM == SKY_GEMM_XW ? c.out : ceil_div(c.rows, c.groups);
+  const int slabs = ceil_div(K, TK);
+  p.ks = 1;
+  for (int ks = 8; ks >= 4 && p.ks == 1; ks /= 2)
+    if (tiles * ks <= 11 * sms && slabs >= 2 * ks) p.ks = ks;
+  SKY_CHECK(tiles * p.ks <= 0x7fffffff, SKY_ERR_UNSUPPORTED, "grouped product too large");
+  const auto a16 = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
+  const bool vec = std::is_same<T, float>::value && c.in % 4 == 0 && c.out % 4 == 0 && a16(c.A) && a16(c.B);
+  const dim3 grid(static_cast<unsigned>(tiles * p.ks));
+  cudaError_t e;
+  if constexpr (std::is_same<T, float>::value) {
+    e = vec ? launch_pdl(grouped_simt<T, FORM, true>, grid, dim3(F_THREADS), 0, st, p.ks, p)
+            : launch_pdl(grouped_simt<T, FORM, false>, grid, dim3(F_THREADS), 0, st, p.ks, p);
+  } else {
+    e = launch_pdl(grouped_simt<T, FORM, false>, grid, dim3(F_THREADS), 0, st, p.ks, p);
+  }
+  count_launches(1);
+  return e == cudaSuccess ? SKY_OK : cuda_fail(e, "grouped product launch");
+}
+
+}  // namespace
+
+template <typename T>
+sky_status launch_simt(const Call& c, cudaStream_t st) {
+  if (c.form == SKY_GEMM_XWT) return launch<T, SKY_GEMM_XWT>(c, st);
+  if (c.form == SKY_GEMM_XW) return launch<T, SKY_GEMM_XW>(c, st);
+  return launch<T, SKY_GEMM_XTW>(c, st);
+}
+template sky_status launch_simt<float>(const Call&, cudaStream_t);
+template sky_status launch_simt<__nv_bfloat16>(const Call&, cudaStream_t);
+
+}  // namespace grouped
+}  // namespace sky

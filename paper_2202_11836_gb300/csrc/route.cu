@@ -1,0 +1,478 @@
+// Routing of tokens to experts (sky_experts.h): the top k logits of every token, their
+// weights, and the plan that sorts the choices by expert, then by token.
+//
+// A warp holds a token's logits, expert lane + 32 j in lane's register j, as unsigned
+// integers in the order of the numbers.  A choice is one warp reduction for the largest and
+// one for the lowest index that has it.
+//
+// The sort is a counting sort over blocks of consecutive tokens.  A token chooses an expert
+// at most once, so a block's choices of an expert are a bit mask over its tokens: the block's
+// count is the mask's population, and a choice's rank the population below its token's bit.
+// Setting bits needs no order, so the plan is deterministic.  The counts of all blocks go
+// through the workspace, and a second launch adds up what lies before each block; up to
+// SMALL tokens one CTA does everything in one launch.  At these sizes (8192 x 64 logits are
+// 2 MB) all of it is latency: launches and the chain of reductions.
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/sky_experts.h"
+#include "abi.h"
+#include "common.cuh"
+
+namespace sky {
+namespace route {
+namespace {
+
+constexpr int MAX_EXPERTS = 1024, MAX_TOP_K = 32;
+constexpr int THREADS = 256, SMALL_THREADS = 1024, SMALL = 64;
+constexpr int MOST_BLOCK = 256;     // tokens of a block
+constexpr int MOST_COUNTS = 16384;  // counts that every block adds up for itself
+constexpr int32_t kStatusNaN = 4;
+
+struct Params {
+  int tokens, experts, top_k, block;  // block: tokens of one, a multiple of 32
+  int blocks;
+  bool over_all, scanned;
+  const void* logits;
+  int32_t* expert;
+  float* weight;
+  int32_t* row;
+  int32_t* offset;
+  int32_t* counts;  // [blocks][experts], and when scanned [experts] totals behind them
+  int32_t* status;
+};
+
+// A logit's place in the order of numbers; 0 for NaN.  -0 counts as 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return x != x ? 0u : (b >> 31 ? ~b : b | 0x80000000u);
+}
+__device__ __forceinline__ float number_of(uint32_t o) {
+  return __uint_as_float(o >> 31 ? o & 0x7fffffffu : ~o);
+}
+constexpr uint32_t LOWEST = 0x007fffffu;  // of -inf: nothing up to here is chosen
+
+// exp(x - top), where equal infinities count as equal.
+__device__ __forceinline__ float exp_below(float x, float top) { return x == top ? 1.f : expf(x - top); }
+
+// The choices of one token, by a warp: lane c gets choice c.
+template <typename T, int V>
+__device__ __forceinline__ void choose(const Params& p, int t, int lane, int& mine, float& weight) {
+  uint32_t key[V];
+  bool nan = false;
+  const T* x = static_cast<const T*>(p.logits) + static_cast<int64_t>(t) * p.experts;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int e = lane + 32 * j;
+    const float f = e < p.experts ? to_f32<T>(x[e]) : -INFINITY;
+    nan |= f != f;
+    key[j] = order_of(f);
+  }
+  if (nan && p.status) atomicOr(p.status, kStatusNaN);
+  float all = 0.f, value = -INFINITY, top = 0.f;
+  mine = -1;
+  for (int c = 0; c < p.top_k; ++c) {
+    uint32_t best = key[0];
+#pragma unroll
+    for (int j = 1; j < V; ++j) best = max(best, key[j]);
+    best = __reduce_max_sync(0xffffffffu, best);
+    if (best <= LOWEST) break;  // warp-uniform
+    if (c == 0) {
+      top = number_of(best);
+      if (p.over_all) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (key[j] > LOWEST) all += exp_below(number_of(key[j]), top);
+      }
+    }
+    int at = MAX_EXPERTS;
+#pragma unroll
+    for (int j = V - 1; j >= 0; --j)
+      if (key[j] == best) at = lane + 32 * j;
+    at = __reduce_min_sync(0xffffffffu, at);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (at == lane + 32 * j) key[j] = 0;
+    if (lane == c) {
+      mine = at;
+      value = number_of(best);
+    }
+  }
+  const float e = mine >= 0 ? exp_below(value, top) : 0.f;
+  const float total = warp_sum(p.over_all ? all : e);
+  weight = mine >= 0 ? e / total : 0.f;
+}
+
+// Exclusive sums over the experts of what `total` holds, by a whole CTA.
+__device__ __forceinline__ void scan_experts(int* total, int experts, int* warp_sums) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const int per = (experts + blockDim.x - 1) / blockDim.x;  // consecutive experts of a thread
+  int own = 0;
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < experts) own += total[tid * per + i];
+  int sum = own;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += up;
+  }
+  if (lane == 31) warp_sums[warp] = sum;
+  __syncthreads();
+  int before = sum - own;
+  for (int w = 0; w < warps; ++w)
+    if (w < warp) before += warp_sums[w];
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < experts) {
+      const int n = total[tid * per + i];
+      total[tid * per + i] = before;
+      before += n;
+    }
+  __syncthreads();
+}
+
+// The places of a block's choices, whose masks are set: base[e] + rank.
+__device__ __forceinline__ void place_block(const Params& p, int t0, const uint32_t* mask, const int* base) {
+  const int words = p.block / 32, n = min(p.block, p.tokens - t0) * p.top_k;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int64_t at = static_cast<int64_t>(t0) * p.top_k + i;
+    const int e = p.expert[at], t = i / p.top_k;
+    int place = -1;
+    if (e >= 0) {
+      place = base[e];
+      for (int w = 0; w < t / 32; ++w) place += __popc(mask[e * words + w]);
+      place += __popc(mask[e * words + t / 32] & ((1u << (t & 31)) - 1u));
+    }
+    p.row[at] = place;
+  }
+}
+
+// Chooses for a block of tokens and sets its masks.
+template <typename T, int V>
+__device__ __forceinline__ void choose_block(const Params& p, int t0, uint32_t* mask) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, words = p.block / 32;
+  for (int i = threadIdx.x; i < p.experts * words; i += blockDim.x) mask[i] = 0;
+  __syncthreads();
+  for (int t = warp; t < p.block && t0 + t < p.tokens; t += blockDim.x >> 5) {
+    int e;
+    float w;
+    choose<T, V>(p, t0 + t, lane, e, w);
+    if (lane < p.top_k) {
+      const int64_t at = static_cast<int64_t>(t0 + t) * p.top_k + lane;
+      p.expert[at] = e;
+      p.weight[at] = w;
+      if (e >= 0) atomicOr(&mask[e * words + t / 32], 1u << (t & 31));
+    }
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int count_of(const uint32_t* mask, int e, int words) {
+  int n = 0;
+  for (int w = 0; w < words; ++w) n += __popc(mask[e * words + w]);
+  return n;
+}
+
+// Everything, for one block of tokens.  (With 32 experts a lane, half the threads: their
+// keys take the registers.)
+constexpr int small_threads(int v) { return v == 32 ? SMALL_THREADS / 2 : SMALL_THREADS; }
+template <typename T, int V>
+__global__ void __launch_bounds__(small_threads(V)) route_small(const Params p) {
+  extern __shared__ uint32_t sm[];
+  __shared__ int sums[32];
+  uint32_t* mask = sm;
+  int* base = reinterpret_cast<int*>(mask + p.experts * (p.block / 32));
+  pdl_wait();
+  pdl_trigger();
+  choose_block<T, V>(p, 0, mask);
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) base[e] = count_of(mask, e, p.block / 32);
+  __syncthreads();
+  const int last = base[p.experts - 1];
+  __syncthreads();
+  scan_experts(base, p.experts, sums);
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.offset[e] = base[e];
+  if (threadIdx.x == 0) p.offset[p.experts] = base[p.experts - 1] + last;
+  place_block(p, 0, mask, base);  // (what it reads of p.expert this CTA wrote before a barrier)
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(THREADS) route_choose(const Params p) {
+  extern __shared__ uint32_t sm[];
+  pdl_wait();
+  pdl_trigger();
+  choose_block<T, V>(p, blockIdx.x * p.block, sm);
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x)
+    p.counts[static_cast<int64_t>(blockIdx.x) * p.experts + e] = count_of(sm, e, p.block / 32);
+}
+
+// Many blocks: counts[b][e] becomes what the blocks before b have, the totals follow.  A warp
+// takes an expert, 32 blocks at a time.
+__global__ void __launch_bounds__(THREADS) route_scan(const Params p) {
+  pdl_wait();
+  pdl_trigger();
+  const int e = blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (e >= p.experts) return;
+  int before = 0;
+  for (int b0 = 0; b0 < p.blocks; b0 += 32) {
+    const int b = b0 + lane;
+    int32_t* at = p.counts + static_cast<int64_t>(b) * p.experts + e;
+    const int own = b < p.blocks ? *at : 0;
+    int sum = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += up;
+    }
+    if (b < p.blocks) *at = before + sum - own;
+    before += __shfl_sync(0xffffffffu, sum, 31);
+  }
+  if (lane == 0) p.counts[static_cast<int64_t>(p.blocks) * p.experts + e] = before;
+}
+
+__global__ void __launch_bounds__(THREADS) route_place(const Params p) {
+  extern __shared__ uint32_t sm[];
+  __shared__ int sums[THREADS / 32];
+  const int words = p.block / 32, t0 = blockIdx.x * p.block;
+  uint32_t* mask = sm;
+  int* base = reinterpret_cast<int*>(mask + p.experts * words);  // totals, then starts
+  int* before = base + p.experts;
+  for (int i = threadIdx.x; i < p.experts * words; i += blockDim.x) mask[i] = 0;
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) base[e] = before[e] = 0;
+  __syncthreads();
+  pdl_wait();
+  pdl_trigger();
+  const int n = min(p.block, p.tokens - t0) * p.top_k;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const int e = p.expert[static_cast<int64_t>(t0) * p.top_k + i], t = i / p.top_k;
+    if (e >= 0) atomicOr(&mask[e * words + t / 32], 1u << (t & 31));
+  }
+  if (p.scanned) {
+    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) {
+      base[e] = p.counts[static_cast<int64_t>(p.blocks) * p.experts + e];
+      before[e] = p.counts[static_cast<int64_t>(blockIdx.x) * p.experts + e];
+    }
+  } else {
+    // thread (expert, part) adds up every parts-th block; whole numbers, so any order will do
+    const int parts = max(1, static_cast<int>(blockDim.x) / p.experts);
+    for (int i = threadIdx.x; i < p.experts * parts; i += blockDim.x) {
+      const int e = i % p.experts;
+      int total = 0, mine = 0;
+#pragma unroll 8
+      for (int b = i / p.experts; b < p.blocks; b += parts) {
+        const int c = p.counts[b * p.experts + e];
+        total += c;
+        if (b < static_cast<int>(blockIdx.x)) mine += c;
+      }
+      if (total) atomicAdd(&base[e], total);
+      if (mine) atomicAdd(&before[e], mine);
+    }
+  }
+  __syncthreads();
+  const int last = base[p.experts - 1];
+  __syncthreads();
+  scan_experts(base, p.experts, sums);
+  if (blockIdx.x == 0) {
+    for (int e = threadIdx.x; e < p.experts; e += blockDim.x) p.offset[e] = base[e];
+    if (threadIdx.x == 0) p.offset[p.experts] = base[p.experts - 1] + last;
+  }
+  for (int e = threadIdx.x; e < p.experts; e += blockDim.x) before[e] += base[e];
+  __syncthreads();
+  place_block(p, t0, mask, before);
+}
+
+// dlogits of a token by a warp.
+template <typename T, int V>
+__global__ void __launch_bounds__(THREADS) route_backward(const Params p, const float* dweight, T* out) {
+  const int lane = threadIdx.x & 31, t = blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+  pdl_wait();
+  pdl_trigger();
+  if (t >= p.tokens) return;
+  const T* x = static_cast<const T*>(p.logits) + static_cast<int64_t>(t) * p.experts;
+  const int64_t at = static_cast<int64_t>(t) * p.top_k + lane;
+  const int mine = lane < p.top_k ? p.expert[at] : -1;
+  const float dmine = lane < p.top_k ? dweight[at] : 0.f;
+  float v[V], dw[V];
+  uint32_t chosen = 0;  // bit j: expert lane + 32 j
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int e = lane + 32 * j;
+    v[j] = e < p.experts ? to_f32<T>(x[e]) : -INFINITY;
+    if (v[j] != v[j]) v[j] = -INFINITY;
+    dw[j] = 0.f;
+  }
+  for (int c = 0; c < p.top_k; ++c) {
+    const int e = __shfl_sync(0xffffffffu, mine, c);
+    const float d = __shfl_sync(0xffffffffu, dmine, c);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (e == lane + 32 * j) {
+        chosen |= 1u << j;
+        dw[j] += d;
+      }
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    if (!p.over_all && !(chosen >> j & 1)) v[j] = -INFINITY;
+    top = fmaxf(top, v[j]);
+  }
+  top = warp_max(top);
+  float total = 0.f, mean = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    v[j] = v[j] > -INFINITY ? exp_below(v[j], top) : 0.f;
+    total += v[j];
+    if (chosen >> j & 1) mean += v[j] * dw[j];
+  }
+  total = warp_sum(total);
+  mean = warp_sum(mean);
+  const float inv = total > 0.f ? 1.f / total : 0.f;
+  mean *= inv;
+  T* y = out + static_cast<int64_t>(t) * p.experts;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int e = lane + 32 * j;
+    const float pr = v[j] * inv;
+    if (e < p.experts) y[e] = from_f32<T>(pr == 0.f ? 0.f : pr * ((chosen >> j & 1 ? dw[j] : 0.f) - mean));
+  }
+}
+
+sky_status check(const sky_route_shape* s) {
+  SKY_CHECK(s, SKY_ERR_INVALID_ARG, "null shape");
+  SKY_CHECK(s->tokens > 0 && s->experts > 0 && s->top_k > 0 && s->top_k <= s->experts, SKY_ERR_INVALID_ARG, "bad sizes");
+  SKY_CHECK(s->dtype == SKY_DTYPE_BF16 || s->dtype == SKY_DTYPE_FP32, SKY_ERR_INVALID_ARG, "unknown dtype");
+  SKY_CHECK(s->weights == SKY_ROUTE_OVER_ALL || s->weights == SKY_ROUTE_OVER_CHOSEN, SKY_ERR_INVALID_ARG,
+            "unknown kind of weights");
+  SKY_CHECK(s->experts <= MAX_EXPERTS && s->top_k <= MAX_TOP_K, SKY_ERR_UNSUPPORTED,
+            "routing to more than %d experts or of more than %d choices", MAX_EXPERTS, MAX_TOP_K);
+  SKY_CHECK(static_cast<int64_t>(s->tokens) * s->experts < (int64_t{1} << 31) &&
+                static_cast<int64_t>(s->tokens) * s->top_k < (int64_t{1} << 31),
+            SKY_ERR_UNSUPPORTED, "routing of 2^31 logits or choices or more");
+  return SKY_OK;
+}
+
+bool on(const void* p, size_t grid) { return reinterpret_cast<uintptr_t>(p) % grid == 0; }
+
+// Tokens of a block: 32, or what keeps the blocks few; they are on all SMs either way.
+int block_of(int tokens) {
+  int b = 32;
+  while (b < MOST_BLOCK && ceil_div(tokens, b) > 256) b *= 2;
+  return b;
+}
+
+size_t workspace(const sky_route_shape& s) {
+  if (s.tokens <= SMALL) return 16;
+  return (static_cast<size_t>(ceil_div(s.tokens, block_of(s.tokens))) + 1) * s.experts * sizeof(int32_t);
+}
+
+// f with the registers a lane needs for its experts.
+template <typename F>
+auto by_experts(int experts, F&& f) {
+  if (experts <= 32) return f(std::integral_constant<int, 1>());
+  if (experts <= 64) return f(std::integral_constant<int, 2>());
+  if (experts <= 128) return f(std::integral_constant<int, 4>());
+  if (experts <= 256) return f(std::integral_constant<int, 8>());
+  return f(std::integral_constant<int, 32>());
+}
+
+template <typename T>
+sky_status forward(Params p, cudaStream_t st) {
+  cudaError_t e;
+  if (p.tokens <= SMALL) {
+    p.block = ceil_div(p.tokens, 32) * 32;
+    p.blocks = 1;
+    const size_t smem = static_cast<size_t>(p.experts) * (p.block / 32 + 1) * 4;
+    e = by_experts(p.experts, [&](auto v) {
+      const int threads = std::min(small_threads(decltype(v)::value), 32 * p.tokens);
+      return launch_pdl(route_small<T, decltype(v)::value>, dim3(1), dim3(threads), smem, st, 1, p);
+    });
+    count_launches(1);
+    return e == cudaSuccess ? SKY_OK : cuda_fail(e, "routing launch");
+  }
+  p.block = block_of(p.tokens);
+  p.blocks = ceil_div(p.tokens, p.block);
+  p.scanned = static_cast<int64_t>(p.blocks) * p.experts > MOST_COUNTS;
+  const size_t masks = static_cast<size_t>(p.experts) * (p.block / 32) * 4;  // up to 32 KiB
+  e = by_experts(p.experts, [&](auto v) {
+    return launch_pdl(route_choose<T, decltype(v)::value>, dim3(p.blocks), dim3(THREADS), masks, st, 1, p);
+  });
+  count_launches(1);
+  if (e == cudaSuccess && p.scanned) {
+    e = launch_pdl(route_scan, dim3(ceil_div(p.experts, THREADS / 32)), dim3(THREADS), 0, st, 1, p);
+    count_launches(1);
+  }
+  if (e == cudaSuccess) {
+    e = launch_pdl(route_place, dim3(p.blocks), dim3(THREADS), masks + 2 * p.experts * 4, st, 1, p);
+    count_launches(1);
+  }
+  return e == cudaSuccess ? SKY_OK : cuda_fail(e, "routing launch");
+}
+
+template <typename T>
+sky_status backward(const Params& p, const float* dweight, void* dlogits, cudaStream_t st) {
+  const cudaError_t e = by_experts(p.experts, [&](auto v) {
+    return launch_pdl(route_backward<T, decltype(v)::value>, dim3(ceil_div(p.tokens, THREADS / 32)), dim3(THREADS), 0, st,
+                      1, p, dweight, static_cast<T*>(dlogits));
+  });
+  count_launches(1);
+  return e == cudaSuccess ? SKY_OK : cuda_fail(e, "routing backward launch");
+}
+
+Params params(const sky_route_shape& s, const void* logits, int32_t* expert) {
+  Params p{};
+  p.tokens = s.tokens; p.experts = s.experts; p.top_k = s.top_k;
+  p.over_all = s.weights == SKY_ROUTE_OVER_ALL;
+  p.logits = logits;
+  p.expert = expert;
+  return p;
+}
+
+}  // namespace
+}  // namespace route
+}  // namespace sky
+
+using namespace sky;
+
+extern "C" {
+
+size_t sky_route_workspace_bytes(const sky_route_shape* shape) {
+  return shape && route::check(shape) == SKY_OK ? route::workspace(*shape) : 0;
+}
+
+sky_status sky_route_fwd(const sky_route_shape* shape, const void* logits, int32_t* expert, float* weight, int32_t* row,
+                         int32_t* offset, void* workspace, size_t workspace_bytes, int32_t* d_status, void* stream) {
+  ABI_GUARD_BEGIN
+  const sky_status ok = route::check(shape);
+  if (ok != SKY_OK) return ok;
+  SKY_CHECK(logits && expert && weight && row && offset && workspace, SKY_ERR_INVALID_ARG, "null argument");
+  SKY_CHECK(route::on(logits, shape->dtype == SKY_DTYPE_BF16 ? 2 : 4) && route::on(expert, 4) && route::on(weight, 4) &&
+                route::on(row, 4) && route::on(offset, 4) && route::on(workspace, 4) && route::on(d_status, 4),
+            SKY_ERR_INVALID_ARG, "a pointer off its type's grid");
+  SKY_CHECK(workspace_bytes >= route::workspace(*shape), SKY_ERR_INVALID_ARG, "workspace too small");
+  route::Params p = route::params(*shape, logits, expert);
+  p.weight = weight;
+  p.row = row;
+  p.offset = offset;
+  p.counts = static_cast<int32_t*>(workspace);
+  p.status = d_status;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return shape->dtype == SKY_DTYPE_BF16 ? route::forward<__nv_bfloat16>(p, st) : route::forward<float>(p, st);
+  ABI_GUARD_END
+}
+
+sky_status sky_route_bwd(const sky_route_shape* shape, const void* logits, const int32_t* expert, const float* dweight,
+                         void* dlogits, void* stream) {
+  ABI_GUARD_BEGIN
+  const sky_status ok = route::check(shape);
+  if (ok != SKY_OK) return ok;
+  SKY_CHECK(logits && expert && dweight && dlogits, SKY_ERR_INVALID_ARG, "null argument");
+  const size_t g = shape->dtype == SKY_DTYPE_BF16 ? 2 : 4;
+  SKY_CHECK(route::on(logits, g) && route::on(dlogits, g) && route::on(expert, 4) && route::on(dweight, 4),
+            SKY_ERR_INVALID_ARG, "a pointer off its type's grid");
+  const route::Params p = route::params(*shape, logits, const_cast<int32_t*>(expert));
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  return shape->dtype == SKY_DTYPE_BF16 ? route::backward<__nv_bfloat16>(p, dweight, dlogits, st)
+                                        : route::backward<float>(p, dweight, dlogits, st);
+  ABI_GUARD_END
+}
+
+}  // extern "C"
