@@ -129,7 +129,7 @@ size_t sky_grouped_gemm_workspace_bytes(sky_gemm_form form, const sky_grouped_sh
  * Errors: INVALID_ARG (null, sizes, an unknown dtype, form or epilogue, a pointer off its
  * type's grid, a workspace that is too small or not 16-byte aligned), UNSUPPORTED (other
  * output dtypes and epilogues; bf16: out or in not a multiple of 8, A, B, C, aux or aux_out
- * not 16-byte aligned; more than 1024 groups, 2^30 rows or more, out or in above 2^20,
+ * not 16-byte aligned; more than 1024 groups, 2^28 rows or more, out or in above 2^20,
  * groups * out of 2^31 or more); offsets that decrease or leave [0, rows] are clamped and
  * set bit 0 of *d_status, and what the calls then write is not defined within C. */
 sky_status sky_grouped_gemm(sky_gemm_form form, const sky_grouped_shape* shape,

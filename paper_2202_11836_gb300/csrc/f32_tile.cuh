@@ -15,9 +15,8 @@ constexpr int LD4 = TK * 64 / 4 / F_THREADS;         // 16-byte groups a thread 
 
 // One operand pair of a tile: element (i, k) of A at i * lda + k where it is K-major, else
 // at k * lda + i, likewise B; rows m < M, columns n < N, and K of the sum.
-template <typename T>
 struct F32Operands {
-  const T *A, *B;
+  const float *A, *B;
   int64_t lda, ldb;
   int M, N, K;
 };
@@ -29,22 +28,22 @@ __device__ __forceinline__ constexpr int swz(int k) { return ((k >> 2) & 7) << 2
 // One operand's slab: 64 rows (M or N index) from i0, k from k0.  KMAJ: element
 // (i, k) at i * ld + k, else at k * ld + i.  VEC: 16-byte loads (ld % 4 == 0 and
 // an aligned base, so a group of four is inside or outside as a whole).
-template <bool KMAJ, bool VEC, typename T>
-__device__ __forceinline__ void load_slab(const T* __restrict__ X, int64_t ld, int i0, int I, int k0,
+template <bool KMAJ, bool VEC>
+__device__ __forceinline__ void load_slab(const float* __restrict__ X, int64_t ld, int i0, int I, int k0,
                                           int K, float (&r)[4 * LD4]) {
   const int t = threadIdx.x;
 #pragma unroll
   for (int j = 0; j < LD4; ++j) {
     const int i = i0 + (KMAJ ? t / (TK / 4) + F_THREADS / (TK / 4) * j : (t & 15) * 4);
     const int k = k0 + (KMAJ ? t % (TK / 4) * 4 : (t >> 4) + F_THREADS / 16 * j);
-    const T* p = X + (KMAJ ? static_cast<int64_t>(i) * ld + k : static_cast<int64_t>(k) * ld + i);
+    const float* p = X + (KMAJ ? static_cast<int64_t>(i) * ld + k : static_cast<int64_t>(k) * ld + i);
     if constexpr (VEC) {
       const float4 v = i < I && k < K ? __ldg(reinterpret_cast<const float4*>(p)) : make_float4(0.f, 0.f, 0.f, 0.f);
       r[4 * j] = v.x; r[4 * j + 1] = v.y; r[4 * j + 2] = v.z; r[4 * j + 3] = v.w;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        r[4 * j + e] = (KMAJ ? i < I && k + e < K : i + e < I && k < K) ? to_f32<T>(__ldg(p + e)) : 0.f;
+        r[4 * j + e] = (KMAJ ? i < I && k + e < K : i + e < I && k < K) ? __ldg(p + e) : 0.f;
     }
   }
 }
@@ -68,8 +67,8 @@ __device__ __forceinline__ void store_slab(float* s, const float (&r)[4 * LD4]) 
 // The tile at (m0, n0) over the slabs [s0, s1) of the sum, one of `ks` splits over a cluster:
 // finish(m, n, value) is called once for every element of the tile, those outside the
 // matrix included.  Each CTA of a split first says that it runs (cluster_arrive).
-template <bool AK, bool BK, bool VEC, typename T, typename F>
-__device__ __forceinline__ void f32_tile(const F32Operands<T>& o, int m0, int n0, int ks, int split, int s0, int s1,
+template <bool AK, bool BK, bool VEC, typename F>
+__device__ __forceinline__ void f32_tile(const F32Operands& o, int m0, int n0, int ks, int split, int s0, int s1,
                                          const F& finish) {
   __shared__ __align__(16) float sm[2][2][TK * 64];  // [buffer][A, B]; later, unsplit, the 64 x 64 tile
   __shared__ __align__(16) float recv[TM * TN];      // split: this CTA's rows from every split

@@ -35,6 +35,10 @@ sky_status launch_bf16(sky_gemm_form form, int M, int N, int K, const void* A, c
 // 2-D bf16 tensor map over a row-major [rows, cols] matrix, box {64, box_rows},
 // 128-byte swizzle; out-of-range elements read as zero.
 bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int box_rows);
+// The same over `mats` such matrices, one after the other (bf16, or fp32), box {box_cols,
+// box_rows, 1} of 128 bytes a row: what is behind a matrix's rows reads as zero too.
+bool make_map_3d(CUtensorMap* map, const void* base, int64_t mats, int64_t rows, int64_t cols, int box_rows, int box_cols,
+                 bool f32);
 
 // The cluster kernel (gemm_cluster.cu): tiles of 128 x bn (pair: 256 x bn on an
 // SM pair), each tile's k-blocks split over ks CTAs (pairs) of one cluster.

@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(F_THREADS) gemm_f32_kernel(const F32Params p) 
     }
     p.C[off] = v;
   };
-  f32_tile<AK, BK, VEC>(F32Operands<float>{p.A, p.B, p.lda, p.ldb, p.M, p.N, p.K}, m0, n0, p.ks, split, s0, s1, finish);
+  f32_tile<AK, BK, VEC>(F32Operands{p.A, p.B, p.lda, p.ldb, p.M, p.N, p.K}, m0, n0, p.ks, split, s0, s1, finish);
 }
 }  // namespace
 

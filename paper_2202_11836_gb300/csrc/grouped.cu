@@ -18,8 +18,8 @@ sky_status check(const sky_grouped_shape* s, bool weights) {
   SKY_CHECK(s, SKY_ERR_INVALID_ARG, "null shape");
   SKY_CHECK(s->groups > 0 && s->rows > 0 && s->out > 0 && (!weights || s->in > 0), SKY_ERR_INVALID_ARG, "bad sizes");
   SKY_CHECK(s->dtype == SKY_DTYPE_BF16 || s->dtype == SKY_DTYPE_FP32, SKY_ERR_INVALID_ARG, "unknown dtype");
-  SKY_CHECK(s->groups <= MAX_GROUPS && s->rows < (1 << 30) && s->out <= (1 << 20) && (!weights || s->in <= (1 << 20)),
-            SKY_ERR_UNSUPPORTED, "more than %d groups, 2^30 rows or more, or weights wider than 2^20", MAX_GROUPS);
+  SKY_CHECK(s->groups <= MAX_GROUPS && s->rows < (1 << 28) && s->out <= (1 << 20) && (!weights || s->in <= (1 << 20)),
+            SKY_ERR_UNSUPPORTED, "more than %d groups, 2^28 rows or more, or weights wider than 2^20", MAX_GROUPS);
   if (weights) {
     SKY_CHECK(s->dtype == SKY_DTYPE_FP32 || (s->out % 8 == 0 && s->in % 8 == 0), SKY_ERR_UNSUPPORTED,
               "bf16 grouped products need weights of multiples of 8 (got %d x %d)", s->out, s->in);
@@ -133,7 +133,7 @@ sky_status sky_grouped_gemm(sky_gemm_form form, const sky_grouped_shape* shape, 
   const grouped::Call c{form, shape->groups, shape->rows, shape->out, shape->in, d_offset, A, B, C, epilogue, bias, aux,
                         aux_out, workspace, workspace_bytes, d_status};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return bf16 ? grouped::launch_simt<__nv_bfloat16>(c, st) : grouped::launch_simt<float>(c, st);
+  return bf16 ? grouped::launch_tc(c, st) : grouped::launch_simt(c, st);
   ABI_GUARD_END
 }
 

@@ -27,8 +27,9 @@ struct Call {
 };
 
 // fp32 arithmetic on the CUDA cores (grouped_f32.cu).
-template <typename T>
 sky_status launch_simt(const Call& c, cudaStream_t st);
+// bf16 on the tensor cores (grouped_tc.cu).
+sky_status launch_tc(const Call& c, cudaStream_t st);
 
 }  // namespace grouped
 }  // namespace sky

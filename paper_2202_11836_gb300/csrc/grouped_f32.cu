@@ -2,9 +2,7 @@
 // each over the rows of one group.  Bound as those are, by the FMA pipe or, with few rows, by
 // the latency of a slab; the number of tiles is known on the device only, so the grid holds as
 // many as the rows may make and those that are too many leave at once.
-#include <cuda_fp16.h>
-
-#include <type_traits>
+#include <algorithm>
 
 #include "common.cuh"
 #include "f32_tile.cuh"
@@ -26,23 +24,14 @@ struct Params {
   int m_tiles, n_tiles, ks;  // m_tiles: XTW only
 };
 
-// GELU' is kept as the dense products keep it: fp16 beside bf16, else fp32.
-template <typename T> struct Slope { using type = float; };
-template <> struct Slope<__nv_bfloat16> { using type = __half; };
-__device__ __forceinline__ float slope_value(float s) { return s; }
-__device__ __forceinline__ float slope_value(__half s) { return __half2float(s); }
-__device__ __forceinline__ void set_slope(float* s, float v) { *s = v; }
-__device__ __forceinline__ void set_slope(__half* s, float v) { *s = __float2half_rn(v); }
-
-template <typename T, int FORM, bool VEC>
-__global__ void __launch_bounds__(F_THREADS) grouped_simt(const __grid_constant__ Params p) {
-  using S = typename Slope<T>::type;
+template <int FORM, bool VEC>
+__global__ void __launch_bounds__(F_THREADS, 4) grouped_simt(const __grid_constant__ Params p) {
   const Call& c = p.c;
   pdl_wait();
   const int split = static_cast<int>(blockIdx.x) % p.ks, tile = static_cast<int>(blockIdx.x) / p.ks;
   if (blockIdx.x == 0) check_offsets(c.offset, c.groups, c.rows, c.status);
-  const T *A = static_cast<const T*>(c.A), *B = static_cast<const T*>(c.B);
-  gemm::F32Operands<T> o;
+  const float *A = static_cast<const float*>(c.A), *B = static_cast<const float*>(c.B);
+  gemm::F32Operands o;
   int m0, n0, g;
   int64_t row0 = 0;
   if constexpr (FORM == SKY_GEMM_XTW) {
@@ -72,19 +61,19 @@ __global__ void __launch_bounds__(F_THREADS) grouped_simt(const __grid_constant_
       static_cast<float*>(c.C)[(static_cast<int64_t>(g) * c.out + m) * c.in + n] = v;
     } else {
       const int64_t off = (row0 + m) * o.N + n;
-      if (FORM == SKY_GEMM_XWT && c.bias) v += to_f32<T>(static_cast<const T*>(c.bias)[static_cast<int64_t>(g) * c.out + n]);
-      if (c.epi == SKY_EPI_GELU_BWD) v *= slope_value(static_cast<const S*>(c.aux)[off]);
+      if (FORM == SKY_GEMM_XWT && c.bias) v += static_cast<const float*>(c.bias)[static_cast<int64_t>(g) * c.out + n];
+      if (c.epi == SKY_EPI_GELU_BWD) v *= static_cast<const float*>(c.aux)[off];
       if (c.epi == SKY_EPI_BIAS_GELU) {
-        set_slope(static_cast<S*>(c.aux_out) + off, gelu_grad_f(v));
+        static_cast<float*>(c.aux_out)[off] = gelu_grad_f(v);
         v = gelu_f(v);
       }
-      static_cast<T*>(c.C)[off] = from_f32<T>(v);
+      static_cast<float*>(c.C)[off] = v;
     }
   };
   gemm::f32_tile<FORM != SKY_GEMM_XTW, FORM == SKY_GEMM_XWT, VEC>(o, m0, n0, p.ks, split, s0, s1, finish);
 }
 
-template <typename T, int FORM>
+template <int FORM>
 sky_status launch(const Call& c, cudaStream_t st) {
   const int sms = sm_count();
   SKY_CHECK(sms > 0, SKY_ERR_CUDA, "no CUDA device");
@@ -105,29 +94,21 @@ sky_status launch(const Call& c, cudaStream_t st) {
     if (tiles * ks <= 11 * sms && slabs >= 2 * ks) p.ks = ks;
   SKY_CHECK(tiles * p.ks <= 0x7fffffff, SKY_ERR_UNSUPPORTED, "grouped product too large");
   const auto a16 = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
-  const bool vec = std::is_same<T, float>::value && c.in % 4 == 0 && c.out % 4 == 0 && a16(c.A) && a16(c.B);
+  const bool vec = c.in % 4 == 0 && c.out % 4 == 0 && a16(c.A) && a16(c.B);
   const dim3 grid(static_cast<unsigned>(tiles * p.ks));
-  cudaError_t e;
-  if constexpr (std::is_same<T, float>::value) {
-    e = vec ? launch_pdl(grouped_simt<T, FORM, true>, grid, dim3(F_THREADS), 0, st, p.ks, p)
-            : launch_pdl(grouped_simt<T, FORM, false>, grid, dim3(F_THREADS), 0, st, p.ks, p);
-  } else {
-    e = launch_pdl(grouped_simt<T, FORM, false>, grid, dim3(F_THREADS), 0, st, p.ks, p);
-  }
+  const cudaError_t e = vec ? launch_pdl(grouped_simt<FORM, true>, grid, dim3(F_THREADS), 0, st, p.ks, p)
+                            : launch_pdl(grouped_simt<FORM, false>, grid, dim3(F_THREADS), 0, st, p.ks, p);
   count_launches(1);
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "grouped product launch");
 }
 
 }  // namespace
 
-template <typename T>
 sky_status launch_simt(const Call& c, cudaStream_t st) {
-  if (c.form == SKY_GEMM_XWT) return launch<T, SKY_GEMM_XWT>(c, st);
-  if (c.form == SKY_GEMM_XW) return launch<T, SKY_GEMM_XW>(c, st);
-  return launch<T, SKY_GEMM_XTW>(c, st);
+  if (c.form == SKY_GEMM_XWT) return launch<SKY_GEMM_XWT>(c, st);
+  if (c.form == SKY_GEMM_XW) return launch<SKY_GEMM_XW>(c, st);
+  return launch<SKY_GEMM_XTW>(c, st);
 }
-template sky_status launch_simt<float>(const Call&, cudaStream_t);
-template sky_status launch_simt<__nv_bfloat16>(const Call&, cudaStream_t);
 
 }  // namespace grouped
 }  // namespace sky

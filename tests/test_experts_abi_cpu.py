@@ -129,7 +129,7 @@ XWT, XW, XTW = L.SKY_GEMM_XWT, L.SKY_GEMM_XW, L.SKY_GEMM_XTW
 GROUPED_REFUSED = [
     (dict(groups=0), INVALID), (dict(rows=0), INVALID), (dict(out=0), INVALID), (dict(in_=0), INVALID),
     (dict(in_=-8), INVALID), (dict(dtype=5), INVALID), (dict(out=60), UNSUPPORTED), (dict(in_=36), UNSUPPORTED),
-    (dict(groups=1025), UNSUPPORTED), (dict(rows=1 << 30), UNSUPPORTED), (dict(out=(1 << 20) + 8), UNSUPPORTED),
+    (dict(groups=1025), UNSUPPORTED), (dict(rows=1 << 28), UNSUPPORTED), (dict(out=(1 << 20) + 8), UNSUPPORTED),
     (dict(in_=(1 << 20) + 8), UNSUPPORTED),
 ]
 
