@@ -40,6 +40,9 @@ bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, in
 bool make_map_3d(CUtensorMap* map, const void* base, int64_t mats, int64_t rows, int64_t cols, int box_rows, int box_cols,
                  bool f32);
 
+// 2-D map for storing a 16-bit [rows, cols] (fp16 or bf16), box {32, 32}, 64-byte swizzle.
+bool make_store_map(CUtensorMap* map, void* base, int64_t rows, int64_t cols, bool half);
+
 // The cluster kernel (gemm_cluster.cu): tiles of 128 x bn (pair: 256 x bn on an
 // SM pair), each tile's k-blocks split over ks CTAs (pairs) of one cluster.
 struct ClusterPlan {

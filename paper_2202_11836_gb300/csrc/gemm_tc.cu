@@ -680,9 +680,8 @@ bool make_map_3d(CUtensorMap* map, const void* base, int64_t mats, int64_t rows,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-namespace {
-// 2-D map of a 16-bit output [rows, cols] for the bias+GELU epilogue's stores:
-// box {32, 32}, 64-byte swizzle; elements outside are not written.
+// 2-D map of a 16-bit output [rows, cols] for the epilogues' stores: box {32, 32},
+// 64-byte swizzle; elements outside are not written.
 bool make_store_map(CUtensorMap* map, void* base, int64_t rows, int64_t cols, bool half) {
   auto fn = encode_fn();
   if (!fn) return false;
@@ -695,6 +694,7 @@ bool make_store_map(CUtensorMap* map, void* base, int64_t rows, int64_t cols, bo
             CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+namespace {
 // Launches the product's work units on a persistent grid: one CTA per SM, or
 // for the pair variant one two-CTA cluster per SM pair, capped by how many
 // such clusters the device holds at once (a single wave).

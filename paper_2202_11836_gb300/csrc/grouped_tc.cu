@@ -9,10 +9,10 @@
 //   warp 0      TMA producer into a ring of 64-deep stages (weights 128 rows a CTA, half of the
 //               tile's tokens a CTA, in the smallest box of 16, 32, 64 or 128 rows that has them)
 //   warp 1      MMA issuer of the pair's leader; two accumulators of 256 TMEM columns
-//   warps 2..   epilogue: features are TMEM lanes and tokens columns, so a row of the output
+//   warps 2..9  epilogue: features are TMEM lanes and tokens columns, so a row of the output
 //               lies across lanes.  16x256b loads put it into the layout of an mma.sync
 //               accumulator, whose 16-bit pairs stmatrix writes transposed: 32 tokens by 32
-//               features in shared memory, read back and stored 64 bytes a row.
+//               features in shared memory, which TMA stores.
 // XTW (weight gradients) sums over the rows of a group: 256 x 256 tiles on a pair, K the rows in
 // blocks of 64.  The last block's steps of 16 may reach into the next group's rows; there a warp
 // clears them in shared memory between the copy and the product, in both operands, since what
@@ -38,27 +38,26 @@ constexpr int BM = 128, BK = 64;             // of a CTA: features; K of a stage
 constexpr int TILE_M = 2 * BM, TILE_N = 256; // of a pair
 constexpr int A_BYTES = BM * BK * 2, B_BYTES = TILE_N / 2 * BK * 2, SBYTES = A_BYTES + B_BYTES;
 constexpr int CHUNK_BYTES = 64 * BK * 2;     // one 64-wide MN-major box
-constexpr int MAX_STAGES = 6;
 constexpr uint64_t WAIT_NS = 2000000000ull;  // of any one wait
 constexpr uint32_t SLEEP_NS = 20000;         // suspend hint of the epilogue's accumulator wait
 
-// Launch shape: the GELU epilogue is bound by its arithmetic and takes 16 warps, and stages
-// two outputs, for a stage less.
+// Launch shape of XWT and XW: eight epilogue warps, each with two staging buffers of 32 x 32 16-bit
+// values (of GELU's two outputs: two pairs, for a stage less).
 template <int EPI>
 struct Shape {
   static constexpr bool GELU = EPI == SKY_EPI_BIAS_GELU;
-  static constexpr int EW = GELU ? 16 : 8;                 // epilogue warps
-  static constexpr int STAGES = GELU ? 5 : MAX_STAGES;
-  static constexpr int STAGING = GELU ? 4096 : 2048;       // of an epilogue warp: 32 x 32 values, one or two
+  static constexpr int EW = 8, STAGES = GELU ? 5 : 6;
+  static constexpr int BUFFER = GELU ? 4096 : 2048, STAGING = 2 * BUFFER;  // of an epilogue warp
   static constexpr int THREADS = 64 + 32 * EW;
   static constexpr int EPI_OFF = STAGES * SBYTES;
   static constexpr int BAR_OFF = EPI_OFF + EW * STAGING;
   static constexpr int SMEM = BAR_OFF + 256 + 1024;
   static_assert(SMEM <= 232448, "shared memory per CTA");
 };
-// Weight gradients: eight epilogue warps with a 32 x 32 fp32 box each, and the clearing warp.
+// Weight gradients: eight epilogue warps with a box of 32 rows by 32 fp32 each, and the
+// clearing warp.
 struct GradShape {
-  static constexpr int EW = 8, STAGES = MAX_STAGES, STAGING = 4096;
+  static constexpr int EW = 8, STAGES = 6, STAGING = 4096;
   static constexpr int THREADS = 96 + 32 * EW;
   static constexpr int EPI_OFF = STAGES * SBYTES;
   static constexpr int BAR_OFF = EPI_OFF + EW * STAGING;
@@ -78,8 +77,12 @@ struct Params {
   int32_t* status;
 };
 struct Maps {
-  CUtensorMap weights;
+  CUtensorMap weights, C, aux_out;
   CUtensorMap rows[4];  // boxes of 16, 32, 64 and 128 rows
+};
+
+struct Tile {
+  int group, row, count;  // first row, rows
 };
 
 // Finds tiles in ascending order; every lane of a warp calls it.
@@ -87,7 +90,7 @@ struct Walk {
   const int32_t* offset;
   int groups, rows, g0 = 0, before = 0, total = 0;
   int lo = 0, hi = 0, n = 0, upto = 0;  // of group g0 + lane
-  __device__ Walk(const int32_t* o, int g, int r) : offset(o), groups(g), rows(r) { load(); }
+  __device__ __forceinline__ Walk(const int32_t* o, int g, int r) : offset(o), groups(g), rows(r) { load(); }
   __device__ __forceinline__ void load() {
     const int lane = threadIdx.x & 31;
     int2 r = make_int2(0, 0);
@@ -102,8 +105,8 @@ struct Walk {
     }
     total = __shfl_sync(0xffffffffu, upto, 31);
   }
-  // The j-th tile of tokens: group, first row, rows; false behind the last.
-  __device__ __forceinline__ bool find(int j, int& group, int& row, int& count) {
+  // The j-th tile of tokens; false behind the last.
+  __device__ __forceinline__ bool find(int j, Tile& t) {
     while (j >= before + total) {
       before += total;
       g0 += 32;
@@ -115,9 +118,9 @@ struct Walk {
     const int a = __shfl_sync(0xffffffffu, lo, at), b = __shfl_sync(0xffffffffu, hi, at);
     const int tiles = __shfl_sync(0xffffffffu, n, at), tile = j - before - __shfl_sync(0xffffffffu, upto - n, at);
     const int each = ((b - a + tiles - 1) / tiles + 31) & ~31;  // equal tiles; at most TILE_N
-    group = g0 + at;
-    row = a + tile * each;
-    count = min(each, b - row);
+    t.group = g0 + at;
+    t.row = a + tile * each;
+    t.count = min(each, b - t.row);
     return true;
   }
 };
@@ -148,7 +151,7 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&tfull[a], 1);
-      ptx::mbar_init(&tempty[a], 2 * 32 * EW);
+      ptx::mbar_init(&tempty[a], 2 * EW);
     }
     ptx::mbar_init(done, 1);
     ptx::fence_mbar_init_cluster();
@@ -168,18 +171,18 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
   if (blockIdx.x == 0) check_offsets(p.offset, p.groups, p.rows, p.status);
 
   Walk walk(p.offset, p.groups, p.rows);
-  int group, row, count;
+  Tile t;
   if (warp == 0) {
     const bool issuer = ptx::elect_one();
     int stage = 0, issued = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int u = cid; ok && walk.find(u / p.f_blocks, group, row, count); u += ncl) {
+    for (int u = cid; ok && walk.find(u / p.f_blocks, t); u += ncl) {
       const int f0 = u % p.f_blocks * TILE_M + static_cast<int>(rank) * BM;
-      const int half = ((count + 31) & ~31) / 2;  // tokens whose rows this CTA loads
+      const int half = ((t.count + 31) & ~31) / 2;  // tokens whose rows this CTA loads
       const int box = half <= 16 ? 0 : half <= 32 ? 1 : half <= 64 ? 2 : 3;
       const uint32_t bytes = 2 * (A_BYTES + (16 << box) * BK * 2);
-      const int r0 = row + static_cast<int>(rank) * half;
+      const int r0 = t.row + static_cast<int>(rank) * half;
       for (int kb = 0; kb < p.k_blocks; ++kb) {
         ok = __all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, WAIT_NS, p.status));
         if (!ok) break;
@@ -189,10 +192,10 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
           const uint32_t bar = ptx::mapa_shared(ptx::smem_u32(&full[stage]), 0);
           const int k0 = kb * BK;
           if (W_MN) {
-            ptx::tma_load_3d_pair(sa, &maps.weights, bar, f0, k0, group);
-            ptx::tma_load_3d_pair(sa + CHUNK_BYTES, &maps.weights, bar, f0 + 64, k0, group);
+            ptx::tma_load_3d_pair(sa, &maps.weights, bar, f0, k0, t.group);
+            ptx::tma_load_3d_pair(sa + CHUNK_BYTES, &maps.weights, bar, f0 + 64, k0, t.group);
           } else {
-            ptx::tma_load_3d_pair(sa, &maps.weights, bar, k0, f0, group);
+            ptx::tma_load_3d_pair(sa, &maps.weights, bar, k0, f0, t.group);
           }
           ptx::tma_load_2d_pair(sa + A_BYTES, &maps.rows[box], bar, k0, r0);
         }
@@ -217,9 +220,9 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
       int stage = 0, acc = 0;
       uint32_t phase = 0, aphase = 0;
       bool ok = true;
-      for (int u = cid; ok && walk.find(u / p.f_blocks, group, row, count); u += ncl) {
+      for (int u = cid; ok && walk.find(u / p.f_blocks, t); u += ncl) {
         const uint32_t idesc =
-            ptx::idesc_bf16_f32(TILE_M, 0, W_MN, false) | static_cast<uint32_t>(((count + 31) & ~31) >> 3) << 17;
+            ptx::idesc_bf16_f32(TILE_M, 0, W_MN, false) | static_cast<uint32_t>(((t.count + 31) & ~31) >> 3) << 17;
         if (!__all_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aphase ^ 1u, WAIT_NS, p.status))) break;
         ptx::tc_fence_after();
         const uint32_t d_tmem = tmem_base + acc * TILE_N;
@@ -248,17 +251,38 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
       ptx::mbar_wait(done, 0, WAIT_NS, p.status);
     }
   } else {
-    // Warp w has TMEM lanes 32 q .. (features) and every (EW / 4)-th chunk of 32 tokens.
+    // Warp w has TMEM lanes 32 q .. (features) and every (EW / 4)-th chunk of 32 tokens.  One lane
+    // hands the accumulator back once the last chunk is in registers.
     constexpr int PARTS = EW / 4, CHUNKS = TILE_N / 32 / PARTS;
     const int q = warp & 3, part = (warp - 2) >> 2;
-    const uint32_t stage = ptx::smem_u32(smem + SH::EPI_OFF + (warp - 2) * SH::STAGING);
-    // 16-byte piece i of token row t of the staging: 64 bytes a row, pieces swizzled
-    const auto piece_at = [&](int t, int i) { return stage + t * 64 + ((i ^ ((t >> 1) & 3)) << 4); };
+    uint8_t* const staging = smem + SH::EPI_OFF + (warp - 2) * SH::STAGING;
+    // 16-byte piece i of token row t of a staging buffer: 64 bytes a row, swizzled as TMA wants it
+    const auto piece_at = [](uint32_t buffer, int t, int i) { return buffer + t * 64 + ((i ^ ((t >> 1) & 3)) << 4); };
+    const int t_at = lane >> 2, f_lane = (lane & 3) * 8;  // where rows are moved by lanes: token of eight, features
+    int turn = 0;  // staging buffer
     int acc = 0;
     uint32_t aphase = 0;
-    for (int u = cid; walk.find(u / p.f_blocks, group, row, count); u += ncl) {
-      const int f0 = u % p.f_blocks * TILE_M + static_cast<int>(rank) * BM + q * 32;
-      const int t_at = lane >> 2, f_at = f0 + (lane & 3) * 8;  // this lane's token of eight, and its features, at the stores
+    // the tile that comes, and its bias at features lane / 4 + 8 i, one tile ahead
+    Tile next;
+    float next_bias[4] = {};
+    const auto look = [&](int u) {
+      if (!walk.find(u / p.f_blocks, next)) return false;
+      if (EPI != SKY_EPI_GELU_BWD && p.bias) {
+        const int f0 = u % p.f_blocks * TILE_M + static_cast<int>(rank) * BM + q * 32 + (lane >> 2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          next_bias[i] = f0 + 8 * i < p.features
+                             ? __bfloat162float(p.bias[static_cast<int64_t>(next.group) * p.features + f0 + 8 * i]) : 0.f;
+      }
+      return true;
+    };
+    bool more = look(cid);
+    for (int u = cid; more; u += ncl) {
+      t = next;
+      float bias[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bias[i] = next_bias[i];
+      const int f0 = u % p.f_blocks * TILE_M + static_cast<int>(rank) * BM + q * 32, f_at = f0 + f_lane;
       const bool f_ok = f_at < p.features;
       uint4 pre[EPI == SKY_EPI_GELU_BWD ? CHUNKS : 1][4];
       if constexpr (EPI == SKY_EPI_GELU_BWD) {  // the tile's GELU', before the accumulator is waited for
@@ -266,48 +290,60 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
         for (int cc = 0; cc < CHUNKS; ++cc)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int t = (cc * PARTS + part) * 32 + 8 * i + t_at;
-            pre[cc][i] = f_ok && t < count ? __ldg(reinterpret_cast<const uint4*>(
-                                                 p.aux + static_cast<int64_t>(row + t) * p.features + f_at))
-                                           : make_uint4(0u, 0u, 0u, 0u);
+            const int n = (cc * PARTS + part) * 32 + 8 * i + t_at;
+            pre[cc][i] = f_ok && n < t.count ? __ldg(reinterpret_cast<const uint4*>(
+                                                   p.aux + static_cast<int64_t>(t.row + n) * p.features + f_at))
+                                             : make_uint4(0u, 0u, 0u, 0u);
           }
       }
-      float bias[4] = {};  // of features f0 + lane / 4 + 8 i
-      if (EPI != SKY_EPI_GELU_BWD && p.bias) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int f = f0 + (lane >> 2) + 8 * i;
-          if (f < p.features) bias[i] = __bfloat162float(p.bias[static_cast<int64_t>(group) * p.features + f]);
-        }
-      }
+      more = look(u + ncl);
       if (!__all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, WAIT_NS, p.status, SLEEP_NS))) break;
       ptx::tc_fence_after();
       const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * TILE_N;
+      // of a chunk's 8 tokens b: r[4 b ..] features lane / 4 and + 8, r[16 + 4 b ..] + 16 and + 24;
+      // a chunk ahead
+      uint32_t r[2][32];
+      const auto load = [&](int cc) {
+        const int t0 = (cc * PARTS + part) * 32;
+        if (t0 >= t.count) return;  // warp-uniform
+        ptx::tmem_ld_16x256b_x4(taddr + t0, r[cc & 1]);
+        ptx::tmem_ld_16x256b_x4(taddr + t0 + (16u << 16), r[cc & 1] + 16);
+      };
+      load(0);
 #pragma unroll
       for (int cc = 0; cc < CHUNKS; ++cc) {
         const int t0 = (cc * PARTS + part) * 32;
-        if (t0 >= count) break;  // warp-uniform
-        uint32_t r[32];  // 8 tokens b: r[4 b ..] features lane / 4, + 8; r[16 + 4 b ..] + 16, + 24
-        ptx::tmem_ld_16x256b_x4(taddr + t0, r);
-        ptx::tmem_ld_16x256b_x4(taddr + t0 + (16u << 16), r + 16);
-        uint32_t sl[4][4];  // GELU' in the same layout
+        ptx::tmem_ld_wait();
+        if (cc + 1 < CHUNKS) {
+          load(cc + 1);
+        } else {  // the accumulator is in registers
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive_cluster_relaxed(ptx::mapa_shared(ptx::smem_u32(&tempty[acc]), 0));
+          if (++acc == 2) { acc = 0; aphase ^= 1u; }
+        }
+        if (t0 >= t.count) continue;
+        uint8_t* const box = staging + turn * SH::BUFFER;
+        const uint32_t buffer = ptx::smem_u32(box);
+        if (lane == 0) ptx::bulk_wait_group_read<1>();  // what was stored from here has left it
+        __syncwarp();
+        uint32_t sl[4][4];  // GELU' in the accumulator's layout
         if constexpr (EPI == SKY_EPI_GELU_BWD) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            ptx::st_shared_v4(piece_at(8 * i + t_at, lane & 3), pre[cc][i].x, pre[cc][i].y, pre[cc][i].z, pre[cc][i].w);
+            ptx::st_shared_v4(piece_at(buffer, 8 * i + t_at, lane & 3), pre[cc][i].x, pre[cc][i].y, pre[cc][i].z, pre[cc][i].w);
           __syncwarp();
 #pragma unroll
-          for (int b = 0; b < 4; ++b) ptx::ldmatrix_x4_trans(piece_at(8 * b + (lane & 7), lane >> 3), sl[b]);
+          for (int b = 0; b < 4; ++b) ptx::ldmatrix_x4_trans(piece_at(buffer, 8 * b + (lane & 7), lane >> 3), sl[b]);
           __syncwarp();
         }
-        ptx::tmem_ld_wait();
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           uint32_t o[4], x[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int at = (i >> 1) * 16 + 4 * b + (i & 1) * 2;
-            float v0 = __uint_as_float(r[at]), v1 = __uint_as_float(r[at + 1]);
+            float v0 = __uint_as_float(r[cc & 1][at]), v1 = __uint_as_float(r[cc & 1][at + 1]);
             if constexpr (EPI == SKY_EPI_GELU_BWD) {
               const float2 s = __half22float2(*reinterpret_cast<const __half2*>(&sl[b][i]));
               v0 *= s.x;
@@ -326,31 +362,39 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
               o[i] = ptx::pack_bf16(v0, v1);
             }
           }
-          const uint32_t to = piece_at(8 * b + (lane & 7), lane >> 3);
+          const uint32_t to = piece_at(buffer, 8 * b + (lane & 7), lane >> 3);
           ptx::stmatrix_x4_trans(to, o[0], o[1], o[2], o[3]);
           if constexpr (EPI == SKY_EPI_BIAS_GELU) ptx::stmatrix_x4_trans(to + 2048, x[0], x[1], x[2], x[3]);
         }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = 8 * i + t_at;
-          uint32_t v[4];
-          ptx::ld_shared_v4(piece_at(t, lane & 3), v);
-          const bool in = f_ok && t0 + t < count;
-          const int64_t off = static_cast<int64_t>(row + t0 + t) * p.features + f_at;
-          if (in) *reinterpret_cast<uint4*>(p.C + off) = make_uint4(v[0], v[1], v[2], v[3]);
-          if constexpr (EPI == SKY_EPI_BIAS_GELU) {
-            ptx::ld_shared_v4(piece_at(t, lane & 3) + 2048, v);
-            if (in) *reinterpret_cast<uint4*>(p.aux_out + off) = make_uint4(v[0], v[1], v[2], v[3]);
+        if (t0 + 32 <= t.count) {  // all of its tokens are the group's: by TMA, which leaves out what is behind the features
+          ptx::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0 && f0 < p.features) {
+            ptx::tma_store_2d(&maps.C, box, f0, t.row + t0);
+            if constexpr (EPI == SKY_EPI_BIAS_GELU) ptx::tma_store_2d(&maps.aux_out, box + 2048, f0, t.row + t0);
           }
+        } else {
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int n = 8 * i + t_at;
+            uint32_t v[4];
+            const bool in = f_ok && t0 + n < t.count;
+            const int64_t off = static_cast<int64_t>(t.row + t0 + n) * p.features + f_at;
+            ptx::ld_shared_v4(piece_at(buffer, n, lane & 3), v);
+            if (in) *reinterpret_cast<uint4*>(p.C + off) = make_uint4(v[0], v[1], v[2], v[3]);
+            if constexpr (EPI == SKY_EPI_BIAS_GELU) {
+              ptx::ld_shared_v4(piece_at(buffer, n, lane & 3) + 2048, v);
+              if (in) *reinterpret_cast<uint4*>(p.aux_out + off) = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+          }
+          __syncwarp();  // before lane 0 goes on to say that the buffer is free
         }
-        __syncwarp();
+        if (lane == 0) ptx::bulk_commit_group();  // (an empty one behind stores by lanes)
+        turn ^= 1;
       }
-      ptx::tc_fence_before();
-      if (leader) ptx::mbar_arrive(&tempty[acc]);
-      else ptx::mbar_arrive_cluster(ptx::mapa_shared(ptx::smem_u32(&tempty[acc]), 0));
-      if (++acc == 2) { acc = 0; aphase ^= 1u; }
     }
+    if (lane == 0) ptx::bulk_wait_group_read0();  // before the CTA's memory goes
   }
   pdl_trigger();
   ptx::tc_fence_before();
@@ -362,9 +406,40 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
   }
 }
 
+// Rows of a group whose products one accumulator takes: the tensor cores cut off where they
+// add up, so a long sum is made of parts, added in fp32 in the epilogue's registers.
+constexpr int PART_ROWS = 512;
+
+// The groups by size, largest first, for up to 32 of them (lane g holds group g's rank, and the
+// group of rank g); the pairs take the tiles of such a list to and fro, so that none gets the
+// larger ones of every round.  More groups come in their own order.
+struct BySize {
+  bool sorted;
+  int at_rank = 0;
+  __device__ __forceinline__ BySize(const int32_t* offset, int groups, int rows) : sorted(groups <= 32) {
+    if (!sorted) return;
+    const int lane = threadIdx.x & 31;
+    int2 r = make_int2(0, -1);
+    if (lane < groups) r = group_rows(offset, lane, rows);
+    const int size = r.y - r.x;
+    int rank = 0;
+#pragma unroll
+    for (int o = 0; o < 32; ++o) {
+      const int other = __shfl_sync(0xffffffffu, size, o);
+      rank += other > size || (other == size && o < lane);
+    }
+#pragma unroll
+    for (int o = 0; o < 32; ++o)
+      if (__shfl_sync(0xffffffffu, rank, o) == lane) at_rank = o;
+  }
+  __device__ __forceinline__ int group(int rank) const { return sorted ? __shfl_sync(0xffffffffu, at_rank, rank) : rank; }
+};
+// The unit of a pair's i-th round.
+__device__ __forceinline__ int to_and_fro(int i, int cid, int ncl) { return i * ncl + (i & 1 ? ncl - 1 - cid : cid); }
+
 struct GradParams {
   const int32_t* offset;
-  int groups, rows;
+  int groups, rows, out, in;
   int m_blocks, n_blocks;  // 256 of out; of in
   int32_t* status;
 };
@@ -399,7 +474,7 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
     }
     for (int a = 0; a < 2; ++a) {
       ptx::mbar_init(&tfull[a], 1);
-      ptx::mbar_init(&tempty[a], 2 * 32 * EW);
+      ptx::mbar_init(&tempty[a], 2 * EW);
     }
     ptx::mbar_init(done, 1);
     ptx::fence_mbar_init_cluster();
@@ -420,13 +495,14 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
   if (blockIdx.x == 0) check_offsets(p.offset, p.groups, p.rows, p.status);
 
   const int per_group = p.m_blocks * p.n_blocks, units = p.groups * per_group;
+  const BySize by_size(p.offset, p.groups, p.rows);
   if (warp == 0) {
     const bool issuer = ptx::elect_one();
     int stage = 0, issued = 0;
     uint32_t phase = 0, here_phase = 0, by_here = 0;  // a bit a stage: parity of `here`; the last copies count there
     bool ok = true;
-    for (int u = cid; ok && u < units; u += ncl) {
-      const int2 r = group_rows(p.offset, u / per_group, p.rows);
+    for (int i = 0, u; ok && (u = to_and_fro(i, cid, ncl)) < units; ++i) {
+      const int2 r = group_rows(p.offset, by_size.group(u / per_group), p.rows);
       const int m0 = u % per_group / p.n_blocks * TILE_M + static_cast<int>(rank) * BM;
       const int n0 = u % p.n_blocks * TILE_N + static_cast<int>(rank) * (TILE_N / 2);
       for (int k0 = r.x; k0 < r.y; k0 += BK) {
@@ -476,12 +552,17 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
       int stage = 0, acc = 0;
       uint32_t phase = 0, aphase = 0, c_phase = 0;  // c_phase: a bit a stage
       bool ok = true;
-      for (int u = cid; ok && u < units; u += ncl) {
-        const int2 r = group_rows(p.offset, u / per_group, p.rows);
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aphase ^ 1u, WAIT_NS, p.status))) break;
-        ptx::tc_fence_after();
-        const uint32_t d_tmem = tmem_base + acc * TILE_N;
+      for (int i = 0, u; ok && (u = to_and_fro(i, cid, ncl)) < units; ++i) {
+        const int2 r = group_rows(p.offset, by_size.group(u / per_group), p.rows);
+        uint32_t d_tmem = 0;
         for (int k0 = r.x; k0 < r.y; k0 += BK) {
+          const bool first = (k0 - r.x) % PART_ROWS == 0;
+          if (first) {
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aphase ^ 1u, WAIT_NS, p.status));
+            if (!ok) break;
+            ptx::tc_fence_after();
+            d_tmem = tmem_base + acc * TILE_N;
+          }
           const int left = r.y - k0, steps = left < BK ? (left + 15) / 16 : BK / 16;
           bool got = ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status);
           if (left < BK && left % 16 != 0) {
@@ -496,16 +577,16 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
 #pragma unroll
             for (int kk = 0; kk < BK / 16; ++kk)
               if (kk < steps)
-                ptx::tc_mma_f16_pair(d_tmem, da + off + kk * 128, db + off + kk * 128, idesc, k0 > r.x || kk > 0);
+                ptx::tc_mma_f16_pair(d_tmem, da + off + kk * 128, db + off + kk * 128, idesc, !first || kk > 0);
             ptx::tc_commit_pair(&empty[stage], 3);
           }
-          __syncwarp();
           if (++stage == NST) { stage = 0; phase ^= 1u; }
+          if (k0 + BK >= r.y || (k0 + BK - r.x) % PART_ROWS == 0) {  // the part is complete
+            if (issuer) ptx::tc_commit_pair(&tfull[acc], 3);
+            if (++acc == 2) { acc = 0; aphase ^= 1u; }
+          }
+          __syncwarp();
         }
-        if (!ok) break;
-        if (issuer) ptx::tc_commit_pair(&tfull[acc], 3);
-        __syncwarp();
-        if (++acc == 2) { acc = 0; aphase ^= 1u; }
       }
       if (issuer) ptx::tc_commit_pair(done, 1);
       __syncwarp();
@@ -516,8 +597,8 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
     int at = 0;  // blocks so far
     uint32_t phase = 0;
     bool ok = true;
-    for (int u = cid; ok && u < units; u += ncl) {
-      const int2 r = group_rows(p.offset, u / per_group, p.rows);
+    for (int i = 0, u; ok && (u = to_and_fro(i, cid, ncl)) < units; ++i) {
+      const int2 r = group_rows(p.offset, by_size.group(u / per_group), p.rows);
       const int left = (r.y - r.x) % BK, blocks = (r.y - r.x + BK - 1) / BK;
       at += blocks;
       if (left % 16 == 0) continue;
@@ -537,42 +618,52 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
   } else {
     // Warp w has TMEM lanes 32 q .. (rows of the tile) and one half of its columns.
     const int q = warp & 3, half = (warp - 2) >> 2;
-    const uint32_t stage = ptx::smem_u32(smem + SH::EPI_OFF + (warp - 2) * SH::STAGING);
+    uint8_t* const staging = smem + SH::EPI_OFF + (warp - 2) * SH::STAGING;
     int acc = 0;
     uint32_t aphase = 0;
-    for (int u = cid; u < units; u += ncl) {
-      const int group = u / per_group;
+    bool ok = true;
+    for (int i = 0, u; ok && (u = to_and_fro(i, cid, ncl)) < units; ++i) {
+      const int group = by_size.group(u / per_group);
       const int2 rr = group_rows(p.offset, group, p.rows);
       const int m0 = u % per_group / p.n_blocks * TILE_M + static_cast<int>(rank) * BM + q * 32;
       const int n0 = u % p.n_blocks * TILE_N + half * (TILE_N / 2);
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, WAIT_NS, p.status, SLEEP_NS))) break;
-      ptx::tc_fence_after();
-      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * TILE_N + half * (TILE_N / 2);
+      float sum[4][32] = {};  // (all of it, for a group without rows)
+      for (int k0 = rr.x; k0 < rr.y; k0 += PART_ROWS) {
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, WAIT_NS, p.status, SLEEP_NS));
+        if (!ok) break;
+        ptx::tc_fence_after();
+        const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * TILE_N + half * (TILE_N / 2);
 #pragma unroll
-      for (int c = 0; c < TILE_N / 2; c += 32) {
-        uint32_t r[32];
-        ptx::tmem_ld_32x32b_x32(taddr + c, r);
-        ptx::tmem_ld_wait();
-        if (rr.x == rr.y) {  // no product was made
+        for (int c = 0; c < 8; ++c) {
+          uint32_t r[16];
+          ptx::tmem_ld_32x32b_x16(taddr + 16 * c, r);
+          ptx::tmem_ld_wait();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) r[i] = 0;
+          for (int e = 0; e < 16; ++e) sum[c >> 1][(c & 1) * 16 + e] += __uint_as_float(r[e]);
         }
-        if (lane == 0) ptx::bulk_wait_group_read0();  // the box before has left the staging
+        ptx::tc_fence_before();
         __syncwarp();
+        if (lane == 0) ptx::mbar_arrive_cluster_relaxed(ptx::mapa_shared(ptx::smem_u32(&tempty[acc]), 0));
+        if (++acc == 2) { acc = 0; aphase ^= 1u; }
+      }
+      if (!ok) break;
+#pragma unroll
+      for (int c = 0; c < TILE_N / 2 / 32; ++c) {
+        if (lane == 0) ptx::bulk_wait_group_read0();  // the box before has left the buffer
+        __syncwarp();
+        const uint32_t to = ptx::smem_u32(staging) + lane * 128;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          ptx::st_shared_v4(stage + lane * 128 + ((j ^ (lane & 7)) << 4), r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+          ptx::st_shared_v4(to + ((j ^ (lane & 7)) << 4), __float_as_uint(sum[c][4 * j]), __float_as_uint(sum[c][4 * j + 1]),
+                            __float_as_uint(sum[c][4 * j + 2]), __float_as_uint(sum[c][4 * j + 3]));
         ptx::fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) {  // (what lies outside out x in is not written)
-          ptx::tma_store_3d(&tmC, smem + SH::EPI_OFF + (warp - 2) * SH::STAGING, n0 + c, m0, group);
+        if (lane == 0) {
+          if (m0 < p.out && n0 + 32 * c < p.in)  // (what lies outside out x in is not written)
+            ptx::tma_store_3d(&tmC, staging, n0 + 32 * c, m0, group);
           ptx::bulk_commit_group();
         }
       }
-      ptx::tc_fence_before();
-      if (leader) ptx::mbar_arrive(&tempty[acc]);
-      else ptx::mbar_arrive_cluster(ptx::mapa_shared(ptx::smem_u32(&tempty[acc]), 0));
-      if (++acc == 2) { acc = 0; aphase ^= 1u; }
     }
     if (lane == 0) ptx::bulk_wait_group_read0();  // before the CTA's memory goes
   }
@@ -645,7 +736,7 @@ sky_status launch_tc(const Call& c, cudaStream_t st) {
     const bool ok = gemm::make_map(&ta, c.A, c.rows, c.out, 64) && gemm::make_map(&tb, c.B, c.rows, c.in, 64) &&
                     gemm::make_map_3d(&tc, c.C, c.groups, c.out, c.in, 32, 32, true);
     SKY_CHECK(ok, SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d x %d x %d)", c.groups, c.out, c.in);
-    const GradParams p{c.offset, c.groups, c.rows, ceil_div(c.out, TILE_M), ceil_div(c.in, TILE_N), c.status};
+    const GradParams p{c.offset, c.groups, c.rows, c.out, c.in, ceil_div(c.out, TILE_M), ceil_div(c.in, TILE_N), c.status};
     SKY_CHECK(static_cast<int64_t>(p.groups) * p.m_blocks * p.n_blocks <= 0x3fffffff, SKY_ERR_UNSUPPORTED,
               "grouped weight gradient too large");
     e = launch_grad(ta, tb, tc, p, sms, st);
@@ -670,6 +761,9 @@ sky_status launch_tc(const Call& c, cudaStream_t st) {
     Maps m;
     bool ok = gemm::make_map_3d(&m.weights, c.B, c.groups, c.out, c.in, xw ? 64 : BM, 64, false);
     for (int b = 0; b < 4; ++b) ok = ok && gemm::make_map(&m.rows[b], c.A, c.rows, p.k, 16 << b);
+    ok = ok && gemm::make_store_map(&m.C, c.C, c.rows, p.features, false);
+    if (c.epi == SKY_EPI_BIAS_GELU) ok = ok && gemm::make_store_map(&m.aux_out, c.aux_out, c.rows, p.features, true);
+    else m.aux_out = m.C;
     SKY_CHECK(ok, SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d x %d x %d)", c.groups, c.out, c.in);
     if (!xw)
       e = c.epi == SKY_EPI_BIAS_GELU ? launch_rows<false, SKY_EPI_BIAS_GELU>(m, p, units, sms, st)
