@@ -30,6 +30,9 @@ struct Call {
 sky_status launch_simt(const Call& c, cudaStream_t st);
 // bf16 on the tensor cores (grouped_tc.cu).
 sky_status launch_tc(const Call& c, cudaStream_t st);
+// The same for few rows (grouped_few.cu), and whether a call is one of those.
+bool few_pays(const Call& c, int sms);
+sky_status launch_few(const Call& c, int sms, cudaStream_t st);
 
 }  // namespace grouped
 }  // namespace sky

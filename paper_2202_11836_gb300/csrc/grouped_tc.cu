@@ -297,6 +297,14 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
           }
       }
       more = look(u + ncl);
+      if (EPI == SKY_EPI_GELU_BWD && more) {  // the next tile's, on its way into L2
+        const int f = (u + ncl) % p.f_blocks * TILE_M + static_cast<int>(rank) * BM + q * 32;
+#pragma unroll
+        for (int cc = 0; cc < CHUNKS; ++cc) {
+          const int n = (cc * PARTS + part) * 32 + lane;
+          if (f < p.features && n < next.count) ptx::prefetch_l2(p.aux + static_cast<int64_t>(next.row + n) * p.features + f);
+        }
+      }
       if (!__all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, WAIT_NS, p.status, SLEEP_NS))) break;
       ptx::tc_fence_after();
       const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * TILE_N;
@@ -730,6 +738,7 @@ cudaError_t launch_grad(const CUtensorMap& ta, const CUtensorMap& tb, const CUte
 sky_status launch_tc(const Call& c, cudaStream_t st) {
   const int sms = sm_count();
   SKY_CHECK(sms > 0, SKY_ERR_CUDA, "no CUDA device");
+  if (few_pays(c, sms)) return launch_few(c, sms, st);
   cudaError_t e;
   if (c.form == SKY_GEMM_XTW) {
     CUtensorMap ta, tb, tc;
