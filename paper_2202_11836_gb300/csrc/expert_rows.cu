@@ -2,9 +2,11 @@
 //
 // Streams bound by HBM: (1 + top_k) rows of a token are read or written once (the gradient
 // of the weighted sum: 1 + 2 top_k).  A warp takes a token's row, or a piece of it, 16
-// bytes a lane; lane c holds where choice c lies.  The loads of up to four choices are
+// bytes a lane; lane c holds where choice c lies.  The loads of two or four choices are
 // issued before the first is used.  Which rows a token names decides nothing but addresses,
 // so there are no atomics, and a sum's order is that of the choices.
+#include <algorithm>
+
 #include "../../include/sky_experts.h"
 #include "abi.h"
 #include "common.cuh"
@@ -16,7 +18,7 @@ namespace {
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int U = 2;               // 16-byte pieces of a lane
 constexpr int SEG = 32 * U;        // pieces of a warp
-constexpr int TOGETHER = 4;        // choices whose loads are in flight together
+constexpr int WIDE = 128;          // pieces that a warp of combine_backward takes, at most, while there are more warps
 constexpr int MAX_TOP_K = 32;
 
 struct Params {
@@ -94,7 +96,9 @@ __global__ void __launch_bounds__(THREADS) dispatch_rows(const Params p) {
   }
 }
 
-template <typename T, bool WEIGHTED>
+// Sums of rows.  N choices' loads are in flight together: two for up to two choices, whose smaller
+// registers leave room for more warps, else four.
+template <typename T, bool WEIGHTED, int N>
 __global__ void __launch_bounds__(THREADS) add_rows(const Params p) {
   using P = Piece<T>;
   pdl_wait();
@@ -105,11 +109,11 @@ __global__ void __launch_bounds__(THREADS) add_rows(const Params p) {
   const int place = place_of(p, t, lane);
   const float weight = WEIGHTED ? weight_of(p, t, lane) : 1.f;
   float sum[U][P::N] = {};
-  for (int c0 = 0; c0 < p.top_k; c0 += TOGETHER) {
-    uint4 v[TOGETHER][U];
-    int r[TOGETHER];
+  for (int c0 = 0; c0 < p.top_k; c0 += N) {
+    uint4 v[N][U];
+    int r[N];
 #pragma unroll
-    for (int c = 0; c < TOGETHER; ++c) {
+    for (int c = 0; c < N; ++c) {
       r[c] = c0 + c < p.top_k ? __shfl_sync(0xffffffffu, place, c0 + c) : -1;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -118,7 +122,7 @@ __global__ void __launch_bounds__(THREADS) add_rows(const Params p) {
       }
     }
 #pragma unroll
-    for (int c = 0; c < TOGETHER; ++c) {
+    for (int c = 0; c < N; ++c) {
       if (r[c] < 0) continue;
       const float w = WEIGHTED ? __shfl_sync(0xffffffffu, weight, c0 + c) : 1.f;
 #pragma unroll
@@ -137,63 +141,75 @@ __global__ void __launch_bounds__(THREADS) add_rows(const Params p) {
   }
 }
 
-// in: rows, in2: dy.  A warp takes a whole row, for its dot products.
-template <typename T>
+// in: rows, in2: dy.  W warps take a row, all of it at once where it has up to 64 W pieces, and
+// add up their parts of the dot products in order.
+template <typename T, int W, int N>
 __global__ void __launch_bounds__(THREADS) combine_backward(const Params p) {
   using P = Piece<T>;
+  constexpr int TOKENS = WARPS / W;
+  __shared__ float parts[TOKENS][W][MAX_TOP_K];
   pdl_wait();
   pdl_trigger();
-  const int t = blockIdx.x * WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (t >= p.tokens) return;
-  const int place = place_of(p, t, lane);
-  const float weight = weight_of(p, t, lane);
-  float mine = 0.f;  // lane c: its choice's dot product
-  for (int c0 = 0; c0 < p.top_k; c0 += TOGETHER) {
-    int r[TOGETHER];
-    float w[TOGETHER], dot[TOGETHER] = {};
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, local = warp / W, w = warp % W;
+  const int t = blockIdx.x * TOKENS + local;
+  if (t < p.tokens) {
+    const int place = place_of(p, t, lane);
+    const float weight = weight_of(p, t, lane);
+    float mine = 0.f;  // lane c: its choice's dot product
+    for (int c0 = 0; c0 < p.top_k; c0 += N) {
+      int r[N];
+      float wt[N], dot[N] = {};
 #pragma unroll
-    for (int c = 0; c < TOGETHER; ++c) {
-      r[c] = c0 + c < p.top_k ? __shfl_sync(0xffffffffu, place, c0 + c) : -1;
-      w[c] = __shfl_sync(0xffffffffu, weight, (c0 + c) & 31);
-    }
-    for (int i0 = lane; i0 < p.pieces; i0 += SEG) {
-      uint4 d4[U], v[TOGETHER][U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + 32 * u;
-        if (i >= p.pieces) continue;
-        d4[u] = p.in2[static_cast<int64_t>(t) * p.pieces + i];
-#pragma unroll
-        for (int c = 0; c < TOGETHER; ++c)
-          if (r[c] >= 0) v[c][u] = p.in[static_cast<int64_t>(r[c]) * p.pieces + i];
+      for (int c = 0; c < N; ++c) {
+        r[c] = c0 + c < p.top_k ? __shfl_sync(0xffffffffu, place, c0 + c) : -1;
+        wt[c] = __shfl_sync(0xffffffffu, weight, (c0 + c) & 31);
       }
+      for (int i0 = w * 32 + lane; i0 < p.pieces; i0 += U * 32 * W) {
+        uint4 d4[U], v[N][U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + 32 * u;
-        if (i >= p.pieces) continue;
-        float d[P::N];
-        P::get(d4[u], d);
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + 32 * W * u;
+          if (i >= p.pieces) continue;
+          d4[u] = p.in2[static_cast<int64_t>(t) * p.pieces + i];
 #pragma unroll
-        for (int c = 0; c < TOGETHER; ++c) {
-          if (r[c] < 0) continue;
-          float x[P::N];
-          P::get(v[c][u], x);
+          for (int c = 0; c < N; ++c)
+            if (r[c] >= 0) v[c][u] = p.in[static_cast<int64_t>(r[c]) * p.pieces + i];
+        }
 #pragma unroll
-          for (int e = 0; e < P::N; ++e) {
-            dot[c] = fmaf(x[e], d[e], dot[c]);
-            x[e] = w[c] * d[e];
+        for (int u = 0; u < U; ++u) {
+          const int i = i0 + 32 * W * u;
+          if (i >= p.pieces) continue;
+          float d[P::N];
+          P::get(d4[u], d);
+#pragma unroll
+          for (int c = 0; c < N; ++c) {
+            if (r[c] < 0) continue;
+            float x[P::N];
+            P::get(v[c][u], x);
+#pragma unroll
+            for (int e = 0; e < P::N; ++e) {
+              dot[c] = fmaf(x[e], d[e], dot[c]);
+              x[e] = wt[c] * d[e];
+            }
+            p.out[static_cast<int64_t>(r[c]) * p.pieces + i] = P::put(x);
           }
-          p.out[static_cast<int64_t>(r[c]) * p.pieces + i] = P::put(x);
         }
       }
-    }
 #pragma unroll
-    for (int c = 0; c < TOGETHER; ++c) {
-      const float s = warp_sum(dot[c]);
-      if (lane == c0 + c) mine = s;
+      for (int c = 0; c < N; ++c) {
+        const float s = warp_sum(dot[c]);
+        if (lane == c0 + c) mine = s;
+      }
     }
+    parts[local][w][lane] = mine;
   }
-  if (lane < p.top_k) p.dweight[static_cast<int64_t>(t) * p.top_k + lane] = mine;
+  __syncthreads();
+  if (t < p.tokens && w == 0 && lane < p.top_k) {
+    float s = parts[local][0][lane];
+#pragma unroll
+    for (int i = 1; i < W; ++i) s += parts[local][i][lane];
+    p.dweight[static_cast<int64_t>(t) * p.top_k + lane] = s;
+  }
 }
 
 sky_status check(const sky_rows_shape* s) {
@@ -209,12 +225,50 @@ sky_status check(const sky_rows_shape* s) {
 
 bool on(const void* p, size_t grid) { return reinterpret_cast<uintptr_t>(p) % grid == 0; }
 
-sky_status launch(const sky_rows_shape& s, Params& p, bool whole_rows, cudaStream_t st, void (*kern)(Params)) {
+using Kernel = void (*)(Params);
+
+// Warps for a row of combine_backward, up to eight: four pieces a lane of each.
+int warps_of(int pieces) {
+  int w = 1;
+  while (w < WARPS && pieces > WIDE * w) w *= 2;
+  return w;
+}
+template <typename T, int N>
+Kernel backward_of(int warps) {
+  switch (warps) {
+    case 1: return combine_backward<T, 1, N>;
+    case 2: return combine_backward<T, 2, N>;
+    case 4: return combine_backward<T, 4, N>;
+    default: return combine_backward<T, 8, N>;
+  }
+}
+template <typename T>
+Kernel backward_of(int warps, int top_k) {
+  return top_k <= 2 ? backward_of<T, 2>(warps) : backward_of<T, 4>(warps);
+}
+
+enum Kind { DISPATCH, ADD, ADD_WEIGHTED, BACKWARD };
+
+template <bool WEIGHTED>
+Kernel add_of(const sky_rows_shape& s) {
+  if (s.dtype == SKY_DTYPE_BF16)
+    return s.top_k <= 2 ? add_rows<__nv_bfloat16, WEIGHTED, 2> : add_rows<__nv_bfloat16, WEIGHTED, 4>;
+  return s.top_k <= 2 ? add_rows<float, WEIGHTED, 2> : add_rows<float, WEIGHTED, 4>;
+}
+
+sky_status launch(const sky_rows_shape& s, Params& p, Kind kind, cudaStream_t st) {
   p.tokens = s.tokens;
   p.top_k = s.top_k;
   p.pieces = s.width / (s.dtype == SKY_DTYPE_BF16 ? 8 : 4);
-  p.segs = whole_rows ? 1 : ceil_div(p.pieces, SEG);
-  const int64_t ctas = (static_cast<int64_t>(p.tokens) * p.segs + WARPS - 1) / WARPS;
+  p.segs = ceil_div(p.pieces, SEG);
+  int64_t warps = static_cast<int64_t>(p.tokens) * p.segs;
+  Kernel kern = kind == DISPATCH ? dispatch_rows : kind == ADD ? add_of<false>(s) : add_of<true>(s);
+  if (kind == BACKWARD) {
+    const int w = warps_of(p.pieces);
+    kern = s.dtype == SKY_DTYPE_BF16 ? backward_of<__nv_bfloat16>(w, s.top_k) : backward_of<float>(w, s.top_k);
+    warps = static_cast<int64_t>(p.tokens) * w;
+  }
+  const int64_t ctas = (warps + WARPS - 1) / WARPS;
   SKY_CHECK(ctas <= 0x7fffffff, SKY_ERR_UNSUPPORTED, "too many rows");
   const cudaError_t e = launch_pdl(kern, dim3(static_cast<unsigned>(ctas)), dim3(THREADS), 0, st, 1, p);
   count_launches(1);
@@ -223,11 +277,10 @@ sky_status launch(const sky_rows_shape& s, Params& p, bool whole_rows, cudaStrea
 
 // One of the two kinds of calls of a matrix, an index and a matrix.
 sky_status run(const sky_rows_shape* s, const void* in, const void* in2, const int32_t* row, const float* weight,
-               bool weighted, void* out, float* dweight, bool backward, void* stream,
-               void (*bf16)(Params), void (*fp32)(Params)) {
+               void* out, float* dweight, Kind kind, void* stream) {
   const sky_status ok = check(s);
   if (ok != SKY_OK) return ok;
-  SKY_CHECK(in && row && out && (!weighted || weight) && (!backward || (in2 && dweight)), SKY_ERR_INVALID_ARG, "null argument");
+  SKY_CHECK(in && row && out && (kind < ADD_WEIGHTED || weight) && (kind != BACKWARD || (in2 && dweight)), SKY_ERR_INVALID_ARG, "null argument");
   SKY_CHECK(on(row, 4) && on(weight, 4) && on(dweight, 4), SKY_ERR_INVALID_ARG, "row or weights off the 4-byte grid");
   SKY_CHECK(on(in, 16) && on(in2, 16) && on(out, 16), SKY_ERR_UNSUPPORTED, "matrices must be 16-byte aligned");
   Params p{};
@@ -237,7 +290,7 @@ sky_status run(const sky_rows_shape* s, const void* in, const void* in2, const i
   p.weight = weight;
   p.out = static_cast<uint4*>(out);
   p.dweight = dweight;
-  return launch(*s, p, backward, static_cast<cudaStream_t>(stream), s->dtype == SKY_DTYPE_BF16 ? bf16 : fp32);
+  return launch(*s, p, kind, static_cast<cudaStream_t>(stream));
 }
 
 }  // namespace
@@ -250,31 +303,27 @@ extern "C" {
 
 sky_status sky_dispatch_fwd(const sky_rows_shape* shape, const void* x, const int32_t* row, void* rows, void* stream) {
   ABI_GUARD_BEGIN
-  return erows::run(shape, x, nullptr, row, nullptr, false, rows, nullptr, false, stream, erows::dispatch_rows,
-                    erows::dispatch_rows);
+  return erows::run(shape, x, nullptr, row, nullptr, rows, nullptr, erows::DISPATCH, stream);
   ABI_GUARD_END
 }
 
 sky_status sky_dispatch_bwd(const sky_rows_shape* shape, const void* drows, const int32_t* row, void* dx, void* stream) {
   ABI_GUARD_BEGIN
-  return erows::run(shape, drows, nullptr, row, nullptr, false, dx, nullptr, false, stream,
-                    erows::add_rows<__nv_bfloat16, false>, erows::add_rows<float, false>);
+  return erows::run(shape, drows, nullptr, row, nullptr, dx, nullptr, erows::ADD, stream);
   ABI_GUARD_END
 }
 
 sky_status sky_combine_fwd(const sky_rows_shape* shape, const void* rows, const int32_t* row, const float* weight, void* y,
                            void* stream) {
   ABI_GUARD_BEGIN
-  return erows::run(shape, rows, nullptr, row, weight, true, y, nullptr, false, stream,
-                    erows::add_rows<__nv_bfloat16, true>, erows::add_rows<float, true>);
+  return erows::run(shape, rows, nullptr, row, weight, y, nullptr, erows::ADD_WEIGHTED, stream);
   ABI_GUARD_END
 }
 
 sky_status sky_combine_bwd(const sky_rows_shape* shape, const void* rows, const void* dy, const int32_t* row,
                            const float* weight, void* drows, float* dweight, void* stream) {
   ABI_GUARD_BEGIN
-  return erows::run(shape, rows, dy, row, weight, true, drows, dweight, true, stream,
-                    erows::combine_backward<__nv_bfloat16>, erows::combine_backward<float>);
+  return erows::run(shape, rows, dy, row, weight, drows, dweight, erows::BACKWARD, stream);
   ABI_GUARD_END
 }
 

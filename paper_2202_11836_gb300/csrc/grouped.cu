@@ -4,6 +4,7 @@
 #include "abi.h"
 #include "grouped.cuh"
 #include "grouped.h"
+#include "ptx.cuh"
 
 namespace sky {
 namespace grouped {
@@ -39,23 +40,30 @@ sky_status check_form(sky_gemm_form form, const sky_grouped_shape& s, sky_dtype 
 
 size_t workspace(sky_gemm_form, const sky_grouped_shape&) { return 16; }
 
-// Column sums over the rows of a group: a CTA takes a strip of V * 8 columns, its 32 groups of
-// eight threads every 32nd row, and the 32 sums are added in order.
-template <typename T, bool VEC>
+// Column sums over the rows of a group: TX threads take TX V columns (512 or 128 bytes of a row), the
+// others of a CTA other rows, and their sums are added in order.  A group's rows are shared by
+// the CTAs of a cluster (up to eight), whose sums the first adds in order.  Long pieces of rows read
+// faster (16384 x 4096 over 8 groups 25.4 us, in short ones 41.0); short ones make more CTAs where
+// there would be few (5000 x 768, one group, 8.6 and 5.8).
+template <typename T, bool VEC, int TX>
 __global__ void __launch_bounds__(256) column_sums(const T* __restrict__ x, const int32_t* offset, int groups, int rows, int N,
-                                                   int strips, float* out, int32_t* status) {
-  constexpr int V = VEC ? 16 / sizeof(T) : 4;
-  __shared__ float part[32][8 * V + 1];
+                                                   int strips, int parts, float* out, int32_t* status) {
+  constexpr int V = VEC ? 16 / sizeof(T) : 4, COLS = TX * V, TY = 256 / TX;
+  __shared__ __align__(16) float part[TY][COLS + (TX < 32 ? 4 : 0)];
+  __shared__ float all[8][COLS];  // of the cluster's CTAs, in the first
+  if (parts > 1) ptx::cluster_arrive();  // this CTA runs: its peers may write its shared memory
   pdl_wait();
   pdl_trigger();
   if (blockIdx.x == 0) check_offsets(offset, groups, rows, status);
-  const int g = blockIdx.x / strips, strip = blockIdx.x % strips;
-  const int cl = (threadIdx.x & 7) * V, col = strip * 8 * V + cl, rl = threadIdx.x >> 3;
+  const int mine = blockIdx.x % parts, unit = blockIdx.x / parts, g = unit / strips, strip = unit % strips;
+  const int cl = threadIdx.x % TX * V, col = strip * COLS + cl, rl = threadIdx.x / TX;
   const int2 r = group_rows(offset, g, rows);
+  const int64_t n = r.y - r.x;
+  const int lo = r.x + static_cast<int>(n * mine / parts), hi = r.x + static_cast<int>(n * (mine + 1) / parts);
   float sum[V] = {};
   if (col < N) {
-#pragma unroll 4
-    for (int i = r.x + rl; i < r.y; i += 32) {
+#pragma unroll 8
+    for (int i = lo + rl; i < hi; i += TY) {
       const T* p = x + static_cast<int64_t>(i) * N + col;
       if constexpr (VEC) {
         const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
@@ -72,23 +80,47 @@ __global__ void __launch_bounds__(256) column_sums(const T* __restrict__ x, cons
     }
   }
 #pragma unroll
-  for (int e = 0; e < V; ++e) part[rl][cl + e] = sum[e];
+  for (int e = 0; e < V; e += 4)
+    *reinterpret_cast<float4*>(&part[rl][cl + e]) = make_float4(sum[e], sum[e + 1], sum[e + 2], sum[e + 3]);
   __syncthreads();
   const int c = threadIdx.x;
-  if (c < 8 * V && strip * 8 * V + c < N) {
-    float s = part[0][c];
+  float s = 0.f;
+  if (c < COLS) {
+    s = part[0][c];
 #pragma unroll
-    for (int i = 1; i < 32; ++i) s += part[i][c];
-    out[static_cast<int64_t>(g) * N + strip * 8 * V + c] = s;
+    for (int i = 1; i < TY; ++i) s += part[i][c];
   }
+  if (parts > 1) {
+    ptx::cluster_wait();  // every peer runs
+    if (c < COLS) ptx::st_cluster_u32(ptx::mapa_shared(ptx::smem_u32(&all[mine][c]), 0), __float_as_uint(s));
+    ptx::cluster_sync();
+    if (mine != 0) return;
+    if (c < COLS) {
+      s = all[0][c];
+      for (int i = 1; i < parts; ++i) s += all[i][c];
+    }
+  }
+  if (c < COLS && strip * COLS + c < N) out[static_cast<int64_t>(g) * N + strip * COLS + c] = s;
 }
 
+template <typename T, bool VEC, int TX>
+cudaError_t launch_strips(const sky_grouped_shape& s, const int32_t* offset, const void* x, float* out, int32_t* status,
+                          cudaStream_t st) {
+  const int strips = ceil_div(s.out, TX * (VEC ? 16 / static_cast<int>(sizeof(T)) : 4));
+  // parts of a mean group's rows, 64 or more each, while the CTAs are no more than 32 an SM
+  int parts = 1;
+  while (parts < 8 && s.rows / s.groups >= 128 * parts && static_cast<int64_t>(s.groups) * strips * parts * 2 <= 32 * sm_count())
+    parts *= 2;
+  return launch_pdl(column_sums<T, VEC, TX>, dim3(s.groups * strips * parts), dim3(256), 0, st, parts,
+                    static_cast<const T*>(x), offset, s.groups, s.rows, s.out, strips, parts, out, status);
+}
 template <typename T, bool VEC>
 cudaError_t launch_sums(const sky_grouped_shape& s, const int32_t* offset, const void* x, float* out, int32_t* status,
                         cudaStream_t st) {
-  const int strips = ceil_div(s.out, 8 * (VEC ? 16 / static_cast<int>(sizeof(T)) : 4));
-  return launch_pdl(column_sums<T, VEC>, dim3(s.groups * strips), dim3(256), 0, st, 1, static_cast<const T*>(x), offset,
-                    s.groups, s.rows, s.out, strips, out, status);
+  const int cols = 32 * (VEC ? 16 / static_cast<int>(sizeof(T)) : 4);
+  return static_cast<int64_t>(s.groups) * ceil_div(s.out, cols) * 8 < sm_count()
+             ? launch_strips<T, VEC, 8>(s, offset, x, out, status, st)
+             : launch_strips<T, VEC, 32>(s, offset, x, out, status, st);
 }
 
 }  // namespace

@@ -24,7 +24,7 @@ namespace route {
 namespace {
 
 constexpr int MAX_EXPERTS = 1024, MAX_TOP_K = 32;
-constexpr int THREADS = 256, SMALL_THREADS = 1024, SMALL = 64;
+constexpr int THREADS = 256, WIDE = 1024, SMALL = 64;
 constexpr int MOST_BLOCK = 256;     // tokens of a block
 constexpr int MOST_COUNTS = 16384;  // counts that every block adds up for itself
 constexpr int32_t kStatusNaN = 4;
@@ -55,16 +55,23 @@ constexpr uint32_t LOWEST = 0x007fffffu;  // of -inf: nothing up to here is chos
 // exp(x - top), where equal infinities count as equal.
 __device__ __forceinline__ float exp_below(float x, float top) { return x == top ? 1.f : expf(x - top); }
 
+// A token's logits as they lie in a warp.
+template <typename T, int V>
+__device__ __forceinline__ void load_logits(const Params& p, int t, int lane, T (&x)[V]) {
+  const T* row = static_cast<const T*>(p.logits) + static_cast<int64_t>(t) * p.experts;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (lane + 32 * j < p.experts) x[j] = row[lane + 32 * j];
+}
+
 // The choices of one token, by a warp: lane c gets choice c.
 template <typename T, int V>
-__device__ __forceinline__ void choose(const Params& p, int t, int lane, int& mine, float& weight) {
+__device__ __forceinline__ void choose(const Params& p, const T (&x)[V], int lane, int& mine, float& weight) {
   uint32_t key[V];
   bool nan = false;
-  const T* x = static_cast<const T*>(p.logits) + static_cast<int64_t>(t) * p.experts;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const int e = lane + 32 * j;
-    const float f = e < p.experts ? to_f32<T>(x[e]) : -INFINITY;
+    const float f = lane + 32 * j < p.experts ? to_f32<T>(x[j]) : -INFINITY;
     nan |= f != f;
     key[j] = order_of(f);
   }
@@ -103,24 +110,27 @@ __device__ __forceinline__ void choose(const Params& p, int t, int lane, int& mi
   weight = mine >= 0 ? e / total : 0.f;
 }
 
-// Exclusive sums over the experts of what `total` holds, by a whole CTA.
+// Exclusive sums over the experts of what `total` holds, by a whole CTA: consecutive experts a
+// thread, the warps' sums scanned by every warp for itself.
 __device__ __forceinline__ void scan_experts(int* total, int experts, int* warp_sums) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  const int per = (experts + blockDim.x - 1) / blockDim.x;  // consecutive experts of a thread
+  const int per = (experts + blockDim.x - 1) / blockDim.x;
   int own = 0;
   for (int i = 0; i < per; ++i)
     if (tid * per + i < experts) own += total[tid * per + i];
-  int sum = own;
+  const auto scan = [&](int v) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int up = __shfl_up_sync(0xffffffffu, sum, o);
-    if (lane >= o) sum += up;
-  }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += up;
+    }
+    return v;
+  };
+  const int sum = scan(own);
   if (lane == 31) warp_sums[warp] = sum;
   __syncthreads();
-  int before = sum - own;
-  for (int w = 0; w < warps; ++w)
-    if (w < warp) before += warp_sums[w];
+  const int upto = scan(lane < warps ? warp_sums[lane] : 0);
+  int before = sum - own + (warp > 0 ? __shfl_sync(0xffffffffu, upto, (warp + 31) & 31) : 0);
   for (int i = 0; i < per; ++i)
     if (tid * per + i < experts) {
       const int n = total[tid * per + i];
@@ -152,10 +162,16 @@ __device__ __forceinline__ void choose_block(const Params& p, int t0, uint32_t* 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, words = p.block / 32;
   for (int i = threadIdx.x; i < p.experts * words; i += blockDim.x) mask[i] = 0;
   __syncthreads();
-  for (int t = warp; t < p.block && t0 + t < p.tokens; t += blockDim.x >> 5) {
+  const int last = min(p.block, p.tokens - t0), warps = blockDim.x >> 5;
+  T x[V], next[V];
+  if (warp < last) load_logits<T, V>(p, t0 + warp, lane, next);
+  for (int t = warp; t < last; t += warps) {
     int e;
     float w;
-    choose<T, V>(p, t0 + t, lane, e, w);
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = next[j];
+    if (t + warps < last) load_logits<T, V>(p, t0 + t + warps, lane, next);
+    choose<T, V>(p, x, lane, e, w);
     if (lane < p.top_k) {
       const int64_t at = static_cast<int64_t>(t0 + t) * p.top_k + lane;
       p.expert[at] = e;
@@ -172,11 +188,12 @@ __device__ __forceinline__ int count_of(const uint32_t* mask, int e, int words) 
   return n;
 }
 
-// Everything, for one block of tokens.  (With 32 experts a lane, half the threads: their
-// keys take the registers.)
-constexpr int small_threads(int v) { return v == 32 ? SMALL_THREADS / 2 : SMALL_THREADS; }
+// Threads where warps choose: with 32 experts a lane, half as many, whose keys take the registers.
+constexpr int choosers(int v) { return v == 32 ? WIDE / 2 : WIDE; }
+
+// Everything, for one block of tokens.
 template <typename T, int V>
-__global__ void __launch_bounds__(small_threads(V)) route_small(const Params p) {
+__global__ void __launch_bounds__(choosers(V)) route_small(const Params p) {
   extern __shared__ uint32_t sm[];
   __shared__ int sums[32];
   uint32_t* mask = sm;
@@ -195,7 +212,7 @@ __global__ void __launch_bounds__(small_threads(V)) route_small(const Params p) 
 }
 
 template <typename T, int V>
-__global__ void __launch_bounds__(THREADS) route_choose(const Params p) {
+__global__ void __launch_bounds__(choosers(V)) route_choose(const Params p) {
   extern __shared__ uint32_t sm[];
   pdl_wait();
   pdl_trigger();
@@ -228,9 +245,9 @@ __global__ void __launch_bounds__(THREADS) route_scan(const Params p) {
   if (lane == 0) p.counts[static_cast<int64_t>(p.blocks) * p.experts + e] = before;
 }
 
-__global__ void __launch_bounds__(THREADS) route_place(const Params p) {
+__global__ void __launch_bounds__(WIDE) route_place(const Params p) {
   extern __shared__ uint32_t sm[];
-  __shared__ int sums[THREADS / 32];
+  __shared__ int sums[WIDE / 32];
   const int words = p.block / 32, t0 = blockIdx.x * p.block;
   uint32_t* mask = sm;
   int* base = reinterpret_cast<int*>(mask + p.experts * words);  // totals, then starts
@@ -256,7 +273,7 @@ __global__ void __launch_bounds__(THREADS) route_place(const Params p) {
     for (int i = threadIdx.x; i < p.experts * parts; i += blockDim.x) {
       const int e = i % p.experts;
       int total = 0, mine = 0;
-#pragma unroll 8
+#pragma unroll 16
       for (int b = i / p.experts; b < p.blocks; b += parts) {
         const int c = p.counts[b * p.experts + e];
         total += c;
@@ -382,7 +399,7 @@ sky_status forward(Params p, cudaStream_t st) {
     p.blocks = 1;
     const size_t smem = static_cast<size_t>(p.experts) * (p.block / 32 + 1) * 4;
     e = by_experts(p.experts, [&](auto v) {
-      const int threads = std::min(small_threads(decltype(v)::value), 32 * p.tokens);
+      const int threads = std::min(choosers(decltype(v)::value), 32 * p.tokens);
       return launch_pdl(route_small<T, decltype(v)::value>, dim3(1), dim3(threads), smem, st, 1, p);
     });
     count_launches(1);
@@ -393,7 +410,7 @@ sky_status forward(Params p, cudaStream_t st) {
   p.scanned = static_cast<int64_t>(p.blocks) * p.experts > MOST_COUNTS;
   const size_t masks = static_cast<size_t>(p.experts) * (p.block / 32) * 4;  // up to 32 KiB
   e = by_experts(p.experts, [&](auto v) {
-    return launch_pdl(route_choose<T, decltype(v)::value>, dim3(p.blocks), dim3(THREADS), masks, st, 1, p);
+    return launch_pdl(route_choose<T, decltype(v)::value>, dim3(p.blocks), dim3(choosers(decltype(v)::value)), masks, st, 1, p);
   });
   count_launches(1);
   if (e == cudaSuccess && p.scanned) {
@@ -401,7 +418,7 @@ sky_status forward(Params p, cudaStream_t st) {
     count_launches(1);
   }
   if (e == cudaSuccess) {
-    e = launch_pdl(route_place, dim3(p.blocks), dim3(THREADS), masks + 2 * p.experts * 4, st, 1, p);
+    e = launch_pdl(route_place, dim3(p.blocks), dim3(WIDE), masks + 2 * p.experts * 4, st, 1, p);
     count_launches(1);
   }
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "routing launch");
