@@ -86,12 +86,17 @@ sky_status launch(const Call& c, cudaStream_t st) {
   const int64_t m_tiles = FORM == SKY_GEMM_XTW ? static_cast<int64_t>(c.groups) * p.m_tiles
                                                : c.rows / TM + static_cast<int64_t>(std::min(c.groups, c.rows));
   const int64_t tiles = m_tiles * p.n_tiles;
-  // splits as gemm_f32.cu makes them, by the slabs of a mean group
+  // Splits, by the slabs of a mean group: the most of 8, 4 and 2 that make no more than four CTAs an
+  // SM and have slabs enough.  us at 1 / 2 / 4 / 8 (tiles that the rows may make, slabs): 257 x 512 x
+  // 128 with GELU, 4 groups (64, 4) 10.0 7.9 6.2 7.9; 1000 x 128 x 512, 16 groups (62, 16) 21.5 13.5
+  // 12.0 10.3; 1000 x 768 x 768 (228, 24) 58 36 38 40; 40 x 200 x 300, 20 groups (80, 10) 16.1 12.7 11.4
+  // 13.7; 4000 x 300 x 200 (320, 7) 21.4 23.6 25.2 31.5; weight gradients of 257 rows (64, 3) 6.7 6.2 4.8
+  // 6.8, of 1000 over 16 groups (256, 2) 9.4 9.9 12.4 19.8, of 4000 over 2 (40, 63) 111 57 36 26.
   const int K = FORM == SKY_GEMM_XWT ? c.in : FORM == SKY_GEMM_XW ? c.out : ceil_div(c.rows, c.groups);
   const int slabs = ceil_div(K, TK);
   p.ks = 1;
-  for (int ks = 8; ks >= 4 && p.ks == 1; ks /= 2)
-    if (tiles * ks <= 11 * sms && slabs >= 2 * ks) p.ks = ks;
+  for (int ks = 8; ks >= 2 && p.ks == 1; ks /= 2)
+    if (tiles * ks <= 4 * sms && slabs >= (ks == 8 ? 16 : ks == 4 ? 3 : 4)) p.ks = ks;
   SKY_CHECK(tiles * p.ks <= 0x7fffffff, SKY_ERR_UNSUPPORTED, "grouped product too large");
   const auto a16 = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
   const bool vec = c.in % 4 == 0 && c.out % 4 == 0 && a16(c.A) && a16(c.B);
