@@ -74,7 +74,7 @@ sky_status sky_route_bwd(const sky_route_shape* shape, const void* logits, const
  * in dtype; row: int32 [tokens, top_k] as sky_route_fwd writes it.  Places outside
  * [0, tokens * top_k) are choices without a row: nothing is read or written for them.
  * Rows that no choice names are left as they are.  Sums are fp32, in the order of the
- * choices, and rounded once.
+ * choices, and rounded once.  Outputs may not overlap inputs but where that is said.
  * Errors: INVALID_ARG (null, sizes, an unknown dtype, row, weight or dweight off the
  * 4-byte grid), UNSUPPORTED (width not a multiple of 16 bytes or above 2^20 values,
  * matrices not 16-byte aligned, top_k above 32, tokens * top_k of 2^31 or more). */

@@ -52,7 +52,7 @@ typedef struct {
 typedef struct {
   float lr;             /* finite, >= 0                                              */
   float beta1, beta2;   /* in [0, 1)                                                 */
-  float eps;            /* finite, > 0                                               */
+  float eps;            /* finite, >= 2^-126 (its inverse is taken)                  */
   float weight_decay;   /* finite, >= 0                                              */
   int64_t step;         /* t >= 1, this update's number                              */
   sky_dtype grad_dtype;

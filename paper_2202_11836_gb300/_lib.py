@@ -227,4 +227,6 @@ def check(status: int, where: str) -> None:
 
 def call(name: str, *args) -> None:
     """Calls an ABI function and raises SkyError on a non-OK status."""
-    check(getattr(lib(), name)(*args), name)
+    status = getattr(_lib or lib(), name)(*args)
+    if status:
+        check(status, name)

@@ -28,6 +28,7 @@
 // bf16 gradients 33.6M values take 96 of 80.  Moments in 32 bits: 33.6M values 158 of 148.
 #include <cuda_fp8.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "../../include/sky_optim.h"
@@ -468,7 +469,7 @@ sky_status check(const sky_adamw_config* c, const sky_adamw_tensor* t, int32_t n
             "unknown gradient dtype");
   SKY_CHECK(c->states == SKY_STATE_FP32 || c->states == SKY_STATE_8BIT, SKY_ERR_INVALID_ARG, "unknown kind of states");
   SKY_CHECK(std::isfinite(c->lr) && c->lr >= 0.f && c->beta1 >= 0.f && c->beta1 < 1.f && c->beta2 >= 0.f &&
-                c->beta2 < 1.f && std::isfinite(c->eps) && c->eps > 0.f && std::isfinite(c->weight_decay) &&
+                c->beta2 < 1.f && std::isfinite(c->eps) && c->eps >= FLT_MIN && std::isfinite(c->weight_decay) &&
                 c->weight_decay >= 0.f && c->step >= 1,
             SKY_ERR_INVALID_ARG, "a setting out of its range");
   SKY_CHECK(on(now, 4), SKY_ERR_INVALID_ARG, "d_now off the 4-byte grid");

@@ -210,7 +210,7 @@ def tensor(**kw):
 
 NAN, INF = float("nan"), float("inf")
 CONFIG_REFUSED = [dict(lr=-1e-9), dict(lr=NAN), dict(lr=INF), dict(beta1=-0.1), dict(beta1=1.0), dict(beta1=NAN),
-                  dict(beta2=1.0), dict(beta2=-1e-9), dict(eps=0.0), dict(eps=-1.0), dict(eps=INF), dict(eps=NAN),
+                  dict(beta2=1.0), dict(beta2=-1e-9), dict(eps=0.0), dict(eps=1e-39), dict(eps=-1.0), dict(eps=INF), dict(eps=NAN),
                   dict(weight_decay=-0.1), dict(weight_decay=NAN), dict(step=0), dict(step=-5), dict(grad_dtype=2),
                   dict(states=2), dict(states=-1)]
 TENSOR_REFUSED = [(dict([(n, None)]), INVALID) for n in ("w", "g", "m", "v", "m_scale", "v_scale")] + \
