@@ -19,6 +19,17 @@
 // they hold may be anything.
 // The groups' sizes are on the device only: every warp finds its next tile from the offsets
 // itself, 32 groups at a time (grouped.cuh).
+//
+// What bounds them: a 256 x 256 tile on a pair takes 64 bytes a clock and SM of operands at the
+// tensor cores' full rate, which is what an SM takes in, and what it sends out competes with that.
+// 16384 rows, 8 groups of 4096 x 1024, a few calls: stored as it is 80 us (1.7 PFLOP/s), bias and
+// GELU with their two outputs 98, a gradient through GELU' 90, weight gradients (134 MB out) 91; without
+// their stores the second and the last take 83 and 79.  Kept up for a second the power cap takes 13%
+// more.  Stores of the GELU tile, us: 64 bytes of a row by lanes 118, four bytes a lane 121, by TMA from
+// a buffer a warp 102, from two 98, from two that two warps share (128 bytes a row) 109, from two for one
+// output at a time 105; sixteen warps 111.  Weight gradients by TMA in rows of 128 bytes 91, of 64 bytes
+// 100, by lanes 94.  Two pairs of a cluster that load their shared operand once (multicast): 80, 100,
+// 90 and 98, since clusters of four leave eight SMs without work.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -415,7 +426,8 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
 }
 
 // Rows of a group whose products one accumulator takes: the tensor cores cut off where they
-// add up, so a long sum is made of parts, added in fp32 in the epilogue's registers.
+// add up, so a long sum is made of parts, added in fp32 in the epilogue's registers.  Off by 4.4 to
+// 4.8e-7 of the norm at any length; as one sum 1.6e-6 over 2000 rows, and growing with them.
 constexpr int PART_ROWS = 512;
 
 // The groups by size, largest first, for up to 32 of them (lane g holds group g's rank, and the
