@@ -1,7 +1,8 @@
 // Products grouped by expert in fp32 arithmetic on the CUDA cores: the tiles of gemm_f32.cu,
 // each over the rows of one group.  Bound as those are, by the FMA pipe or, with few rows, by
-// the latency of a slab; the number of tiles is known on the device only, so the grid holds as
-// many as the rows may make and those that are too many leave at once.
+// the latency of a slab (grouped_few_f32.cu has the forward of those); the number of tiles is known
+// on the device only, so the grid holds as many as the rows may make and those that are too many
+// leave at once.
 #include <algorithm>
 
 #include "common.cuh"
@@ -110,6 +111,7 @@ sky_status launch(const Call& c, cudaStream_t st) {
 }  // namespace
 
 sky_status launch_simt(const Call& c, cudaStream_t st) {
+  if (few_f32_pays(c)) return launch_few_f32(c, st);
   if (c.form == SKY_GEMM_XWT) return launch<SKY_GEMM_XWT>(c, st);
   if (c.form == SKY_GEMM_XW) return launch<SKY_GEMM_XW>(c, st);
   return launch<SKY_GEMM_XTW>(c, st);

@@ -154,6 +154,39 @@ def test_fp32(form, epi, sizes, out, in_, first, behind):
     c.check(*c.run())
 
 
+# Few rows: groups of one to more than eight rows, features that are no multiple of four, inner sizes odd, short and long
+F32_FEW = [([1], 5, 3, 0, 0), ([1, 2, 3, 4, 5, 0, 7, 8, 9], 768, 768, 1, 2), ([64], 100, 640, 0, 0), ([1] * 40, 33, 129, 0, 5),
+           ([25, 0, 33], 18, 1001, 0, 1), ([2, 1], 200, 5000, 0, 0), ([11], 16, 4097, 3, 0), ([4, 3], 1023, 128, 0, 57)]
+
+
+@pytest.mark.parametrize("epi", ["store", "gelu"])
+@pytest.mark.parametrize("sizes,out,in_,first,behind", F32_FEW, ids=lambda v: str(v) if isinstance(v, int) else f"{len(v)}g{sum(v)}")
+def test_fp32_of_few_rows(epi, sizes, out, in_, first, behind):
+    c = Case("xwt", sizes, out, in_, "fp32", epi, first, behind)
+    c.check(*c.run())
+
+
+def test_fp32_of_few_rows_keeps_groups_apart():
+    """Infinities in a group's rows and weights, or in rows that none owns, stay where they are; weights off 16 bytes do too."""
+    sizes, out, in_ = [5, 9, 0, 3], 70, 132
+    c = Case("xwt", sizes, out, in_, "fp32", "store", 0, 4)
+    want = c.run()[0].clone()
+    c.a[5:14] = float("inf")
+    c.a[17:] = float("nan")
+    c.b[1] = float("-inf")
+    got = c.run()[0]
+    n = out * 5
+    assert torch.equal(got[:n], want[:n]) and torch.equal(got[14 * out:], want[14 * out:])
+    assert bool((got[n:14 * out] == float("-inf")).all())
+    at = torch.empty(c.b.numel() + 1, device="cuda")[1:]  # 4 bytes off
+    at.copy_(c.b.reshape(-1))
+    c.b = at.reshape(c.b.shape)
+    close = c.run()[0]
+    # either order of the sum, each of fp32 products: both within (in + 1) half steps of the sum of magnitudes
+    size = c.a[:5].abs().double() @ c.b[0].abs().double().T
+    assert bool(((close[:n].reshape(5, out) - want[:n].reshape(5, out)).abs().double() <= 2 * (in_ + 1) * 2.0 ** -24 * size).all())
+
+
 def test_gelu_without_a_bias():
     c = Case("xwt", [40, 3], 64, 128, "bf16", "gelu", seed=1)
     assert c.bias is None
