@@ -33,6 +33,9 @@ sky_status launch_tc(const Call& c, cudaStream_t st);
 // The same for few rows (grouped_few.cu), and whether a call is one of those.
 bool few_pays(const Call& c, int sms);
 sky_status launch_few(const Call& c, int sms, cudaStream_t st);
+// XTW of few tiles (grouped_grad_few.cu), and into how many splits of the rows it then pays (1: it does not).
+int grad_few_splits(const Call& c, int sms);
+sky_status launch_grad_few(const Call& c, int splits, cudaStream_t st);
 bool few_f32_pays(const Call& c);  // fp32 (grouped_few_f32.cu)
 sky_status launch_few_f32(const Call& c, cudaStream_t st);
 

@@ -132,7 +132,8 @@ __global__ void __launch_bounds__(THREADS, 2) grouped_few_tc(const __grid_consta
     int stage = 0;
     uint32_t phase = 0;
     bool good = true;
-    for (int kb = kb0; kb < kb1; ++kb) {
+    int kb = kb0;
+    for (; kb < kb1; ++kb) {
       good = __all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status));
       if (!good) break;
       ptx::tc_fence_after();
@@ -152,7 +153,7 @@ __global__ void __launch_bounds__(THREADS, 2) grouped_few_tc(const __grid_consta
       if (issuer) ptx::tc_commit(tfull);
       __syncwarp();
       ptx::mbar_wait(tfull, 0, WAIT_NS, p.status);
-    } else if (stage > 0 || phase > 0) {
+    } else if (kb > kb0) {
       const int last = stage > 0 ? stage - 1 : STAGES - 1;
       ptx::mbar_wait(&empty[last], stage > 0 ? phase : phase ^ 1u, WAIT_NS, p.status);
     }

@@ -13,8 +13,8 @@
 //               lies across lanes.  16x256b loads put it into the layout of an mma.sync
 //               accumulator, whose 16-bit pairs stmatrix writes transposed: 32 tokens by 32
 //               features in shared memory, which TMA stores.
-// XTW (weight gradients) sums over the rows of a group: 256 x 256 tiles on a pair, K the rows in
-// blocks of 64.  The last block's steps of 16 may reach into the next group's rows; there a warp
+// XTW (weight gradients; grouped_grad_few.cu has those of few tiles) sums over the rows of a group:
+// 256 x 256 tiles on a pair, K the rows in blocks of 64.  The last block's steps of 16 may reach into the next group's rows; there a warp
 // clears them in shared memory between the copy and the product, in both operands, since what
 // they hold may be anything.
 // The groups' sizes are on the device only: every warp finds its next tile from the offsets
@@ -751,6 +751,7 @@ sky_status launch_tc(const Call& c, cudaStream_t st) {
   const int sms = sm_count();
   SKY_CHECK(sms > 0, SKY_ERR_CUDA, "no CUDA device");
   if (few_pays(c, sms)) return launch_few(c, sms, st);
+  if (const int splits = grad_few_splits(c, sms); splits > 1) return launch_grad_few(c, splits, st);
   cudaError_t e;
   if (c.form == SKY_GEMM_XTW) {
     CUtensorMap ta, tb, tc;

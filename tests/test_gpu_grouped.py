@@ -154,6 +154,32 @@ def test_fp32(form, epi, sizes, out, in_, first, behind):
     c.check(*c.run())
 
 
+# Weight gradients of few tiles: up to four sums of 512 rows a split, splits without rows, empty groups, both remainders
+GRAD_FEW = [([5000], 128, 104, 3, 7), ([9000, 0, 4100], 256, 72, 0, 1), ([3100, 1], 2432, 120, 0, 0), ([7001], 2560, 72, 0, 0),
+            ([0, 3, 1600], 40, 200, 5, 40), ([2049] + [0] * 7, 64, 192, 0, 0), ([63], 600, 600, 1, 1)]
+
+
+@pytest.mark.parametrize("sizes,out,in_,first,behind", GRAD_FEW, ids=lambda v: str(v) if isinstance(v, int) else f"{len(v)}g{sum(v)}")
+def test_weight_gradients_of_few_tiles(sizes, out, in_, first, behind):
+    c = Case("xtw", sizes, out, in_, "bf16", "store", first, behind)
+    got = c.run()[0]
+    c.check(got, None)
+    assert torch.equal(got, c.run()[0])
+
+
+def test_weight_gradients_of_few_tiles_keep_groups_apart():
+    """Infinities in a group's rows, and what the rows behind the last hold, stay out of the others' sums."""
+    sizes, out, in_ = [1300, 37, 1201], 136, 200
+    c = Case("xtw", sizes, out, in_, "bf16", "store", 0, 70)
+    want = c.run()[0].clone()
+    c.a[1300:1337] = float("inf")
+    c.b[1300:1337] = 1.0
+    got = c.run()[0]
+    n = out * in_
+    assert torch.equal(got[:n], want[:n]) and torch.equal(got[2 * n:], want[2 * n:])
+    assert bool((got[n:2 * n] == float("inf")).all())
+
+
 # Few rows: groups of one to more than eight rows, features that are no multiple of four, inner sizes odd, short and long
 F32_FEW = [([1], 5, 3, 0, 0), ([1, 2, 3, 4, 5, 0, 7, 8, 9], 768, 768, 1, 2), ([64], 100, 640, 0, 0), ([1] * 40, 33, 129, 0, 5),
            ([25, 0, 33], 18, 1001, 0, 1), ([2, 1], 200, 5000, 0, 0), ([11], 16, 4097, 3, 0), ([4, 3], 1023, 128, 0, 57)]
