@@ -93,7 +93,8 @@ sky_status sky_dispatch_bwd(const sky_rows_shape* shape, const void* drows, cons
 sky_status sky_combine_fwd(const sky_rows_shape* shape, const void* rows, const int32_t* row,
                            const float* weight, void* y, void* stream);
 /* drows[row[t, c]] = weight[t, c] dy[t] and dweight[t, c] = dot(dy[t], rows[row[t, c]])
- * (fp32 [tokens, top_k], 0 where there is no row).  drows may be rows. */
+ * (fp32 [tokens, top_k], 0 where there is no row).  No place may be named twice.  drows
+ * may be rows. */
 sky_status sky_combine_bwd(const sky_rows_shape* shape, const void* rows, const void* dy,
                            const int32_t* row, const float* weight, void* drows, float* dweight,
                            void* stream);
@@ -130,7 +131,7 @@ size_t sky_grouped_gemm_workspace_bytes(sky_gemm_form form, const sky_grouped_sh
  * type's grid, a workspace that is too small or not 16-byte aligned), UNSUPPORTED (other
  * output dtypes and epilogues; bf16: out or in not a multiple of 8, A, B, C, aux or aux_out
  * not 16-byte aligned; more than 1024 groups, 2^28 rows or more, out or in above 2^20,
- * groups * out of 2^31 or more); offsets that decrease or leave [0, rows] are clamped and
+ * groups * out of 2^31 or more, or 2^31 tiles of 64 x 64 or more); offsets that decrease or leave [0, rows] are clamped and
  * set bit 0 of *d_status, and what the calls then write is not defined within C. */
 sky_status sky_grouped_gemm(sky_gemm_form form, const sky_grouped_shape* shape,
                             const int32_t* d_offset, const void* A, const void* B, void* C,

@@ -21,7 +21,8 @@
  *     UNSUPPORTED for shapes a kernel does not handle (listed per call),
  *     CUDA if a launch fails.  Device-side conditions (bad lengths, timed-out
  *     waits) are written to the int32 status word `d_status` if non-null:
- *     bit 0 = a length outside [1,S] was clamped, bit 1 = a wait timed out.
+ *     bit 0 = a length outside [1,S] was clamped, bit 1 = a wait timed out
+ *     (sky_experts.h: bit 2 = a NaN among routing logits).
  */
 #ifndef SKY_OPS_H
 #define SKY_OPS_H
