@@ -1,6 +1,7 @@
 // bf16 products grouped by expert for few rows (a decoder's new tokens): the weights of every
 // group that has a row are read once, for a handful of tokens each, so HBM bounds them and what
-// counts is that all SMs read at once and how soon.
+// counts is that all SMs read at once and how soon.  And for few tiles with long sums, where the
+// pairs of grouped_tc.cu would leave most SMs without work.
 //
 // As in grouped_tc.cu the weights are the M side: a tile is 128 features by up to 32 tokens of one
 // group, by one CTA, and the sum may be split over the CTAs of a cluster.  Two CTAs an SM, each
@@ -243,9 +244,15 @@ int64_t tiles_of(const Call& c) { return c.rows / TOKENS + static_cast<int64_t>(
 // 4.2, 8 rows 14.5 12.9, 32 rows 15.3 14.6, 64 rows (over two an SM) 15.5 15.5; 1024 x 4096: 1 row
 // 13.1 4.6, 8 rows 16.7 13.0, 64 rows 17.4 14.6, 256 rows 18.0 18.5; 768 x 768: 64 rows 5.3 4.7, 128
 // rows 5.4 5.7; 64 groups of 768 x 768 (384 tiles), 64 rows 15.2 17.7.
+// With more rows where the tiles leave room for splits and the sum is long enough for them: one
+// group, 256 rows of 1024 x 1024 (72 tiles) 8.8 6.9, of 1024 x 4096 21.4 9.6, 1024 rows of 256 x 2048 (66)
+// 13.0 7.6, of 1024 x 2048 (264) 13.1 14.1; 4 groups, 256 rows of 1024 x 1024 (96) 6.3 7.3, of 768 x 768 (72,
+// 12 blocks) 5.7 6.4.
 bool few_pays(const Call& c, int sms) {
-  if (c.form == SKY_GEMM_XTW || c.rows > 64) return false;
-  return tiles_of(c) * ceil_div(c.form == SKY_GEMM_XW ? c.in : c.out, BM) <= 2 * sms;
+  if (c.form == SKY_GEMM_XTW) return false;
+  const bool xw = c.form == SKY_GEMM_XW;
+  const int64_t units = tiles_of(c) * ceil_div(xw ? c.in : c.out, BM);
+  return units <= (c.rows <= 64 ? 2 * sms : ceil_div(xw ? c.out : c.in, BK) >= 16 ? sms / 2 : 0);
 }
 
 sky_status launch_few(const Call& c, int sms, cudaStream_t st) {

@@ -154,6 +154,18 @@ def test_fp32(form, epi, sizes, out, in_, first, behind):
     c.check(*c.run())
 
 
+# More than 64 rows of few tiles, with sums long enough to be split: remainders of tokens, features and blocks
+LONG_SUMS = [([80], 256, 1024, 0, 0), ([33, 0, 190], 136, 4104, 2, 3), ([1000, 1], 72, 1544, 0, 9), ([7, 90, 64], 520, 2048, 0, 0)]
+
+
+@pytest.mark.parametrize("form,epi", [k for k in KINDS if k[0] != "xtw"])
+@pytest.mark.parametrize("sizes,features,inner,first,behind", LONG_SUMS, ids=lambda v: str(v) if isinstance(v, int) else f"{len(v)}g{sum(v)}")
+def test_few_tiles_with_long_sums(form, epi, sizes, features, inner, first, behind):
+    out, in_ = (features, inner) if form == "xwt" else (inner, features)
+    c = Case(form, sizes, out, in_, "bf16", epi, first, behind)
+    c.check(*c.run())
+
+
 # Weight gradients of few tiles: up to four sums of 512 rows a split, splits without rows, empty groups, both remainders
 GRAD_FEW = [([5000], 128, 104, 3, 7), ([9000, 0, 4100], 256, 72, 0, 1), ([3100, 1], 2432, 120, 0, 0), ([7001], 2560, 72, 0, 0),
             ([0, 3, 1600], 40, 200, 5, 40), ([2049] + [0] * 7, 64, 192, 0, 0), ([63], 600, 600, 1, 1)]
