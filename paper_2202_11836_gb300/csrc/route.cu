@@ -26,7 +26,8 @@ namespace {
 constexpr int MAX_EXPERTS = 1024, MAX_TOP_K = 32;
 constexpr int THREADS = 256, WIDE = 1024, SMALL = 64;
 constexpr int MOST_BLOCK = 256;     // tokens of a block
-constexpr int MOST_COUNTS = 16384;  // counts that every block adds up for itself
+constexpr int MOST_COUNTS = 16384;  // counts that every block adds up for itself (15000: 16.2 us, scanned 17.5; 20480: 13.0, 12.0)
+constexpr int AT_ONCE = 4;          // of them that a thread waits for together
 constexpr int32_t kStatusNaN = 4;
 
 struct Params {
@@ -273,11 +274,15 @@ __global__ void __launch_bounds__(WIDE) route_place(const Params p) {
     for (int i = threadIdx.x; i < p.experts * parts; i += blockDim.x) {
       const int e = i % p.experts;
       int total = 0, mine = 0;
-#pragma unroll 16
-      for (int b = i / p.experts; b < p.blocks; b += parts) {
-        const int c = p.counts[b * p.experts + e];
-        total += c;
-        if (b < static_cast<int>(blockIdx.x)) mine += c;
+      for (int b0 = i / p.experts; b0 < p.blocks; b0 += AT_ONCE * parts) {
+        int c[AT_ONCE];  // on their way together, the last ones too
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) c[k] = b0 + k * parts < p.blocks ? p.counts[(b0 + k * parts) * p.experts + e] : 0;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+          total += c[k];
+          if (b0 + k * parts < static_cast<int>(blockIdx.x)) mine += c[k];
+        }
       }
       if (total) atomicAdd(&base[e], total);
       if (mine) atomicAdd(&before[e], mine);
@@ -370,7 +375,8 @@ sky_status check(const sky_route_shape* s) {
 bool on(const void* p, size_t grid) { return reinterpret_cast<uintptr_t>(p) % grid == 0; }
 
 // Tokens of a block: 32, or what keeps the blocks to 128 or fewer, each of which adds up the counts
-// of all (8192 x 64 logits, four choices, us at up to 64 / 128 / 256 blocks: 11.0 8.9 9.8).
+// of all (8192 x 64 logits, four choices, us at up to 64 / 128 / 256 blocks: 11.0 8.2 10.3; 4495 x 190,
+// six, 20.4 13.5 12.5).
 int block_of(int tokens) {
   int b = 32;
   while (b < MOST_BLOCK && ceil_div(tokens, b) > 128) b *= 2;
@@ -410,8 +416,12 @@ sky_status forward(Params p, cudaStream_t st) {
   p.blocks = ceil_div(p.tokens, p.block);
   p.scanned = static_cast<int64_t>(p.blocks) * p.experts > MOST_COUNTS;
   const size_t masks = static_cast<size_t>(p.experts) * (p.block / 32) * 4;  // up to 32 KiB
+  const size_t starts = 2 * p.experts * 4;
+  // (As much shared memory as route_place, whose CTAs come while these run: where the two would make an
+  // SM divide its first-level memory differently, 16384 x 128 logits, six choices, 27.0 us for 16.3.)
   e = by_experts(p.experts, [&](auto v) {
-    return launch_pdl(route_choose<T, decltype(v)::value>, dim3(p.blocks), dim3(choosers(decltype(v)::value)), masks, st, 1, p);
+    return launch_pdl(route_choose<T, decltype(v)::value>, dim3(p.blocks), dim3(choosers(decltype(v)::value)),
+                      masks + starts + sizeof(int) * WIDE / 32, st, 1, p);
   });
   count_launches(1);
   if (e == cudaSuccess && p.scanned) {
@@ -419,7 +429,7 @@ sky_status forward(Params p, cudaStream_t st) {
     count_launches(1);
   }
   if (e == cudaSuccess) {
-    e = launch_pdl(route_place, dim3(p.blocks), dim3(WIDE), masks + 2 * p.experts * 4, st, 1, p);
+    e = launch_pdl(route_place, dim3(p.blocks), dim3(WIDE), masks + starts, st, 1, p);
     count_launches(1);
   }
   return e == cudaSuccess ? SKY_OK : cuda_fail(e, "routing launch");
