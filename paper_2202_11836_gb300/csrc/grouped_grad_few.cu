@@ -242,7 +242,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
     for (int s = 0; s < 8; ++s)
       if (s < p.ks) ptx::ld_shared_v4(recv + s * own * 512 + piece(row, j), v[s]);
-    float4 sum = make_float4(__uint_as_float(v[0][0]), __uint_as_float(v[0][1]), __uint_as_float(v[0][2]), __uint_as_float(v[0][3]));
+    float4 sum = make_float4(__uint_as_float(v[0][0]), __uint_as_float(v[0][1]), __uint_as_float(v[0][2]),
+                             __uint_as_float(v[0][3]));
 #pragma unroll
     for (int s = 1; s < 8; ++s)
       if (s < p.ks) {
@@ -295,7 +296,8 @@ int grad_few_splits(const Call& c, int sms) {
 }
 
 sky_status launch_grad_few(const Call& c, int splits, cudaStream_t st) {
-  Params p{c.offset, c.groups, c.rows, c.out, c.in, ceil_div(c.out, BM), ceil_div(c.in, BN), 0, splits, static_cast<float*>(c.C), c.status};
+  Params p{c.offset, c.groups, c.rows, c.out, c.in, ceil_div(c.out, BM), ceil_div(c.in, BN), 0, splits,
+           static_cast<float*>(c.C), c.status};
   p.n_width = ceil_div(ceil_div(c.in, p.n_blocks), 16) * 16;
   CUtensorMap ta, tb;
   const bool ok = gemm::make_map(&ta, c.A, c.rows, c.out, 64) && gemm::make_map(&tb, c.B, c.rows, c.in, 64);

@@ -3,7 +3,9 @@
 //
 // A warp holds a token's logits, expert lane + 32 j in lane's register j, as unsigned
 // integers in the order of the numbers.  A choice is one warp reduction for the largest and
-// one for the lowest index that has it.
+// one for the lowest index that has it.  Choosing is bound by the instructions issued, so up to
+// 16 experts 16 or 8 lanes hold a token and a warp has two or four (16384 x 8 logits, two choices,
+// us at 32 / 16 / 8 lanes: 9.1 7.1 5.7; 65536 x 8: 22.6 15.3 10.7).
 //
 // The sort is a counting sort over blocks of consecutive tokens.  A token chooses an expert
 // at most once, so a block's choices of an expert are a bit mask over its tokens: the block's
@@ -26,7 +28,8 @@ namespace {
 constexpr int MAX_EXPERTS = 1024, MAX_TOP_K = 32;
 constexpr int THREADS = 256, WIDE = 1024, SMALL = 64;
 constexpr int MOST_BLOCK = 256;     // tokens of a block
-constexpr int MOST_COUNTS = 16384;  // counts that every block adds up for itself (15000: 16.2 us, scanned 17.5; 20480: 13.0, 12.0)
+// Counts that every block adds up for itself (us so and scanned: 15000 counts 16.2 17.5, 20480 13.0 12.0).
+constexpr int MOST_COUNTS = 16384;
 constexpr int AT_ONCE = 4;          // of them that a thread waits for together
 constexpr int32_t kStatusNaN = 4;
 
@@ -56,7 +59,7 @@ constexpr uint32_t LOWEST = 0x007fffffu;  // of -inf: nothing up to here is chos
 // exp(x - top), where equal infinities count as equal.
 __device__ __forceinline__ float exp_below(float x, float top) { return x == top ? 1.f : expf(x - top); }
 
-// A token's logits as they lie in a warp.
+// A token's logits as they lie in a warp, or in one of its groups of lanes.
 template <typename T, int V>
 __device__ __forceinline__ void load_logits(const Params& p, int t, int lane, T (&x)[V]) {
   const T* row = static_cast<const T*>(p.logits) + static_cast<int64_t>(t) * p.experts;
@@ -65,14 +68,33 @@ __device__ __forceinline__ void load_logits(const Params& p, int t, int lane, T 
     if (lane + 32 * j < p.experts) x[j] = row[lane + 32 * j];
 }
 
-// The choices of one token, by a warp: lane c gets choice c.
-template <typename T, int V>
-__device__ __forceinline__ void choose(const Params& p, const T (&x)[V], int lane, int& mine, float& weight) {
+// Over groups of G lanes.
+template <int G>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  if constexpr (G == 32) {
+    return __reduce_max_sync(0xffffffffu, v);
+  } else {
+#pragma unroll
+    for (int o = G / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+  }
+}
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// The choices of one token, by G lanes (32, or fewer where V is 1): lane c of them gets choice c.
+// `there`: there is a token.  Every lane of the warp calls.
+template <typename T, int V, int G>
+__device__ __forceinline__ void choose(const Params& p, const T (&x)[V], int lane, bool there, int& mine, float& weight) {
   uint32_t key[V];
   bool nan = false;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const float f = lane + 32 * j < p.experts ? to_f32<T>(x[j]) : -INFINITY;
+    const float f = there && lane + 32 * j < p.experts ? to_f32<T>(x[j]) : -INFINITY;
     nan |= f != f;
     key[j] = order_of(f);
   }
@@ -83,9 +105,10 @@ __device__ __forceinline__ void choose(const Params& p, const T (&x)[V], int lan
     uint32_t best = key[0];
 #pragma unroll
     for (int j = 1; j < V; ++j) best = max(best, key[j]);
-    best = __reduce_max_sync(0xffffffffu, best);
-    if (best <= LOWEST) break;  // warp-uniform
-    if (c == 0) {
+    best = group_max<G>(best);
+    const bool some = best > LOWEST;  // the same in a group
+    if (G == 32 ? !some : !__any_sync(0xffffffffu, some)) break;  // warp-uniform
+    if (c == 0 && some) {
       top = number_of(best);
       if (p.over_all) {
 #pragma unroll
@@ -94,20 +117,25 @@ __device__ __forceinline__ void choose(const Params& p, const T (&x)[V], int lan
       }
     }
     int at = MAX_EXPERTS;
+    if constexpr (G == 32) {
 #pragma unroll
-    for (int j = V - 1; j >= 0; --j)
-      if (key[j] == best) at = lane + 32 * j;
-    at = __reduce_min_sync(0xffffffffu, at);
+      for (int j = V - 1; j >= 0; --j)
+        if (key[j] == best) at = lane + 32 * j;
+      at = __reduce_min_sync(0xffffffffu, at);
+    } else {
+      const uint32_t equal = __ballot_sync(0xffffffffu, key[0] == best) >> (threadIdx.x & 31 & ~(G - 1));
+      at = __ffs(equal) - 1;
+    }
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (at == lane + 32 * j) key[j] = 0;
-    if (lane == c) {
+    if (some && lane == c) {
       mine = at;
       value = number_of(best);
     }
   }
   const float e = mine >= 0 ? exp_below(value, top) : 0.f;
-  const float total = warp_sum(p.over_all ? all : e);
+  const float total = group_sum<G>(p.over_all ? all : e);
   weight = mine >= 0 ? e / total : 0.f;
 }
 
@@ -158,22 +186,23 @@ __device__ __forceinline__ void place_block(const Params& p, int t0, const uint3
 }
 
 // Chooses for a block of tokens and sets its masks.
-template <typename T, int V>
+template <typename T, int V, int G>
 __device__ __forceinline__ void choose_block(const Params& p, int t0, uint32_t* mask) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, words = p.block / 32;
+  const int lane = threadIdx.x % G, words = p.block / 32;
   for (int i = threadIdx.x; i < p.experts * words; i += blockDim.x) mask[i] = 0;
   __syncthreads();
-  const int last = min(p.block, p.tokens - t0), warps = blockDim.x >> 5;
-  T x[V], next[V];
-  if (warp < last) load_logits<T, V>(p, t0 + warp, lane, next);
-  for (int t = warp; t < last; t += warps) {
+  const int last = min(p.block, p.tokens - t0), groups = blockDim.x / G;
+  T x[V] = {}, next[V] = {};
+  int t = threadIdx.x / G;
+  if (t < last) load_logits<T, V>(p, t0 + t, lane, next);
+  for (int first = (threadIdx.x >> 5) * (32 / G); first < last; first += groups, t += groups) {  // (a warp's first token)
     int e;
     float w;
 #pragma unroll
     for (int j = 0; j < V; ++j) x[j] = next[j];
-    if (t + warps < last) load_logits<T, V>(p, t0 + t + warps, lane, next);
-    choose<T, V>(p, x, lane, e, w);
-    if (lane < p.top_k) {
+    if (t + groups < last) load_logits<T, V>(p, t0 + t + groups, lane, next);
+    choose<T, V, G>(p, x, lane, t < last, e, w);
+    if (t < last && lane < p.top_k) {
       const int64_t at = static_cast<int64_t>(t0 + t) * p.top_k + lane;
       p.expert[at] = e;
       p.weight[at] = w;
@@ -193,7 +222,7 @@ __device__ __forceinline__ int count_of(const uint32_t* mask, int e, int words) 
 constexpr int choosers(int v) { return v == 32 ? WIDE / 2 : WIDE; }
 
 // Everything, for one block of tokens.
-template <typename T, int V>
+template <typename T, int V, int G>
 __global__ void __launch_bounds__(choosers(V)) route_small(const Params p) {
   extern __shared__ uint32_t sm[];
   __shared__ int sums[32];
@@ -201,7 +230,7 @@ __global__ void __launch_bounds__(choosers(V)) route_small(const Params p) {
   int* base = reinterpret_cast<int*>(mask + p.experts * (p.block / 32));
   pdl_wait();
   pdl_trigger();
-  choose_block<T, V>(p, 0, mask);
+  choose_block<T, V, G>(p, 0, mask);
   for (int e = threadIdx.x; e < p.experts; e += blockDim.x) base[e] = count_of(mask, e, p.block / 32);
   __syncthreads();
   const int last = base[p.experts - 1];
@@ -212,12 +241,12 @@ __global__ void __launch_bounds__(choosers(V)) route_small(const Params p) {
   place_block(p, 0, mask, base);  // (what it reads of p.expert this CTA wrote before a barrier)
 }
 
-template <typename T, int V>
+template <typename T, int V, int G>
 __global__ void __launch_bounds__(choosers(V)) route_choose(const Params p) {
   extern __shared__ uint32_t sm[];
   pdl_wait();
   pdl_trigger();
-  choose_block<T, V>(p, blockIdx.x * p.block, sm);
+  choose_block<T, V, G>(p, blockIdx.x * p.block, sm);
   for (int e = threadIdx.x; e < p.experts; e += blockDim.x)
     p.counts[static_cast<int64_t>(blockIdx.x) * p.experts + e] = count_of(sm, e, p.block / 32);
 }
@@ -388,14 +417,21 @@ size_t workspace(const sky_route_shape& s) {
   return (static_cast<size_t>(ceil_div(s.tokens, block_of(s.tokens))) + 1) * s.experts * sizeof(int32_t);
 }
 
-// f with the registers a lane needs for its experts.
+// How a token's experts lie: V a lane, over G lanes.
+template <int V_, int G_>
+struct Lie {
+  static constexpr int V = V_, G = G_;
+};
+// Up to 16 experts several tokens share a warp.
 template <typename F>
 auto by_experts(int experts, F&& f) {
-  if (experts <= 32) return f(std::integral_constant<int, 1>());
-  if (experts <= 64) return f(std::integral_constant<int, 2>());
-  if (experts <= 128) return f(std::integral_constant<int, 4>());
-  if (experts <= 256) return f(std::integral_constant<int, 8>());
-  return f(std::integral_constant<int, 32>());
+  if (experts <= 8) return f(Lie<1, 8>());
+  if (experts <= 16) return f(Lie<1, 16>());
+  if (experts <= 32) return f(Lie<1, 32>());
+  if (experts <= 64) return f(Lie<2, 32>());
+  if (experts <= 128) return f(Lie<4, 32>());
+  if (experts <= 256) return f(Lie<8, 32>());
+  return f(Lie<32, 32>());
 }
 
 template <typename T>
@@ -405,9 +441,10 @@ sky_status forward(Params p, cudaStream_t st) {
     p.block = ceil_div(p.tokens, 32) * 32;
     p.blocks = 1;
     const size_t smem = static_cast<size_t>(p.experts) * (p.block / 32 + 1) * 4;
-    e = by_experts(p.experts, [&](auto v) {
-      const int threads = std::min(choosers(decltype(v)::value), 32 * p.tokens);
-      return launch_pdl(route_small<T, decltype(v)::value>, dim3(1), dim3(threads), smem, st, 1, p);
+    e = by_experts(p.experts, [&](auto lie) {
+      using L = decltype(lie);
+      const int threads = std::min(choosers(L::V), 32 * p.tokens);
+      return launch_pdl(route_small<T, L::V, L::G>, dim3(1), dim3(threads), smem, st, 1, p);
     });
     count_launches(1);
     return e == cudaSuccess ? SKY_OK : cuda_fail(e, "routing launch");
@@ -419,8 +456,9 @@ sky_status forward(Params p, cudaStream_t st) {
   const size_t starts = 2 * p.experts * 4;
   // (As much shared memory as route_place, whose CTAs come while these run: where the two would make an
   // SM divide its first-level memory differently, 16384 x 128 logits, six choices, 27.0 us for 16.3.)
-  e = by_experts(p.experts, [&](auto v) {
-    return launch_pdl(route_choose<T, decltype(v)::value>, dim3(p.blocks), dim3(choosers(decltype(v)::value)),
+  e = by_experts(p.experts, [&](auto lie) {
+    using L = decltype(lie);
+    return launch_pdl(route_choose<T, L::V, L::G>, dim3(p.blocks), dim3(choosers(L::V)),
                       masks + starts + sizeof(int) * WIDE / 32, st, 1, p);
   });
   count_launches(1);
@@ -437,8 +475,8 @@ sky_status forward(Params p, cudaStream_t st) {
 
 template <typename T>
 sky_status backward(const Params& p, const float* dweight, void* dlogits, cudaStream_t st) {
-  const cudaError_t e = by_experts(p.experts, [&](auto v) {
-    return launch_pdl(route_backward<T, decltype(v)::value>, dim3(ceil_div(p.tokens, THREADS / 32)), dim3(THREADS), 0, st,
+  const cudaError_t e = by_experts(p.experts, [&](auto lie) {
+    return launch_pdl(route_backward<T, decltype(lie)::V>, dim3(ceil_div(p.tokens, THREADS / 32)), dim3(THREADS), 0, st,
                       1, p, dweight, static_cast<T*>(dlogits));
   });
   count_launches(1);

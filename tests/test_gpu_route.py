@@ -96,6 +96,21 @@ def test_equal_closed_and_padded(tokens):
             assert out[1][3].tolist()[:2] == [0.5, 0.5]
 
 
+@pytest.mark.parametrize("tokens,experts,top_k", [(61, 5, 5), (1, 4, 2), (64, 8, 8), (67, 9, 9), (131, 16, 16), (5003, 8, 2),
+                                                 (4097, 11, 3), (12100, 14, 8), (40001, 7, 1)])
+def test_few_experts(tokens, experts, top_k):
+    """Up to 16 experts: equal logits, tokens with some or none left beside others that have all."""
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    x = torch.randint(-3, 4, (tokens, experts), device="cuda", generator=g).float() / 2
+    x[torch.rand(tokens, experts, device="cuda", generator=g) < 0.3] = -torch.inf
+    x[torch.rand(tokens, device="cuda", generator=g) < 0.2] = -torch.inf
+    x[tokens // 2, experts - 1] = torch.inf
+    for over in OVER:
+        for dtype in TYPES:
+            c = Case(tokens, experts, top_k, dtype, over, logits=x)
+            c.check(*c.forward())
+
+
 def test_all_to_one_expert_and_none():
     x = torch.full((300, 8), -torch.inf, device="cuda")
     c = Case(300, 8, 2, "fp32", "chosen", logits=x)
