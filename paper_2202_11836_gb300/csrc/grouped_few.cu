@@ -216,10 +216,10 @@ __global__ void __launch_bounds__(THREADS, 2) grouped_few_tc(const __grid_consta
       v += bias;
     }
     if constexpr (EPI == SKY_EPI_BIAS_GELU) {
-      float g, gp;
-      gelu_and_grad_as(v, g, gp);
-      v = g;
-      p.aux_out[off] = __float2half_rn(gp);
+      float2 g, gp;
+      gelu_and_grad2(v, 0.f, g, gp);  // (one value a step; it is the weights that are waited for)
+      v = g.x;
+      p.aux_out[off] = __float2half_rn(gp.x);
     }
     p.C[off] = __float2bfloat16_rn(v);
   }

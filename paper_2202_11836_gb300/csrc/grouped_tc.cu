@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
             }
             if constexpr (EPI == SKY_EPI_BIAS_GELU) {
               float2 g, gp;
-              gelu_and_grad_as2(v0, v1, g, gp);
+              gelu_and_grad2(v0, v1, g, gp);
               o[i] = ptx::pack_bf16(g.x, g.y);
               const __half2 h = __floats2half2_rn(gp.x, gp.y);
               x[i] = *reinterpret_cast<const uint32_t*>(&h);
