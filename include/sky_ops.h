@@ -294,14 +294,15 @@ sky_status sky_column_sum_noalloc(const void* x, int32_t T, int32_t N, sky_dtype
                                   float* out, void* stream);
 
 /* Test hook of the tensor-core GEMM's failure path (not for production use).
- * limit_ns caps every mbarrier wait of GEMM launches made after the call
- * (0 restores the default, 2 s).  skip_loads != 0 makes the TMA producer
- * arrive on its barriers without issuing the copies, so the consumers' waits
- * run out: the kernel then sets the timeout bit (2) of the status word it was
+ * limit_ns caps every mbarrier wait of GEMM launches, grouped ones among them, made
+ * after the call (0 restores the default, 2 s; below 0.1 ms it is 0.1 ms).
+ * skip_loads != 0 makes the TMA producer arrive on its barriers without issuing
+ * the copies (of grouped products: expecting more than they bring), so the
+ * consumers' waits run out: the kernel then sets the timeout bit (2) of the status word it was
  * given, frees its tensor memory and exits without storing the tiles
  * concerned, and the context stays usable.  skip_loads == 2: of a product
  * whose K range is split over a cluster only the last part's copies are left
- * out.
+ * out (or expected short).
  * Process-wide setting; pass (0, 0) to restore normal operation. */
 void sky_debug_gemm_fault(uint64_t limit_ns, int32_t skip_loads);
 

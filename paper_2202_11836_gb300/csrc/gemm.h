@@ -70,7 +70,12 @@ size_t workspace_bytes(sky_gemm_form form, int M, int N, int K, bool out_f32);
 int choose_splits(int64_t mn, int tiles, int k_blocks, int sms);
 // Debug controls: per-wait timeout (0 = default 2 s) and the fault-injection
 // switch that makes the TMA producer skip its loads (waits then time out).
+struct Debug {
+  uint64_t wait_ns;  // limit of any one wait
+  int skip_loads;    // 2: only those of a product's last split
+};
 void set_debug(uint64_t timeout_ns, int skip_loads);
+Debug debug();
 
 // fp32 SIMT path (exact fp32 FMA accumulation); same forms and epilogues.
 sky_status launch_f32(sky_gemm_form form, int M, int N, int K, const float* A, const float* B,

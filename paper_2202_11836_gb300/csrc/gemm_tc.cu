@@ -762,9 +762,11 @@ int g_skip_loads = 0;
 }  // namespace
 
 void set_debug(uint64_t timeout_ns, int skip_loads) {
-  g_timeout_ns = timeout_ns ? timeout_ns : 2000000000ull;
+  // (not below what copies on their way take, which a kernel that gives up waits for under the same limit)
+  g_timeout_ns = timeout_ns ? std::max<uint64_t>(timeout_ns, 100000) : 2000000000ull;
   g_skip_loads = skip_loads;
 }
+Debug debug() { return {g_timeout_ns, g_skip_loads}; }
 
 int colpart_rows_max(int M) {
   return std::max(ceil_div(M, BM) * 4, ceil_div(M, 2 * BM) * 8);

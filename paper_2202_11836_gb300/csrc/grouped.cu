@@ -1,7 +1,9 @@
 // The C ABI of the products grouped by expert, and their bias gradients (sky_experts.h).
+#include <climits>
 #include <type_traits>
 
 #include "abi.h"
+#include "gemm.h"
 #include "grouped.cuh"
 #include "grouped.h"
 #include "ptx.cuh"
@@ -37,6 +39,15 @@ sky_status check_form(sky_gemm_form form, const sky_grouped_shape& s, sky_dtype 
             "grouped products are in the operands' dtype, weight gradients in fp32");
   return SKY_OK;
 }
+
+}  // namespace
+
+Fault fault_of(int splits) {
+  const gemm::Debug d = gemm::debug();
+  return {d.wait_ns, d.skip_loads == 0 ? INT_MAX : d.skip_loads == 2 ? splits - 1 : 0};
+}
+
+namespace {
 
 size_t workspace(sky_gemm_form, const sky_grouped_shape&) { return 16; }
 

@@ -26,6 +26,16 @@ struct Call {
   int32_t* status;
 };
 
+// The limit of any one wait of the tensor-core kernels, and the splits, from one on, that expect
+// 16 bytes more than their copies bring, so that their waits run out (sky_debug_gemm_fault).  A branch
+// around the copies in its place takes 2% more of a small call.
+struct Fault {
+  uint64_t wait_ns;
+  int missing_from;
+  __host__ __device__ uint32_t missing(int split) const { return split >= missing_from ? 16 : 0; }
+};
+Fault fault_of(int splits);
+
 // fp32 arithmetic on the CUDA cores (grouped_f32.cu).
 sky_status launch_simt(const Call& c, cudaStream_t st);
 // bf16 on the tensor cores (grouped_tc.cu).

@@ -34,7 +34,6 @@ constexpr int BAR_OFF = RECV_OFF + RECV_BYTES;
 constexpr int SMEM = BAR_OFF + 256 + 1024;
 static_assert(SMEM >= kClusterProductSmem, "see residency.h");
 static_assert(2 * (SMEM + kSmemPerCta) <= kSmemPerSM, "two CTAs an SM");
-constexpr uint64_t WAIT_NS = 2000000000ull;
 
 struct Params {
   const int32_t* offset;
@@ -45,6 +44,7 @@ struct Params {
   const __half* aux;
   __half* aux_out;
   int32_t* status;
+  Fault fault;
 };
 struct Maps {
   CUtensorMap weights;
@@ -99,13 +99,14 @@ __global__ void __launch_bounds__(THREADS, 2) grouped_few_tc(const __grid_consta
 
   if (warp == 0) {
     const bool issuer = ptx::elect_one();
+    const uint32_t missing = p.fault.missing(split);
     int stage = 0, issued = 0;
     uint32_t phase = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, WAIT_NS, p.status))) break;
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, p.fault.wait_ns, p.status))) break;
       if (issuer) {
         uint8_t* sa = smem + stage * SBYTES;
-        ptx::mbar_arrive_expect_tx(&full[stage], A_BYTES + n_pad * BK * 2);
+        ptx::mbar_arrive_expect_tx(&full[stage], A_BYTES + n_pad * BK * 2 + missing);
         const int k0 = kb * BK;
         if (W_MN) {
           ptx::tma_load_3d(sa, &maps.weights, &full[stage], f0, k0, at.group);
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(THREADS, 2) grouped_few_tc(const __grid_consta
     const int n_tail = min(issued, STAGES);  // drain (bounded): the loads still in flight
     for (int i = 0; i < n_tail; ++i) {
       if (--stage < 0) { stage = STAGES - 1; phase ^= 1u; }
-      ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status);
+      ptx::mbar_wait(&full[stage], phase, p.fault.wait_ns, p.status);
     }
   } else if (warp == 1) {
     const bool issuer = ptx::elect_one();
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(THREADS, 2) grouped_few_tc(const __grid_consta
     bool good = true;
     int kb = kb0;
     for (; kb < kb1; ++kb) {
-      good = __all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status));
+      good = __all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, p.fault.wait_ns, p.status));
       if (!good) break;
       ptx::tc_fence_after();
       if (issuer) {
@@ -153,10 +154,10 @@ __global__ void __launch_bounds__(THREADS, 2) grouped_few_tc(const __grid_consta
     if (good) {
       if (issuer) ptx::tc_commit(tfull);
       __syncwarp();
-      ptx::mbar_wait(tfull, 0, WAIT_NS, p.status);
+      ptx::mbar_wait(tfull, 0, p.fault.wait_ns, p.status);
     } else if (kb > kb0) {
       const int last = stage > 0 ? stage - 1 : STAGES - 1;
-      ptx::mbar_wait(&empty[last], stage > 0 ? phase : phase ^ 1u, WAIT_NS, p.status);
+      ptx::mbar_wait(&empty[last], stage > 0 ? phase : phase ^ 1u, p.fault.wait_ns, p.status);
     }
   }
   // ------------------------------------------------------------------ epilogue
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(THREADS, 2) grouped_few_tc(const __grid_consta
   const auto piece = [](int f, int j) { return static_cast<uint32_t>(f * 128 + ((j ^ (f & 7)) << 4)); };
   uint32_t r[32];
   if (warp >= 2) {
-    const bool ok = __all_sync(0xffffffffu, ptx::mbar_wait(tfull, 0, WAIT_NS, p.status));
+    const bool ok = __all_sync(0xffffffffu, ptx::mbar_wait(tfull, 0, p.fault.wait_ns, p.status));
     ptx::tc_fence_after();
     if (ok) {
       ptx::tmem_ld_32x32b_x32(tmem_base + (static_cast<uint32_t>(q * 32) << 16), r);
@@ -277,6 +278,7 @@ sky_status launch_few(const Call& c, int sms, cudaStream_t st) {
   p.ks = 1;
   while (p.ks < 8 && units * p.ks * 2 <= 2 * sms && p.k_blocks >= 6 * p.ks) p.ks *= 2;
   SKY_CHECK(units * p.ks <= 0x3fffffff, SKY_ERR_UNSUPPORTED, "grouped product too large");
+  p.fault = fault_of(p.ks);
   Maps m;
   const bool ok = gemm::make_map_3d(&m.weights, c.B, c.groups, c.out, c.in, xw ? 64 : BM, 64, false) &&
                   gemm::make_map(&m.rows[0], c.A, c.rows, k, 16) && gemm::make_map(&m.rows[1], c.A, c.rows, k, 32);

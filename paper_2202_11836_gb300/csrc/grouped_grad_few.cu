@@ -36,7 +36,6 @@ constexpr int THREADS = 192;
 constexpr int RECV_OFF = STAGES * SBYTES, BAR_OFF = RECV_OFF + BM * BN * 4;
 constexpr int SMEM = BAR_OFF + 256 + 1024;
 static_assert(SMEM + kSmemPerCta + kSplitAttentionSmem + kSmemPerCta > kSmemPerSM, "see residency.h");
-constexpr uint64_t WAIT_NS = 2000000000ull;
 
 struct Params {
   const int32_t* offset;
@@ -44,10 +43,12 @@ struct Params {
   int m_blocks, n_blocks, n_width, ks;  // n_width: of a tile, a multiple of 16
   float* C;
   int32_t* status;
+  Fault fault;
 };
 
 __global__ void __launch_bounds__(THREADS, 1)
-    grouped_grad_few_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p) {
+    grouped_grad_few_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                        const __grid_constant__ Params p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw_addr = ptx::smem_u32(smem_raw);
   uint8_t* smem = smem_raw + (((raw_addr + 1023u) & ~1023u) - raw_addr);
@@ -99,19 +100,20 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (warp == 0) {
     const bool issuer = ptx::elect_one();
+    const uint32_t missing = p.fault.missing(split);
     const bool two_a = p.out - m0 > 64, two_b = p.n_width > 64;  // boxes
     const uint32_t bytes = (2 + (two_a ? 1 : 0) + (two_b ? 1 : 0)) * CHUNK_BYTES;
     int stage = 0, issued = 0;
     uint32_t phase = 0;
     bool last_here = false;
     for (int kb = kb0; kb < kb1; ++kb) {
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, WAIT_NS, p.status))) break;
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, p.fault.wait_ns, p.status))) break;
       const int k0 = r.x + kb * BK, left = r.y - k0;
       const bool clear = left < BK && left % 16 != 0;  // (the last block only)
       uint8_t* sa = smem + stage * SBYTES;
       if (issuer) {
         uint64_t* bar = clear ? here : &full[stage];
-        ptx::mbar_arrive_expect_tx(bar, bytes);
+        ptx::mbar_arrive_expect_tx(bar, bytes + missing);
         ptx::tma_load_2d(sa, &tmA, bar, m0, k0);
         if (two_a) ptx::tma_load_2d(sa + CHUNK_BYTES, &tmA, bar, m0 + 64, k0);
         ptx::tma_load_2d(sa + A_BYTES, &tmB, bar, n0, k0);
@@ -120,7 +122,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
       if (clear) {
         last_here = true;
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait(here, 0, WAIT_NS, p.status))) break;
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait(here, 0, p.fault.wait_ns, p.status))) break;
         const uint32_t to = ptx::smem_u32(sa) + left * 128;
         const int pieces = ((left + 15) / 16 * 16 - left) * 8;  // of 16 bytes, in a box
         for (int b = 0; b < 4; ++b)
@@ -135,9 +137,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int n_tail = min(issued, STAGES);  // drain (bounded): the loads still in flight
     for (int i = 0; i < n_tail; ++i) {
       if (--stage < 0) { stage = STAGES - 1; phase ^= 1u; }
-      ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status);
+      ptx::mbar_wait(&full[stage], phase, p.fault.wait_ns, p.status);
     }
-    if (last_here) ptx::mbar_wait(here, 0, WAIT_NS, p.status);
+    if (last_here) ptx::mbar_wait(here, 0, p.fault.wait_ns, p.status);
   } else if (warp == 1) {
     const bool issuer = ptx::elect_one();
     const uint32_t idesc = ptx::idesc_bf16_f32(BM, 0, true, true) | static_cast<uint32_t>(p.n_width >> 3) << 17;
@@ -150,8 +152,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     int kb = kb0;
     for (; kb < kb1; ++kb) {
       const bool first = (kb - kb0) % PART_BLOCKS == 0;
-      if (first) good = __all_sync(0xffffffffu, ptx::mbar_wait(&tempty[acc], aphase ^ 1u, WAIT_NS, p.status));
-      good = good && __all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status));
+      if (first) good = __all_sync(0xffffffffu, ptx::mbar_wait(&tempty[acc], aphase ^ 1u, p.fault.wait_ns, p.status));
+      good = good && __all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, p.fault.wait_ns, p.status));
       if (!good) break;
       ptx::tc_fence_after();
       const int left = r.y - (r.x + kb * BK), steps = left < BK ? (left + 15) / 16 : BK / 16;
@@ -173,7 +175,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     // stage that they read.
     if (kb > kb0) {
       const int at = stage > 0 ? stage - 1 : STAGES - 1;
-      ptx::mbar_wait(&empty[at], stage > 0 ? phase : phase ^ 1u, WAIT_NS, p.status);
+      ptx::mbar_wait(&empty[at], stage > 0 ? phase : phase ^ 1u, p.fault.wait_ns, p.status);
     }
   }
   // ------------------------------------------------------------------ epilogue
@@ -191,7 +193,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     bool ok = true;
     for (int kb = kb0; kb == kb0 || kb < kb1; kb += PART_BLOCKS) {
       const bool any = kb < kb1, last = kb + PART_BLOCKS >= kb1;
-      if (any) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, WAIT_NS, p.status));
+      if (any) ok = __all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, p.fault.wait_ns, p.status));
       if (!ok) break;
       ptx::tc_fence_after();
 #pragma unroll 1
@@ -297,7 +299,7 @@ int grad_few_splits(const Call& c, int sms) {
 
 sky_status launch_grad_few(const Call& c, int splits, cudaStream_t st) {
   Params p{c.offset, c.groups, c.rows, c.out, c.in, ceil_div(c.out, BM), ceil_div(c.in, BN), 0, splits,
-           static_cast<float*>(c.C), c.status};
+           static_cast<float*>(c.C), c.status, fault_of(splits)};
   p.n_width = ceil_div(ceil_div(c.in, p.n_blocks), 16) * 16;
   CUtensorMap ta, tb;
   const bool ok = gemm::make_map(&ta, c.A, c.rows, c.out, 64) && gemm::make_map(&tb, c.B, c.rows, c.in, 64);

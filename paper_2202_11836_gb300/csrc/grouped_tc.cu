@@ -49,7 +49,6 @@ constexpr int BM = 128, BK = 64;             // of a CTA: features; K of a stage
 constexpr int TILE_M = 2 * BM, TILE_N = 256; // of a pair
 constexpr int A_BYTES = BM * BK * 2, B_BYTES = TILE_N / 2 * BK * 2, SBYTES = A_BYTES + B_BYTES;
 constexpr int CHUNK_BYTES = 64 * BK * 2;     // one 64-wide MN-major box
-constexpr uint64_t WAIT_NS = 2000000000ull;  // of any one wait
 constexpr uint32_t SLEEP_NS = 20000;         // suspend hint of the epilogue's accumulator wait
 
 // Launch shape of XWT and XW: eight epilogue warps, each with two staging buffers of 32 x 32 16-bit
@@ -86,6 +85,7 @@ struct Params {
   const __half* aux;
   __half* aux_out;
   int32_t* status;
+  Fault fault;
 };
 struct Maps {
   CUtensorMap weights, C, aux_out;
@@ -192,10 +192,10 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
       const int f0 = u % p.f_blocks * TILE_M + static_cast<int>(rank) * BM;
       const int half = ((t.count + 31) & ~31) / 2;  // tokens whose rows this CTA loads
       const int box = half <= 16 ? 0 : half <= 32 ? 1 : half <= 64 ? 2 : 3;
-      const uint32_t bytes = 2 * (A_BYTES + (16 << box) * BK * 2);
+      const uint32_t bytes = 2 * (A_BYTES + (16 << box) * BK * 2) + p.fault.missing(0);
       const int r0 = t.row + static_cast<int>(rank) * half;
       for (int kb = 0; kb < p.k_blocks; ++kb) {
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, WAIT_NS, p.status));
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, p.fault.wait_ns, p.status));
         if (!ok) break;
         if (issuer) {
           uint8_t* sa = smem + stage * SBYTES;
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
     const int n_tail = leader ? min(issued, NST) : 0;
     for (int i = 0; i < n_tail; ++i) {
       if (--stage < 0) { stage = NST - 1; phase ^= 1u; }
-      ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status);
+      ptx::mbar_wait(&full[stage], phase, p.fault.wait_ns, p.status);
     }
   } else if (warp == 1) {
     // the whole warp walks, so that descriptors stay warp-uniform, and one lane issues
@@ -234,11 +234,11 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
       for (int u = cid; ok && walk.find(u / p.f_blocks, t); u += ncl) {
         const uint32_t idesc =
             ptx::idesc_bf16_f32(TILE_M, 0, W_MN, false) | static_cast<uint32_t>(((t.count + 31) & ~31) >> 3) << 17;
-        if (!__all_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aphase ^ 1u, WAIT_NS, p.status))) break;
+        if (!__all_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aphase ^ 1u, p.fault.wait_ns, p.status))) break;
         ptx::tc_fence_after();
         const uint32_t d_tmem = tmem_base + acc * TILE_N;
         for (int kb = 0; kb < p.k_blocks; ++kb) {
-          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status));
+          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&full[stage], phase, p.fault.wait_ns, p.status));
           if (!ok) break;
           ptx::tc_fence_after();
           if (issuer) {
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
       // All issued MMAs must finish before TMEM is released.
       if (issuer) ptx::tc_commit_pair(done, 1);
       __syncwarp();
-      ptx::mbar_wait(done, 0, WAIT_NS, p.status);
+      ptx::mbar_wait(done, 0, p.fault.wait_ns, p.status);
     }
   } else {
     // Warp w has TMEM lanes 32 q .. (features) and every (EW / 4)-th chunk of 32 tokens.  One lane
@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(Shape<EPI>::THREADS, 1)
           if (f < p.features && n < next.count) ptx::prefetch_l2(p.aux + static_cast<int64_t>(next.row + n) * p.features + f);
         }
       }
-      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, WAIT_NS, p.status, SLEEP_NS))) break;
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, p.fault.wait_ns, p.status, SLEEP_NS))) break;
       ptx::tc_fence_after();
       const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * TILE_N;
       // of a chunk's 8 tokens b: r[4 b ..] features lane / 4 and + 8, r[16 + 4 b ..] + 16 and + 24;
@@ -462,11 +462,12 @@ struct GradParams {
   int groups, rows, out, in;
   int m_blocks, n_blocks;  // 256 of out; of in
   int32_t* status;
+  Fault fault;
 };
 
 __global__ void __launch_bounds__(GradShape::THREADS, 1)
     grouped_grad_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                    const __grid_constant__ CUtensorMap tmC, const GradParams p) {
+                    const __grid_constant__ CUtensorMap tmC, const __grid_constant__ GradParams p) {
   using SH = GradShape;
   constexpr int NST = SH::STAGES, EW = SH::EW;
   extern __shared__ uint8_t smem_raw[];
@@ -526,7 +527,7 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
       const int m0 = u % per_group / p.n_blocks * TILE_M + static_cast<int>(rank) * BM;
       const int n0 = u % p.n_blocks * TILE_N + static_cast<int>(rank) * (TILE_N / 2);
       for (int k0 = r.x; k0 < r.y; k0 += BK) {
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, WAIT_NS, p.status));
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&empty[stage], phase ^ 1u, p.fault.wait_ns, p.status));
         if (!ok) break;
         const bool clear = r.y - k0 < BK && (r.y - k0) % 16 != 0;
         if (issuer) {
@@ -534,13 +535,13 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
           uint8_t* sb = sa + A_BYTES;
           if (clear) {
             if (leader) ptx::mbar_arrive(&full[stage]);
-            ptx::mbar_arrive_expect_tx(&here[stage], SBYTES);
+            ptx::mbar_arrive_expect_tx(&here[stage], SBYTES + p.fault.missing(0));
             ptx::tma_load_2d(sa, &tmA, &here[stage], m0, k0);
             ptx::tma_load_2d(sa + CHUNK_BYTES, &tmA, &here[stage], m0 + 64, k0);
             ptx::tma_load_2d(sb, &tmB, &here[stage], n0, k0);
             ptx::tma_load_2d(sb + CHUNK_BYTES, &tmB, &here[stage], n0 + 64, k0);
           } else {
-            if (leader) ptx::mbar_arrive_expect_tx(&full[stage], 2 * SBYTES);
+            if (leader) ptx::mbar_arrive_expect_tx(&full[stage], 2 * SBYTES + p.fault.missing(0));
             const uint32_t bar = ptx::mapa_shared(ptx::smem_u32(&full[stage]), 0);
             ptx::tma_load_2d_pair(sa, &tmA, bar, m0, k0);
             ptx::tma_load_2d_pair(sa + CHUNK_BYTES, &tmA, bar, m0 + 64, k0);
@@ -559,8 +560,8 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
     const int n_tail = min(issued, NST);
     for (int i = 0; i < n_tail; ++i) {
       if (--stage < 0) { stage = NST - 1; phase ^= 1u; }
-      if (by_here >> stage & 1) ptx::mbar_wait(&here[stage], (here_phase >> stage & 1) ^ 1u, WAIT_NS, p.status);
-      else if (leader) ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status);
+      if (by_here >> stage & 1) ptx::mbar_wait(&here[stage], (here_phase >> stage & 1) ^ 1u, p.fault.wait_ns, p.status);
+      else if (leader) ptx::mbar_wait(&full[stage], phase, p.fault.wait_ns, p.status);
     }
   } else if (warp == 1) {
     if (leader) {
@@ -578,15 +579,15 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
         for (int k0 = r.x; k0 < r.y; k0 += BK) {
           const bool first = (k0 - r.x) % PART_ROWS == 0;
           if (first) {
-            ok = __all_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aphase ^ 1u, WAIT_NS, p.status));
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait_cluster(&tempty[acc], aphase ^ 1u, p.fault.wait_ns, p.status));
             if (!ok) break;
             ptx::tc_fence_after();
             d_tmem = tmem_base + acc * TILE_N;
           }
           const int left = r.y - k0, steps = left < BK ? (left + 15) / 16 : BK / 16;
-          bool got = ptx::mbar_wait(&full[stage], phase, WAIT_NS, p.status);
+          bool got = ptx::mbar_wait(&full[stage], phase, p.fault.wait_ns, p.status);
           if (left < BK && left % 16 != 0) {
-            got = got && ptx::mbar_wait_cluster(&cleared[stage], c_phase >> stage & 1, WAIT_NS, p.status);
+            got = got && ptx::mbar_wait_cluster(&cleared[stage], c_phase >> stage & 1, p.fault.wait_ns, p.status);
             c_phase ^= 1u << stage;
           }
           ok = __all_sync(0xffffffffu, got);
@@ -610,7 +611,7 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
       }
       if (issuer) ptx::tc_commit_pair(done, 1);
       __syncwarp();
-      ptx::mbar_wait(done, 0, WAIT_NS, p.status);
+      ptx::mbar_wait(done, 0, p.fault.wait_ns, p.status);
     }
   } else if (warp == 2 + EW) {
     // ------------------------------------------- rows behind a group's last
@@ -623,7 +624,7 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
       at += blocks;
       if (left % 16 == 0) continue;
       const int stage = (at - 1) % NST;
-      ok = __all_sync(0xffffffffu, ptx::mbar_wait(&here[stage], phase >> stage & 1, WAIT_NS, p.status));
+      ok = __all_sync(0xffffffffu, ptx::mbar_wait(&here[stage], phase >> stage & 1, p.fault.wait_ns, p.status));
       phase ^= 1u << stage;
       if (!ok) break;
       const uint32_t s = ptx::smem_u32(smem) + stage * SBYTES;
@@ -649,7 +650,7 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
       const int n0 = u % p.n_blocks * TILE_N + half * (TILE_N / 2);
       float sum[4][32] = {};  // (all of it, for a group without rows)
       for (int k0 = rr.x; k0 < rr.y; k0 += PART_ROWS) {
-        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, WAIT_NS, p.status, SLEEP_NS));
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&tfull[acc], aphase, p.fault.wait_ns, p.status, SLEEP_NS));
         if (!ok) break;
         ptx::tc_fence_after();
         const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * TILE_N + half * (TILE_N / 2);
@@ -758,7 +759,8 @@ sky_status launch_tc(const Call& c, cudaStream_t st) {
     const bool ok = gemm::make_map(&ta, c.A, c.rows, c.out, 64) && gemm::make_map(&tb, c.B, c.rows, c.in, 64) &&
                     gemm::make_map_3d(&tc, c.C, c.groups, c.out, c.in, 32, 32, true);
     SKY_CHECK(ok, SKY_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d x %d x %d)", c.groups, c.out, c.in);
-    const GradParams p{c.offset, c.groups, c.rows, c.out, c.in, ceil_div(c.out, TILE_M), ceil_div(c.in, TILE_N), c.status};
+    const GradParams p{c.offset, c.groups, c.rows, c.out, c.in, ceil_div(c.out, TILE_M), ceil_div(c.in, TILE_N),
+                       c.status, fault_of(1)};
     SKY_CHECK(static_cast<int64_t>(p.groups) * p.m_blocks * p.n_blocks <= 0x3fffffff, SKY_ERR_UNSUPPORTED,
               "grouped weight gradient too large");
     e = launch_grad(ta, tb, tc, p, sms, st);
@@ -777,6 +779,7 @@ sky_status launch_tc(const Call& c, cudaStream_t st) {
     p.aux = static_cast<const __half*>(c.aux);
     p.aux_out = static_cast<__half*>(c.aux_out);
     p.status = c.status;
+    p.fault = fault_of(1);
     // tiles of tokens: every group that has any may end inside one
     const int64_t units = (c.rows / TILE_N + static_cast<int64_t>(std::min(c.groups, c.rows))) * p.f_blocks;
     SKY_CHECK(units <= 0x3fffffff, SKY_ERR_UNSUPPORTED, "grouped product too large");
