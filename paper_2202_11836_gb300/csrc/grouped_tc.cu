@@ -481,6 +481,7 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
   uint64_t* tempty = tfull + 2;
   uint64_t* done = tempty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+  const uint32_t sent = ptx::smem_u32(tmem_slot + 1);  // blocks that this CTA's producer has sent
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = ptx::cluster_ctarank();
@@ -498,6 +499,7 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
       ptx::mbar_init(&tempty[a], 2 * EW);
     }
     ptx::mbar_init(done, 1);
+    ptx::st_shared_u32(sent, 0);
     ptx::fence_mbar_init_cluster();
     ptx::fence_proxy_async_smem();
     ptx::prefetch_tensormap(&tmA);
@@ -553,6 +555,7 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
         by_here = (by_here & ~(1u << stage)) | (clear ? 1u << stage : 0u);
         if (clear) here_phase ^= 1u << stage;
         ++issued;
+        if (issuer) ptx::st_shared_u32(sent, issued);
         if (++stage == NST) { stage = 0; phase ^= 1u; }
       }
     }
@@ -624,9 +627,20 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
       at += blocks;
       if (left % 16 == 0) continue;
       const int stage = (at - 1) % NST;
-      ok = __all_sync(0xffffffffu, ptx::mbar_wait(&here[stage], phase >> stage & 1, p.fault.wait_ns, p.status));
+      // Whole tiles may lie between two such blocks, so this wait goes on while others are being sent.
+      bool got = false;
+      for (uint32_t before = ~0u;;) {
+        got = ptx::mbar_wait(&here[stage], phase >> stage & 1, p.fault.wait_ns, nullptr);
+        const uint32_t now = ptx::ld_shared_u32(sent);
+        if (got || now == before) break;
+        before = now;
+      }
+      ok = __all_sync(0xffffffffu, got);
       phase ^= 1u << stage;
-      if (!ok) break;
+      if (!ok) {
+        if (lane == 0 && p.status) atomicOr(p.status, kStatusTimeout);
+        break;
+      }
       const uint32_t s = ptx::smem_u32(smem) + stage * SBYTES;
       const int pieces = ((left + 15) / 16 * 16 - left) * 8;  // of 16 bytes, in a 64-wide box
 #pragma unroll

@@ -74,3 +74,34 @@ def test_waits_that_run_out(name, form, epi, sizes, out, in_, skip):
     assert bool((c == MARK).all()) and (slope is None or bool((slope == MARK).all()))
     assert go() == 0
     assert torch.equal(c, want) and (slope is None or torch.equal(slope, want_slope))
+
+
+def test_a_limit_is_of_a_wait_not_of_a_call():
+    """A weight gradient of several limits' length: the rows behind a group's last are cleared by a warp that has
+    nothing to do before, here for the 1.2 ms that a pair takes for a tile of the first group."""
+    sizes, n = [262144, 7], 2560  # 100 tiles of 256 x 256 a group: most pairs take one of either
+    g = torch.Generator(device="cuda").manual_seed(3)
+    a, b = (torch.randn(sum(sizes), n, device="cuda", generator=g, dtype=torch.bfloat16) for _ in range(2))
+    offset = torch.tensor([0, sizes[0], sum(sizes)], dtype=torch.int32, device="cuda")
+    c = torch.full((2, n, n), MARK, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    shape = L.SkyGroupedShape(2, sum(sizes), n, n, L.SKY_DTYPE_BF16)
+    ws = torch.empty(L.lib().sky_grouped_gemm_workspace_bytes(XTW, shape, L.SKY_DTYPE_FP32), dtype=torch.uint8, device="cuda")
+    L.lib().sky_debug_gemm_fault(300_000, 0)
+    try:
+        L.call("sky_grouped_gemm", XTW, shape, P(offset), P(a), P(b), P(c), L.SKY_DTYPE_FP32, L.SKY_EPI_STORE, None, None, None,
+               P(ws), ws.numel(), P(status), C.c_void_p(int(torch.cuda.current_stream().cuda_stream)))
+        torch.cuda.synchronize()
+    finally:
+        L.lib().sky_debug_gemm_fault(0, 0)
+    assert status.item() == 0
+    lo = sizes[0]
+    want = a[lo:].double().T @ b[lo:].double()
+    # seven products, each addition off by up to 2^-23 of the sum of magnitudes
+    size = a[lo:].double().abs().T @ b[lo:].double().abs()
+    assert bool(((c[1].double() - want).abs() <= 8 * 2.0 ** -23 * size).all())
+    part = slice(1000, 1300)
+    want = a[:lo, part].double().T @ b[:lo, part].double()
+    # parts of 512 rows, each cut off 32 times by up to 2^-23, and 512 of them added with half of that
+    size = a[:lo, part].double().abs().T @ b[:lo, part].double().abs()
+    assert bool(((c[0, part, part].double() - want).abs() <= (32 + 256) * 2.0 ** -23 * size).all())
