@@ -193,6 +193,33 @@ cudaError_t allow_smem(OncePerDevice& once, K* kern, size_t bytes) {
   });
 }
 
+// Clusters of `size` CTAs that the current device holds at once, one CTA an SM, 0 on error.  `count` is the
+// kernel's own for that size, static at its launch site; its shared memory is allowed before.
+template <typename K>
+int clusters_at_once(CountPerDevice& count, K* kern, int size, int threads, size_t smem, int sms) {
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess) return 0;
+  return count(device, [&] {
+    cudaLaunchConfig_t q = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = size;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    q.gridDim = dim3(size * (sms / size));
+    q.blockDim = dim3(threads);
+    q.dynamicSmemBytes = smem;
+    q.attrs = at;
+    q.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &q) != cudaSuccess) {
+      cudaGetLastError();
+      n = 0;
+    }
+    return n;
+  });
+}
+
 // cudaLaunchKernelEx with the programmatic-serialization attribute (when
 // enabled) and optionally a cluster of `cluster_x` CTAs.
 template <typename... KArgs, typename... Args>

@@ -708,27 +708,9 @@ cudaError_t launch_variant(const Params& p, int sms, const CUtensorMap& ta, cons
   if (attr != cudaSuccess) return attr;
   int ctas = sms;
   if constexpr (PAIR) {
-    static int max_clusters = [&] {
-      cudaLaunchConfig_t q = {};
-      cudaLaunchAttribute at[1];
-      at[0].id = cudaLaunchAttributeClusterDimension;
-      at[0].val.clusterDim.x = 2;
-      at[0].val.clusterDim.y = 1;
-      at[0].val.clusterDim.z = 1;
-      q.blockDim = dim3(SH::THREADS);
-      q.dynamicSmemBytes = SH::SMEM;
-      q.attrs = at;
-      q.numAttrs = 1;
-      q.gridDim = dim3(2 * (sms / 2));
-      int n = 0;
-      if (cudaOccupancyMaxActiveClusters(&n, kern, &q) != cudaSuccess) {
-        cudaGetLastError();
-        n = 0;
-      }
-      return n;
-    }();
-    if (max_clusters < 1) return cudaErrorLaunchOutOfResources;
-    ctas = max_clusters;
+    static CountPerDevice count;
+    ctas = clusters_at_once(count, kern, 2, SH::THREADS, SH::SMEM, sms);
+    if (ctas < 1) return cudaErrorLaunchOutOfResources;
   }
   const int units = p.m_tiles * p.n_tiles * p.splits;
   const int grid = units < ctas ? units : ctas;

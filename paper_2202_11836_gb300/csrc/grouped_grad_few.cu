@@ -258,27 +258,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
 }
 
-// Clusters of `size` that the device holds at once.
-int clusters_at_once(int size, int sms) {
-  cudaLaunchConfig_t q = {};
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = size;
-  at[0].val.clusterDim.y = 1;
-  at[0].val.clusterDim.z = 1;
-  q.blockDim = dim3(THREADS);
-  q.dynamicSmemBytes = SMEM;
-  q.attrs = at;
-  q.numAttrs = 1;
-  q.gridDim = dim3(size * (sms / size));
-  int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, grouped_grad_few_tc, &q) != cudaSuccess) {
-    cudaGetLastError();
-    n = 0;
-  }
-  return n;
-}
-
 }  // namespace
 
 // As many CTAs a tile as have their rows and leave all clusters on the device at once (76, 36 and 15
@@ -289,12 +268,15 @@ int clusters_at_once(int size, int sms) {
 int grad_few_splits(const Call& c, int sms) {
   static OncePerDevice once;
   if (c.form != SKY_GEMM_XTW || allow_smem(once, grouped_grad_few_tc, SMEM) != cudaSuccess) return 1;
-  static const int most[] = {clusters_at_once(2, sms), clusters_at_once(4, sms), clusters_at_once(8, sms)};
+  static CountPerDevice count[3];
+  const auto most = [&](int splits) {
+    return clusters_at_once(count[splits / 4], grouped_grad_few_tc, splits, THREADS, SMEM, sms);
+  };
   const int64_t units = static_cast<int64_t>(c.groups) * ceil_div(c.out, BM) * ceil_div(c.in, BN);
   const int rows = ceil_div(c.rows, c.groups);  // of a mean group
-  if (units <= most[2] && rows >= 1024) return 8;
-  if (units <= most[1] && rows >= 512) return 4;
-  return units <= most[0] ? 2 : 1;
+  if (rows >= 1024 && units <= most(8)) return 8;
+  if (rows >= 512 && units <= most(4)) return 4;
+  return units <= most(2) ? 2 : 1;
 }
 
 sky_status launch_grad_few(const Call& c, int splits, cudaStream_t st) {

@@ -712,28 +712,6 @@ __global__ void __launch_bounds__(GradShape::THREADS, 1)
   }
 }
 
-// Clusters of two that the device holds at once, one CTA an SM.
-template <typename K>
-int pairs_at_once(K* kern, int threads, size_t smem, int sms) {
-  cudaLaunchConfig_t q = {};
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = 2;
-  at[0].val.clusterDim.y = 1;
-  at[0].val.clusterDim.z = 1;
-  q.blockDim = dim3(threads);
-  q.dynamicSmemBytes = smem;
-  q.attrs = at;
-  q.numAttrs = 1;
-  q.gridDim = dim3(2 * (sms / 2));
-  int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, kern, &q) != cudaSuccess) {
-    cudaGetLastError();
-    n = 0;
-  }
-  return n;
-}
-
 template <bool W_MN, int EPI>
 cudaError_t launch_rows(const Maps& maps, const Params& p, int64_t units, int sms, cudaStream_t st) {
   using SH = Shape<EPI>;
@@ -741,7 +719,8 @@ cudaError_t launch_rows(const Maps& maps, const Params& p, int64_t units, int sm
   static OncePerDevice once;
   const cudaError_t attr = allow_smem(once, kern, SH::SMEM);
   if (attr != cudaSuccess) return attr;
-  static const int most = pairs_at_once(kern, SH::THREADS, SH::SMEM, sms);
+  static CountPerDevice count;
+  const int most = clusters_at_once(count, kern, 2, SH::THREADS, SH::SMEM, sms);
   if (most < 1) return cudaErrorLaunchOutOfResources;
   const int pairs = static_cast<int>(std::min<int64_t>(units, most));
   return launch_pdl(kern, dim3(2 * pairs), dim3(SH::THREADS), SH::SMEM, st, 2, maps, p);
@@ -753,7 +732,8 @@ cudaError_t launch_grad(const CUtensorMap& ta, const CUtensorMap& tb, const CUte
   static OncePerDevice once;
   const cudaError_t attr = allow_smem(once, grouped_grad_tc, SH::SMEM);
   if (attr != cudaSuccess) return attr;
-  static const int most = pairs_at_once(grouped_grad_tc, SH::THREADS, SH::SMEM, sms);
+  static CountPerDevice count;
+  const int most = clusters_at_once(count, grouped_grad_tc, 2, SH::THREADS, SH::SMEM, sms);
   if (most < 1) return cudaErrorLaunchOutOfResources;
   const int64_t units = static_cast<int64_t>(p.groups) * p.m_blocks * p.n_blocks;
   const int pairs = static_cast<int>(std::min<int64_t>(units, most));
