@@ -110,7 +110,7 @@ typedef struct {
 } sky_grouped_shape;
 
 /* Scratch bytes of sky_grouped_gemm; 0 for a call that it refuses.  The workspace must be
- * 16-byte aligned. */
+ * 16-byte aligned.  (The present kernels write nothing to it.) */
 size_t sky_grouped_gemm_workspace_bytes(sky_gemm_form form, const sky_grouped_shape* shape,
                                         sky_dtype out_dtype);
 

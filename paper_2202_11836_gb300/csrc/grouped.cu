@@ -49,7 +49,8 @@ Fault fault_of(int splits) {
 
 namespace {
 
-size_t workspace(sky_gemm_form, const sky_grouped_shape&) { return 16; }
+// Asked for and checked, not used: partial sums go through distributed shared memory.
+constexpr size_t WORKSPACE = 16;
 
 // Column sums over the rows of a group: TX threads take TX V columns (512 or 128 bytes of a row), the
 // others of a CTA other rows, and their sums are added in order.  A group's rows are shared by
@@ -144,7 +145,7 @@ extern "C" {
 
 size_t sky_grouped_gemm_workspace_bytes(sky_gemm_form form, const sky_grouped_shape* shape, sky_dtype out_dtype) {
   if (grouped::check(shape, true) != SKY_OK || grouped::check_form(form, *shape, out_dtype) != SKY_OK) return 0;
-  return grouped::workspace(form, *shape);
+  return grouped::WORKSPACE;
 }
 
 sky_status sky_grouped_gemm(sky_gemm_form form, const sky_grouped_shape* shape, const int32_t* d_offset, const void* A,
@@ -172,9 +173,9 @@ sky_status sky_grouped_gemm(sky_gemm_form form, const sky_grouped_shape* shape, 
                       (epilogue != SKY_EPI_GELU_BWD || grouped::on(aux, 16)) &&
                       (epilogue != SKY_EPI_BIAS_GELU || grouped::on(aux_out, 16))),
             SKY_ERR_UNSUPPORTED, "bf16 grouped products need A, B, C, aux and aux_out 16-byte aligned");
-  SKY_CHECK(workspace_bytes >= grouped::workspace(form, *shape), SKY_ERR_INVALID_ARG, "workspace too small");
+  SKY_CHECK(workspace_bytes >= grouped::WORKSPACE, SKY_ERR_INVALID_ARG, "workspace too small");
   const grouped::Call c{form, shape->groups, shape->rows, shape->out, shape->in, d_offset, A, B, C, epilogue, bias, aux,
-                        aux_out, workspace, workspace_bytes, d_status};
+                        aux_out, d_status};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   return bf16 ? grouped::launch_tc(c, st) : grouped::launch_simt(c, st);
   ABI_GUARD_END

@@ -21,8 +21,6 @@ struct Call {
   sky_epilogue epi;
   const void *bias, *aux;
   void* aux_out;
-  void* ws;
-  size_t ws_bytes;
   int32_t* status;
 };
 

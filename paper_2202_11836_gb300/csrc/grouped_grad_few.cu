@@ -16,6 +16,8 @@
 // took 0.4 to 1.9 us more (16384 rows 26.8, 3769 rows of 160 x 80 over 38 groups 7.4 against 6.0).
 #include <cuda.h>
 
+#include <algorithm>
+
 #include "common.cuh"
 #include "gemm.h"
 #include "grouped.cuh"
@@ -35,7 +37,8 @@ constexpr int COLUMNS = 512;              // TMEM: two accumulators and the sum 
 constexpr int THREADS = 192;
 constexpr int RECV_OFF = STAGES * SBYTES, BAR_OFF = RECV_OFF + BM * BN * 4;
 constexpr int SMEM = BAR_OFF + 256 + 1024;
-static_assert(SMEM + kSmemPerCta + kSplitAttentionSmem + kSmemPerCta > kSmemPerSM, "see residency.h");
+static_assert(SMEM + kSmemPerCta + std::min(kSplitAttentionSmem, kClusterProductSmem) + kSmemPerCta > kSmemPerSM,
+              "see residency.h");
 
 struct Params {
   const int32_t* offset;

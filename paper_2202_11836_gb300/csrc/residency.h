@@ -10,7 +10,8 @@
 //   the attention kernels where they are split over a cluster (the forward, delta, dQ,
 //   dK/dV, the one-launch backward: 256 columns) take so much shared memory that two of their
 //   CTAs leave no room for a third or for a cluster product's;
-//   cluster products (at most 128 columns) take at least kClusterProductSmem.
+//   cluster products (at most 128 columns) take at least kClusterProductSmem;
+//   grouped weight gradients of few tiles (512 columns) take so much that neither of those fits beside them.
 // (The persistent product takes a whole SM, and everything else that allocates
 // finishes by itself.)
 #pragma once
