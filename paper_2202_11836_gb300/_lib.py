@@ -114,6 +114,10 @@ class SkyAdamwConfig(C.Structure):
                 ("states", C.c_int)]
 
 
+class SkyAdamwNow(C.Structure):  # in device memory
+    _fields_ = [("lr", C.c_float), ("correction1", C.c_float), ("correction2", C.c_float), ("grad_scale", C.c_float)]
+
+
 _VP, _I32, _SZ = C.c_void_p, C.c_int32, C.c_size_t
 _SIGNATURES = {
     "sky_slice_create": (C.c_int, [C.POINTER(SkySliceConfig), C.POINTER(_VP)]),
