@@ -32,6 +32,11 @@ extern "C" {
  *         value is below 1e-30 is all 0.  The update itself uses the moments before they
  *         are rounded.  A change of a moment by less than half a step (1/16 of m, 1/32
  *         of r, at most) beside its block's largest is not kept.
+ *         So r does not end at its 32-bit value but near it: over 24576 values and 12000
+ *         steps of N(0, 1) gradients, of one size in a block or of sizes up to a
+ *         hundredfold apart, it settles at 0.77 to 1.47 times that (5th to 95th percentile;
+ *         the median 0.98 to 1.19) with beta2 of 0.99 to 0.9999, and at 0.94 to 1.07 with
+ *         0.95.  It follows gradients that shrink together.
  * Tensors of zeros are the moments before the first step, in either form. */
 typedef enum { SKY_STATE_FP32 = 0, SKY_STATE_8BIT = 1 } sky_state_type;
 #define SKY_STATE_BLOCK 256

@@ -26,7 +26,7 @@ def structs():
             yield name, fields
 
 
-@pytest.mark.parametrize("name,fields", structs(), ids=lambda v: v if isinstance(v, str) else None)
+@pytest.mark.parametrize("name,fields", list(structs()), ids=lambda v: v if isinstance(v, str) else None)
 def test_struct(name, fields):
     t = getattr(L, "".join(p.capitalize() for p in name.split("_")))
     assert [n.rstrip("_") for n, _ in t._fields_] == [n for n, _ in fields]
