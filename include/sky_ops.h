@@ -297,12 +297,11 @@ sky_status sky_column_sum_noalloc(const void* x, int32_t T, int32_t N, sky_dtype
  * limit_ns caps every mbarrier wait of GEMM launches, grouped ones among them, made
  * after the call (0 restores the default, 2 s; below 0.1 ms it is 0.1 ms).
  * skip_loads != 0 makes the TMA producer arrive on its barriers without issuing
- * the copies (of grouped products: expecting more than they bring), so the
- * consumers' waits run out: the kernel then sets the timeout bit (2) of the status word it was
- * given, frees its tensor memory and exits without storing the tiles
- * concerned, and the context stays usable.  skip_loads == 2: of a product
- * whose K range is split over a cluster only the last part's copies are left
- * out (or expected short).
+ * the copies (grouped products: expecting more than they bring), so the
+ * consumers' waits run out: the kernel then sets the timeout bit (2) of the
+ * status word it was given, frees its tensor memory and exits without storing
+ * the tiles concerned, and the context stays usable.  skip_loads == 2: only the
+ * last part's of a product whose K range is split over a cluster.
  * Process-wide setting; pass (0, 0) to restore normal operation. */
 void sky_debug_gemm_fault(uint64_t limit_ns, int32_t skip_loads);
 

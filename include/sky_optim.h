@@ -80,8 +80,9 @@ typedef struct {
  * `tensors` is host memory, read before the call returns.  d_now: NULL (lr and step of
  * the config, gradients as they are) or a device pointer read when the work runs.
  * Tensors may start anywhere on their types' grids (on 16 bytes they are faster), and may
- * not overlap each other.  A gradient that is not finite, or whose square is not in fp32,
- * leaves its value's second moment, and in 8 bits its whole block's moments, not finite.
+ * not overlap each other.  A gradient that is not finite leaves its value, and in 8 bits
+ * its whole block's moments, not finite; a finite one whose square overflows fp32 does so
+ * to its second moment, in 8 bits to both of its whole block.
  * Errors: INVALID_ARG (null, n_tensors < 1, n < 1, the ranges above, a pointer off its
  * type's grid), UNSUPPORTED (more than 2^40 values in a tensor, or 2^41 in all), CUDA. */
 sky_status sky_adamw_step(const sky_adamw_config* config, const sky_adamw_tensor* tensors,

@@ -58,7 +58,7 @@ __device__ __forceinline__ void check_offsets(const int32_t* offset, int groups,
 // outputs are what bf16 and fp16 make of the exact values but for a few borders, in the tail too.  The
 // three terms of the dense epilogues (gelu_and_grad_as2) are off by 2.2e-5 of 1, 0.4% of GELU(-3) and 2% of
 // GELU(-5).  16384 rows, 8 groups of 4096 x 1024: 100.2 us with those, 100.7 with these; with one more
-// term 102, and with the sign by arithmetic in the place of selects 4 more.
+// term 102, and with the sign by arithmetic in the place of selects 5 more.
 __device__ __forceinline__ void gelu_and_grad2(float h0, float h1, float2& g, float2& gp) {
   const auto both = [](float v) { return pack2(v, v); };
   constexpr float c = 0.265f;

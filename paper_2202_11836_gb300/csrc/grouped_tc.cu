@@ -23,14 +23,13 @@
 // What bounds them: a 256 x 256 tile on a pair takes 64 bytes a clock and SM of operands at the
 // tensor cores' full rate, which is what an SM takes in, and what it sends out competes with that.
 // 16384 rows, 8 groups of 4096 x 1024, a few calls: stored as it is 80 us (1.7 PFLOP/s), bias and
-// GELU with their two outputs 99, a gradient through GELU' 90, weight gradients (134 MB out) 91; without
+// GELU with their two outputs 100, a gradient through GELU' 90, weight gradients (134 MB out) 91; without
 // their stores the second and the last take 83 and 79.  Kept up for a second the power cap takes 13%
-// more.  Stores of the GELU tile, us, a GELU of fewer
-// terms taking one less: 64 bytes of a row by lanes 118, four bytes a lane 121, by TMA from
-// a buffer a warp 102, from two 98, from two that two warps share (128 bytes a row) 109, from two for one
-// output at a time 105; sixteen warps 111.  Weight gradients by TMA in rows of 128 bytes 91, of 64 bytes
-// 100, by lanes 94.  Two pairs of a cluster that load their shared operand once (multicast): 80, 100,
-// 90 and 98, since clusters of four leave eight SMs without work.
+// more.  Stores of the GELU tile, us, with a GELU of fewer terms that takes one less: 64 bytes of a row by
+// lanes 118, four bytes a lane 121, by TMA from a buffer a warp 102, from two 98, from two that two warps
+// share (128 bytes a row) 109, from two for one output at a time 105; sixteen warps 111.  Weight gradients
+// by TMA in rows of 128 bytes 91, of 64 bytes 100, by lanes 94.  Two pairs of a cluster that load their
+// shared operand once (multicast): 80, 100, 90 and 98, since clusters of four leave eight SMs without work.
 #include <cuda.h>
 #include <cuda_fp16.h>
 

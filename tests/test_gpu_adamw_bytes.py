@@ -127,3 +127,19 @@ def test_bytes_beside_borders(shift):
         want = expected(y)
         step([y], 1, True)
         same(y, want)
+
+
+def test_a_square_that_overflows():
+    """A finite gradient whose square is not in fp32: its second moment is lost, in 8 bits its block's moments."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, y = Tensor(700, True, F32, g), Tensor(700, False, F32, g)
+    for z in (x, y):
+        z.at("g")[300] = 1e21
+        step([z], 1, z.small)
+    m, v = x.moments()
+    assert not np.isfinite(m[256:512]).any() and not np.isfinite(v[256:512]).any()
+    for part in (slice(0, 256), slice(512, 700)):
+        assert np.isfinite(m[part]).all() and np.isfinite(v[part]).all()
+    lost = torch.nonzero(~torch.isfinite(y.at("v"))).flatten()
+    assert lost.tolist() == [300] and bool(torch.isfinite(y.at("m")).all())
+    assert bool(torch.isfinite(x.at("w")).all()) and bool(torch.isfinite(y.at("w")).all())  # (a step of 0 there)
